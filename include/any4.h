@@ -49,10 +49,10 @@ extern "C" {
 
 #define ANY4_OK             0
 #define ANY4_ERR_NULL      -1   /* a required pointer is NULL */
-#define ANY4_ERR_SHAPE     -2   /* M, N or K < 1, or K not a multiple of 128 */
-#define ANY4_ERR_BITS      -3   /* bits is not 4, 3 or 2 */
-#define ANY4_ERR_ALIGN     -4   /* a pointer is not 16-byte aligned */
-#define ANY4_ERR_WORKSPACE -5   /* workspace smaller than any4_gemm_workspace_bytes() */
+#define ANY4_ERR_SHAPE     -2   /* M, N or K < 1, or K not a multiple of 128; a size of the cache or of attention out of range */
+#define ANY4_ERR_BITS      -3   /* bits is not 4, 3 or 2 (cache: 16, 8 or 4) */
+#define ANY4_ERR_ALIGN     -4   /* a pointer is not 16-byte aligned, or a stride no multiple of 8 values */
+#define ANY4_ERR_WORKSPACE -5   /* workspace smaller than the entry point's ..._workspace_bytes() */
 #define ANY4_ERR_HIP       -6   /* the HIP runtime refused a launch */
 
 #define ANY4_GROUP 128          /* weights per scale/offset group along K */
@@ -277,6 +277,105 @@ int64_t any4_quantize_max_k(void);
 int any4_gemm_noalloc(const uint16_t* x, const uint32_t* codes, const uint16_t* lut,
                       const uint16_t* scale, const uint16_t* offset,
                       int64_t M, int64_t N, int64_t K, int bits, uint16_t* y, void* stream);
+
+/*
+ * The key-value cache and the attention over it: what lies between the QKV and the O projection of a
+ * decoder layer (section 5 lists those linears), for prompts and for single tokens.  Inference
+ * only, as everything here: there is no backward pass.
+ *
+ * The cache is paged.  k and v are [pages][kv_heads][page_size][head_dim], dense, in 16 bits or as codes:
+ *   bits = 16   bf16 (fp16 with f16 = 1) values; scales is not used and may be NULL
+ *   bits = 8    one byte a value
+ *   bits = 4    two codes a byte, the first in the low half
+ * With 8 and 4 bits every (token, head) of k and of v is a group of its own, scaled as any4_quantize scales
+ * its groups (section 2.5.1, asymmetric): scale = bf16((max - min) / (2^bits - 1)), 1 where that is 0;
+ * offset = bf16(min); code = (x - offset) / scale rounded to the nearest integer, ties to even, within 0 ..
+ * 2^bits - 1; it stands for scale * code + offset.  A group with a value that is not finite, or whose range
+ * is not, has a NaN for scale and offset and reads back as NaN.  scales is bf16 [pages][kv_heads][page_size][4]:
+ * k scale, k offset, v scale, v offset.
+ * Token s of the cache ("slot") is token s % page_size of page s / page_size.
+ *   pages       1 .. 2^31 - 1
+ *   page_size   a power of two, 16 .. 1024
+ *   kv_heads    1 .. 4095; query heads: a multiple of kv_heads, at most 65535
+ *   head_dim    64 or 128
+ *   f16         0: the 16-bit values of every call with this cache are bf16, 1: fp16.  (scales is bf16 in both)
+ * Every pointer must be 16-byte aligned, arrays of int32 and int64 by their own 4 and 8 bytes.  Where inputs come as rows with strides (in values, each a multiple of 8, from a token to
+ * the next and from a head to the next), the head_dim values of a head lie side by side: slices of a fused QKV
+ * projection's output serve as they are.
+ */
+typedef struct any4_kv_cache {
+    void* k;
+    void* v;
+    uint16_t* scales;
+    int64_t pages;
+    int page_size, kv_heads, head_dim, bits, f16;
+} any4_kv_cache;
+
+/*
+ * any4_kv_write - k and v of `tokens` tokens into their slots of the cache.
+ *   k, v     in   16-bit [tokens][kv_heads][head_dim], strided rows
+ *   slots    in   int64 [tokens], each slot at most once; a token whose slot is not one of the cache's (negative, for
+ *                 padding, or too large) is left out
+ * Nothing else in the cache is touched.  tokens = 0 is a call that does nothing.
+ */
+int any4_kv_write(const uint16_t* k, int64_t k_token_stride, int64_t k_head_stride,
+                  const uint16_t* v, int64_t v_token_stride, int64_t v_head_stride,
+                  int64_t tokens, const int64_t* slots, const any4_kv_cache* cache, void* stream);
+
+/*
+ * any4_kv_read - what slots of the cache hold, as packed rows (what any4_attn_prompt takes as the context in front of a
+ * prompt's next part).
+ *   slots    in   int64 [tokens], any order, repeats allowed; a slot that is not one of the cache's reads as zeros
+ *   k, v     out  16-bit [tokens][kv_heads][head_dim], dense, fully overwritten
+ */
+int any4_kv_read(const any4_kv_cache* cache, const int64_t* slots, int64_t tokens, uint16_t* k, uint16_t* v,
+                 void* stream);
+
+/*
+ * any4_attn_decode - one new token of each request attends to the first lengths[r] tokens of its pages:
+ *     s_j = softmax_scale * q . k_j,   out = sum_j softmax(s)_j v_j
+ * Query head h reads KV head h / (heads / kv_heads).  A request without a token gets zeros.  Scores, softmax and sums
+ * are fp32; the weights are rounded to 16 bits for the matrix cores, the result once to the output's type.  The result is
+ * reproducible run to run; its last bits may depend on the page table's width and on the number of requests.
+ *   q           in   16-bit [requests][heads][head_dim], strided rows
+ *   page_table  in   int32 [requests][table_width], rows table_stride entries apart: the pages of a request's tokens in their
+ *                    order.  Entries past a request's last token are not read; one that is not a page of the cache has its
+ *                    tokens left out as if masked (a request without any other gets NaN)
+ *   lengths     in   int32 [requests]; taken as at least 0 and at most table_width * page_size
+ *   out         out  16-bit [requests][heads][head_dim], dense
+ *   workspace   at least any4_attn_decode_workspace_bytes() bytes; may be NULL when that is 0.  What is said of any4_gemm's
+ *               holds here too
+ * The cache behind a request's last token, up to the end of its page, may hold anything, NaN among it.
+ * requests at most 65535, table_width * page_size at most 2^31 - 2048, softmax_scale finite and above 0
+ * (ANY4_ERR_SHAPE).  requests = 0 does nothing.
+ */
+int any4_attn_decode(const uint16_t* q, int64_t q_request_stride, int64_t q_head_stride, const any4_kv_cache* cache,
+                     const int32_t* page_table, int64_t table_stride, int64_t table_width, const int32_t* lengths,
+                     int64_t requests, int heads, float softmax_scale, uint16_t* out,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace any4_attn_decode needs (0 for invalid arguments); max_tokens = table_width * page_size. */
+size_t any4_attn_decode_workspace_bytes(int64_t requests, int heads, int kv_heads, int head_dim, int64_t max_tokens);
+
+/*
+ * any4_attn_prompt - attention of whole prompts, packed one behind the other.  Request r has the rows q_starts[r] ..
+ * q_starts[r + 1] - 1 of q and k_starts[r] .. k_starts[r + 1] - 1 of k and v; where it has more of the latter, the first of them
+ * are its context: with causal = 1 query i of nq sees keys 0 .. i + nk - nq, with causal = 0 all nk.  A query that sees
+ * no key (nk < nq, or nk = 0) gets zeros.  A key that a query does not see has no influence on it, whatever it holds.
+ * Arithmetic as in any4_attn_decode.
+ *   q        in   16-bit [q_tokens][heads][head_dim], k, v 16-bit [k_tokens][kv_heads][head_dim], strided rows (strides
+ *                 below 2^23)
+ *   q_starts, k_starts   in   int32 [requests + 1], ascending; values are taken as at least 0 and at most q_tokens / k_tokens
+ *   f16      0: bf16, 1: fp16
+ *   out      out  16-bit [q_tokens][heads][head_dim], dense; rows that no request has are left as they are
+ * Requests and tokens may be 0 in number (then nothing is done).  Needs no workspace.
+ */
+int any4_attn_prompt(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride,
+                     const uint16_t* k, int64_t k_token_stride, int64_t k_head_stride,
+                     const uint16_t* v, int64_t v_token_stride, int64_t v_head_stride,
+                     int64_t q_tokens, int64_t k_tokens, const int32_t* q_starts, const int32_t* k_starts,
+                     int64_t requests, int heads, int kv_heads, int head_dim, int f16, int causal,
+                     float softmax_scale, uint16_t* out, void* stream);
 
 /* Static, human-readable text for a return code. */
 const char* any4_strerror(int code);

@@ -19,11 +19,19 @@ LIB_PATH = os.path.join(_PKG, "libany4.so")
 GROUP = 128
 
 EXPORTS = ("any4_pack", "any4_dequant", "any4_gemm", "any4_gemm_workspace_bytes", "any4_repack", "any4_repack_bytes", "any4_gemm_repacked", "any4_dequant_grouped", "any4_gemm_grouped", "any4_dequant_f16", "any4_gemm_f16",
-           "any4_quantize", "any4_quantize_with_gap", "any4_quantize_max_k", "any4_gemm_noalloc", "any4_dequant_single_table", "any4_gemm_single_table", "any4_strerror", "any4_version")
+           "any4_quantize", "any4_quantize_with_gap", "any4_quantize_max_k", "any4_gemm_noalloc", "any4_dequant_single_table", "any4_gemm_single_table",
+           "any4_kv_write", "any4_kv_read", "any4_attn_decode", "any4_attn_decode_workspace_bytes", "any4_attn_prompt", "any4_strerror", "any4_version")
 
 
 class Any4Error(RuntimeError):
     pass
+
+
+class _KvCache(ctypes.Structure):
+    """any4_kv_cache of include/any4.h"""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("pages", ctypes.c_int64),
+                ("page_size", ctypes.c_int), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("bits", ctypes.c_int),
+                ("f16", ctypes.c_int)]
 
 
 _lib = None
@@ -74,6 +82,17 @@ def load_library() -> ctypes.CDLL:
     lib.any4_quantize_with_gap.argtypes = [vp, vp, vp, i64, i64, ci, ci, ci, ctypes.c_double, vp, vp, vp, vp, vp, vp]
     lib.any4_quantize_max_k.restype = i64
     lib.any4_quantize_max_k.argtypes = []
+    cache, f32 = ctypes.POINTER(_KvCache), ctypes.c_float
+    lib.any4_kv_write.restype = ci
+    lib.any4_kv_write.argtypes = [vp, i64, i64, vp, i64, i64, i64, vp, cache, vp]
+    lib.any4_kv_read.restype = ci
+    lib.any4_kv_read.argtypes = [cache, vp, i64, vp, vp, vp]
+    lib.any4_attn_decode.restype = ci
+    lib.any4_attn_decode.argtypes = [vp, i64, i64, cache, vp, i64, i64, vp, i64, ci, f32, vp, vp, ctypes.c_size_t, vp]
+    lib.any4_attn_decode_workspace_bytes.restype = ctypes.c_size_t
+    lib.any4_attn_decode_workspace_bytes.argtypes = [i64, ci, ci, ci, i64]
+    lib.any4_attn_prompt.restype = ci
+    lib.any4_attn_prompt.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, i64, i64, vp, vp, i64, ci, ci, ci, ci, ci, f32, vp, vp]
     lib.any4_strerror.restype = ctypes.c_char_p
     lib.any4_strerror.argtypes = [ci]
     lib.any4_version.restype = ci
@@ -362,3 +381,166 @@ def any4_quantize(w: torch.Tensor, act: torch.Tensor | None, u: torch.Tensor, bi
                                           codes.data_ptr(), lut.data_ptr(), scale.data_ptr(), offset.data_ptr(),
                                           msteps.data_ptr(), _stream()), "any4_quantize_with_gap")
     return {"codes_u8": codes, "lut": lut, "scale": scale, "offset": offset, "msteps": msteps}
+
+
+# The key-value cache and the attention over it
+
+def any4_kv_cache(pages: int, kv_heads: int, head_dim: int, page_size: int = 64, bits: int = 16, dtype: torch.dtype = torch.bfloat16,
+                  device="cuda"):
+    """(cache_k, cache_v, scales) of a paged cache, zeros: [pages, kv_heads, page_size, head_dim] of dtype with 16 bits, with 8 and 4
+    bits codes (uint8, two to a byte with 4) and bf16 scales [pages, kv_heads, page_size, 4]; scales is None with 16 bits."""
+    if bits not in (16, 8, 4):
+        raise Any4Error(f"bits must be 16, 8 or 4, got {bits}")
+    shape = (pages, kv_heads, page_size, head_dim if bits == 16 else head_dim * bits // 8)
+    k, v = (torch.zeros(shape, dtype=dtype if bits == 16 else torch.uint8, device=device) for _ in range(2))
+    return k, v, None if bits == 16 else torch.zeros((pages, kv_heads, page_size, 4), dtype=torch.bfloat16, device=device)
+
+
+def _rows(t, dtype, name: str, shape) -> tuple[int, int, int]:
+    """address and strides of rows [tokens, heads, head_dim]: a head's values side by side, the rest as it comes"""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise Any4Error(f"{name} must be a tensor in device memory")
+    if t.dtype != dtype:
+        raise Any4Error(f"{name} must have dtype {dtype}, got {t.dtype}")
+    _shape(t, shape, name)
+    if t.stride(2) != 1:
+        raise Any4Error(f"{name}: the values of a head must lie side by side")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _same_device(first, *others) -> None:
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise Any4Error(f"all tensors must be on one device, got {first.device} and {t.device}")
+
+
+def _cache(cache_k, cache_v, scales, bits: int, dtype) -> tuple[_KvCache, int, int]:
+    """the C structure, KV heads and head_dim"""
+    if bits not in (16, 8, 4):
+        raise Any4Error(f"bits must be 16, 8 or 4, got {bits}")
+    if dtype not in (torch.bfloat16, torch.float16):
+        raise Any4Error(f"the 16-bit values must be bf16 or fp16, got {dtype}")
+    if not isinstance(cache_k, torch.Tensor) or cache_k.dim() != 4:
+        raise Any4Error("cache_k must be a tensor of 4 dimensions: pages, kv_heads, page_size, head_dim (codes: bytes)")
+    held = dtype if bits == 16 else torch.uint8
+    pk, pv = _dev(cache_k, held, "cache_k"), _dev(cache_v, held, "cache_v")
+    _shape(cache_v, cache_k.shape, "cache_v")
+    pages, heads, page, width = cache_k.shape
+    ps = None
+    if bits != 16:
+        ps = _dev(scales, torch.bfloat16, "scales")
+        _shape(scales, (pages, heads, page, 4), "scales")
+    _same_device(cache_k, cache_v, scales if bits != 16 else None)
+    dim = width if bits == 16 else width * 8 // bits
+    return _KvCache(pk, pv, ps, pages, page, heads, dim, bits, int(dtype == torch.float16)), heads, dim
+
+
+def any4_kv_write(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tensor,
+                  scales: torch.Tensor | None = None, bits: int = 16) -> None:
+    """k, v [tokens, kv_heads, head_dim] (bf16 or fp16; slices of a fused projection's rows serve as they are) into slots
+    (int64 [tokens]; a slot outside the cache leaves its token out) of the cache, with 8 and 4 bits quantised on the way."""
+    lib = load_library()
+    if not isinstance(k, torch.Tensor):
+        raise Any4Error("k must be a tensor in device memory")
+    cache, heads, dim = _cache(cache_k, cache_v, scales, bits, k.dtype)
+    shape = (slots.shape[0] if isinstance(slots, torch.Tensor) and slots.dim() == 1 else -1, heads, dim)
+    ptr = _dev(slots, torch.int64, "slots")
+    if shape[0] < 0:
+        raise Any4Error("slots must have one dimension")
+    pk, pv = _rows(k, k.dtype, "k", shape), _rows(v, k.dtype, "v", shape)
+    _same_device(k, v, slots, cache_k)
+    _check(lib.any4_kv_write(*pk, *pv, shape[0], ptr, ctypes.byref(cache), _stream()), "any4_kv_write")
+
+
+def any4_kv_read(cache_k: torch.Tensor, cache_v: torch.Tensor, slots: torch.Tensor, scales: torch.Tensor | None = None, bits: int = 16,
+                 dtype: torch.dtype = torch.bfloat16, out: tuple[torch.Tensor, torch.Tensor] | None = None):
+    """(k, v) [tokens, kv_heads, head_dim] of slots (int64 [tokens]) of the cache, in dtype (the cache's own with 16 bits); zeros
+    for a slot outside the cache."""
+    lib = load_library()
+    cache, heads, dim = _cache(cache_k, cache_v, scales, bits, dtype)
+    ptr = _dev(slots, torch.int64, "slots")
+    if slots.dim() != 1:
+        raise Any4Error("slots must have one dimension")
+    n = slots.shape[0]
+    k, v = out if out is not None else (torch.empty((n, heads, dim), dtype=dtype, device=cache_k.device) for _ in range(2))
+    pk, pv = _dev(k, dtype, "out[0]"), _dev(v, dtype, "out[1]")
+    _shape(k, (n, heads, dim), "out[0]")
+    _shape(v, (n, heads, dim), "out[1]")
+    _same_device(cache_k, slots, k, v)
+    _check(lib.any4_kv_read(ctypes.byref(cache), ptr, n, pk, pv, _stream()), "any4_kv_read")
+    return k, v
+
+
+def any4_attn_decode_workspace_bytes(requests: int, heads: int, kv_heads: int, head_dim: int, max_tokens: int) -> int:
+    return int(load_library().any4_attn_decode_workspace_bytes(requests, heads, kv_heads, head_dim, max_tokens))
+
+
+def any4_attn_decode(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
+                     scales: torch.Tensor | None = None, bits: int = 16, softmax_scale: float | None = None,
+                     out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """[requests, heads, head_dim]: the newest token of each request (q, of that shape; slices of a fused projection's rows serve as
+    they are) attends to the first lengths[r] (int32 [requests]) tokens of its pages (page_table, int32 [requests, table_width]) in
+    the cache.  Query head h reads KV head h // (heads // kv_heads); softmax_scale is head_dim ** -0.5 unless given."""
+    lib = load_library()
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise Any4Error("q must be a tensor of 3 dimensions: requests, heads, head_dim")
+    n, heads = q.shape[:2]
+    cache, kv_heads, dim = _cache(cache_k, cache_v, scales, bits, q.dtype)
+    pq = _rows(q, q.dtype, "q", (n, heads, dim))
+    if heads < 1 or kv_heads < 1 or heads % kv_heads:
+        raise Any4Error(f"{heads} query heads are no multiple of {kv_heads} KV heads")
+    if not isinstance(page_table, torch.Tensor) or not page_table.is_cuda or page_table.dtype != torch.int32:
+        raise Any4Error("page_table must be an int32 tensor in device memory")
+    if page_table.dim() != 2 or page_table.shape[0] != n or page_table.stride(1) != 1:
+        raise Any4Error(f"page_table must have {n} rows of page numbers that lie side by side, got shape {tuple(page_table.shape)}")
+    pl = _dev(lengths, torch.int32, "lengths")
+    _shape(lengths, (n,), "lengths")
+    if out is None:
+        out = torch.empty((n, heads, dim), dtype=q.dtype, device=q.device)
+    _shape(out, (n, heads, dim), "out")
+    po = _dev(out, q.dtype, "out")
+    _same_device(q, cache_k, page_table, lengths, out)
+    width = page_table.shape[1]
+    need = int(lib.any4_attn_decode_workspace_bytes(n, heads, kv_heads, dim, width * cache.page_size))
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    pw, wbytes = _scratch(workspace, q.device) if workspace is not None else (None, 0)
+    _check(lib.any4_attn_decode(*pq, ctypes.byref(cache), page_table.data_ptr(), page_table.stride(0), width, pl, n, heads,
+                                dim ** -0.5 if softmax_scale is None else softmax_scale, po, pw, wbytes, _stream()), "any4_attn_decode")
+    return out
+
+
+def any4_attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts: torch.Tensor, k_starts: torch.Tensor | None = None,
+                     causal: bool = True, softmax_scale: float | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """[q_tokens, heads, head_dim]: packed prompts, request r in rows q_starts[r] .. q_starts[r + 1] - 1 of q and k_starts[r] .. of k and v
+    [k_tokens, kv_heads, head_dim] (int32 [requests + 1]; k_starts None: q_starts).  Where a request has more rows in k, the first
+    of them are the context in front of its queries: causal, query i of nq sees keys 0 .. i + nk - nq."""
+    lib = load_library()
+    for t, name in ((q, "q"), (k, "k"), (v, "v")):
+        if not isinstance(t, torch.Tensor) or t.dim() != 3:
+            raise Any4Error(f"{name} must be a tensor of 3 dimensions: tokens, heads, head_dim")
+    if q.dtype not in (torch.bfloat16, torch.float16):
+        raise Any4Error(f"q must be bf16 or fp16, got {q.dtype}")
+    n, heads, dim = q.shape
+    kv_heads = k.shape[1]
+    if heads < 1 or kv_heads < 1 or heads % kv_heads:
+        raise Any4Error(f"{heads} query heads are no multiple of {kv_heads} KV heads")
+    pq, pk, pv = _rows(q, q.dtype, "q", q.shape), _rows(k, q.dtype, "k", (k.shape[0], kv_heads, dim)), _rows(v, q.dtype, "v", (k.shape[0], kv_heads, dim))
+    ps = _dev(q_starts, torch.int32, "q_starts")
+    if q_starts.dim() != 1 or q_starts.shape[0] < 1:
+        raise Any4Error("q_starts must have one entry for each request and one more")
+    if k_starts is None:
+        if k.shape[0] != n:
+            raise Any4Error(f"without k_starts k has as many rows as q, {n}, got {k.shape[0]}")
+        k_starts = q_starts
+    pt = _dev(k_starts, torch.int32, "k_starts")
+    _shape(k_starts, q_starts.shape, "k_starts")
+    if out is None:
+        out = torch.empty((n, heads, dim), dtype=q.dtype, device=q.device)
+    _shape(out, (n, heads, dim), "out")
+    po = _dev(out, q.dtype, "out")
+    _same_device(q, k, v, q_starts, k_starts, out)
+    _check(lib.any4_attn_prompt(*pq, *pk, *pv, n, k.shape[0], ps, pt, q_starts.shape[0] - 1, heads, kv_heads, dim,
+                                int(q.dtype == torch.float16), int(causal), dim ** -0.5 if softmax_scale is None else softmax_scale, po, _stream()),
+           "any4_attn_prompt")
+    return out

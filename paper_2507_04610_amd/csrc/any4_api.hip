@@ -309,10 +309,10 @@ const char* any4_strerror(int code) {
     switch (code) {
         case ANY4_OK: return "ok";
         case ANY4_ERR_NULL: return "a required pointer is NULL";
-        case ANY4_ERR_SHAPE: return "bad shape: M, N, K must be >= 1 and K a multiple of 128";
-        case ANY4_ERR_BITS: return "bits must be 4, 3 or 2";
-        case ANY4_ERR_ALIGN: return "a pointer is not 16-byte aligned";
-        case ANY4_ERR_WORKSPACE: return "workspace is missing or smaller than any4_gemm_workspace_bytes()";
+        case ANY4_ERR_SHAPE: return "bad shape: GEMM and quantiser take M, N, K >= 1 and K a multiple of 128, cache and attention the sizes that any4.h lists";
+        case ANY4_ERR_BITS: return "bits must be 4, 3 or 2 (key-value cache: 16, 8 or 4)";
+        case ANY4_ERR_ALIGN: return "a pointer is not 16-byte aligned or a stride no multiple of 8 values";
+        case ANY4_ERR_WORKSPACE: return "workspace is missing or smaller than the entry point's ..._workspace_bytes()";
         case ANY4_ERR_HIP: return "the HIP runtime refused a kernel launch";
         default: return "unknown any4 error code";
     }

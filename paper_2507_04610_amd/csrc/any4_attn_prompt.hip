@@ -1,0 +1,297 @@
+// any4_attn_prompt: attention of packed prompts, causal or not, query heads sharing KV heads.
+//
+//     s_ij = scale q_i . k_j,   o_i = sum_j exp(s_ij - m_i) v_j / sum_j exp(s_ij - m_i)
+// in one pass over the keys with a running maximum m_i; neither scores nor weights leave the registers.
+// Two matrix products of 2 D operations a score bound it, beside the exponential and its sums on the vector units.
+//
+// A block takes 128 queries of one head, a wavefront 32 of them, and walks over the keys 64 at a time.  k and v are copied to
+// LDS without passing registers, the next 64 while these are worked on.  S^T = K Q^T with v_mfma_f32_32x32x16: a query's
+// scores then lie in two lanes, a maximum is one exchange, and the weights are at once the B operand of O^T = V^T P^T, whose keys are
+// taken in the order in which the lanes have them (lane half g: keys 4 g .. 4 g + 3 and 8 + 4 g .. of every 16).  V^T's operand comes
+// out of the row-major tile by transposing LDS reads.  Tiles are swizzled in pieces of 16 bytes so that 16 (k) or 4 (v)
+// neighbouring rows' pieces lie in different banks.
+//
+// The maximum in use is raised only when a score exceeds it by 2^kSlack, which spares nearly all rescaling of o: weights of
+// up to 2^kSlack lose nothing in floating point.
+//
+// Rounding: scores, maxima, sums and accumulators are fp32; the weights are rounded to 16 bits for the matrix cores, once.
+#include "any4_attn.h"
+#include "any4_internal.h"
+#include "any4_lds_copy.h"
+
+namespace any4 {
+
+namespace {
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves, kKeys = 64;
+constexpr float kSlack = 8.0f;
+
+#pragma clang diagnostic ignored "-Wint-to-pointer-cast"          // LDS offsets as pointers
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) u32x4* lds_u4;
+typedef __attribute__((address_space(3))) u32x2* lds_u2;
+typedef __attribute__((address_space(3))) s16x4* lds_s4;
+
+struct Args {
+    Rows q, k, v;
+    const int32_t* q_starts;
+    const int32_t* k_starts;
+    int q_tokens, k_tokens, requests, heads, kv_heads, shared, causal;
+    float scale_log2;
+    uint16_t* out;
+};
+
+// 4 rows x 16 columns: lane i of 16 gives the address of row i / 4, columns 4 * (i % 4) .., and gets column i of the four rows
+__device__ __forceinline__ u32x2 lds_read_transposed(uint32_t at) {
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at)));
+}
+
+// the part of a tile that a wavefront copies: 16-byte pieces, 64 an instruction
+template <int D> struct Tile {
+    static constexpr int kRow = 2 * D, kBytes = kKeys * kRow, kPieces = D / 8, kRows = 64 / kPieces;     // rows an instruction
+    static constexpr int kCopies = kKeys / kRows / kWaves;                                                // of a wavefront
+    __device__ static __forceinline__ int swizzle_k(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+    __device__ static __forceinline__ int swizzle_v(int row) { return D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; }
+};
+
+template <int D, bool F16>
+__global__ __launch_bounds__(kThreads, 2) void attn_prompt_kernel(Args a) {
+    using T = Tile<D>;
+    constexpr int QM = D / 16, OM = D / 32, ROWS = 32 * kWaves;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 31, g = lane >> 5;
+
+    // KV heads fastest: blocks that read the same keys tend to share an XCD and its L2
+    const unsigned rest = blockIdx.x / (unsigned)a.kv_heads, kv_head = blockIdx.x - rest * (unsigned)a.kv_heads;
+    const unsigned place = rest / (unsigned)a.shared;
+    const int head = (int)(kv_head * (unsigned)a.shared + (rest - place * (unsigned)a.shared));
+
+    // which request's tile this is
+    int request = -1, tile = 0, lq = 0, q_at = 0;
+    for (int r0 = 0, before = 0; r0 < a.requests && request < 0; r0 += 64) {
+        const int r = min(r0 + lane, a.requests - 1);
+        const int s0 = min(max(a.q_starts[r], 0), a.q_tokens), s1 = min(max(a.q_starts[r + 1], 0), a.q_tokens);
+        const int rows = r0 + lane < a.requests ? max(s1 - s0, 0) : 0, tiles = (rows + ROWS - 1) / ROWS;
+        int sum = tiles;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int u = __shfl_up(sum, d);
+            if (lane >= d) sum += u;
+        }
+        const unsigned long long past = __builtin_amdgcn_ballot_w64(before + sum > (int)place);
+        if (past) {
+            const int f = __builtin_ctzll(past);
+            request = r0 + f;
+            lq = __builtin_amdgcn_readlane(rows, f);
+            q_at = __builtin_amdgcn_readlane(s0, f);
+            const int all = __builtin_amdgcn_readlane(tiles, f);
+            tile = (int)place - (before + __builtin_amdgcn_readlane(sum, f) - all);
+            if (a.causal) tile = all - 1 - tile;               // the most keys first
+        }
+        before += __builtin_amdgcn_readlane(sum, 63);
+    }
+    if (request < 0) return;
+    const int k_at = min(max(a.k_starts[request], 0), a.k_tokens);
+    const int lk = max(min(max(a.k_starts[request + 1], 0), a.k_tokens) - k_at, 0);
+    const int q0 = tile * ROWS, q_wave = q0 + 32 * wave, query = q_wave + n;
+    const int ahead = lk - lq;                                  // query i sees keys 0 .. i + ahead
+    const int end = a.causal ? min(lk, min(q0 + ROWS, lq) + ahead) : lk;          // of the block's keys
+    const int tiles = end > 0 ? (end + kKeys - 1) / kKeys : 0;
+    const int lim = a.causal ? min(query + ahead, lk - 1) : lk - 1;                // last key of this lane's query
+
+    u32x4 q[QM];
+    {
+        const uint16_t* qp = a.q.p + (int64_t)(q_at + min(query, lq - 1)) * a.q.token + (int64_t)head * a.q.head + 8 * g;
+#pragma unroll
+        for (int i = 0; i < QM; ++i) q[i] = *reinterpret_cast<const u32x4*>(qp + 16 * i);
+    }
+
+    // copies: lane -> row and piece of each instruction; LDS has piece c of row r at c ^ swizzle(r)
+    const char* k_base = reinterpret_cast<const char*>(a.k.p + (int64_t)k_at * a.k.token + (int64_t)kv_head * a.k.head);
+    const char* v_base = reinterpret_cast<const char*>(a.v.p + (int64_t)k_at * a.v.token + (int64_t)kv_head * a.v.head);
+    const uint32_t k_step = (uint32_t)a.k.token * 2u, v_step = (uint32_t)a.v.token * 2u;
+    auto copy = [&](int t, int buffer) {
+        const int k0 = t * kKeys;
+        const char* kb = k_base + (int64_t)k0 * k_step;
+        const char* vb = v_base + (int64_t)k0 * v_step;
+#pragma unroll
+        for (int j = 0; j < T::kCopies; ++j) {
+            const int at = T::kCopies * wave + j, row = at * T::kRows + lane / T::kPieces, piece = lane % T::kPieces;
+            const uint32_t from = (uint32_t)min(row, lk - 1 - k0);          // (rows past the last are copies of it; they are masked)
+            copy_to_lds(buffer * 2 * T::kBytes + at * 1024, kb, from * k_step + 16u * (uint32_t)(piece ^ T::swizzle_k(row)));
+            copy_to_lds(buffer * 2 * T::kBytes + T::kBytes + at * 1024, vb, from * v_step + 16u * (uint32_t)(piece ^ T::swizzle_v(row)));
+        }
+    };
+
+    // operand addresses within a buffer
+    const uint32_t k_lane = (uint32_t)(n * T::kRow), k_swz = (uint32_t)((g ^ T::swizzle_k(n)) << 4);
+    const int i16 = lane & 15, v_row = 4 * g + (i16 >> 2);
+    const uint32_t v_lane = (uint32_t)(T::kBytes + v_row * T::kRow + 8 * (i16 & 1)),
+                   v_swz = (uint32_t)(((2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1)) ^ T::swizzle_v(v_row)) << 4);
+
+    float m_ref = -__builtin_inff(), l = 0.0f;
+    f32x16 o[OM];
+#pragma unroll
+    for (int m = 0; m < OM; ++m)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[m][r] = 0.0f;
+
+    // MASKED: some query of the block may not see some key of the tile
+    auto step = [&](int t, auto masked_tile) {
+        constexpr bool MASKED = decltype(masked_tile)::value;
+        loads_left<0>();
+        lds_barrier();                                          // tile t is there, and nobody reads the other buffer any more
+        if (t + 1 < tiles) copy(t + 1, (t + 1) & 1);
+        const int k0 = t * kKeys;
+        const uint32_t buf = (uint32_t)((t & 1) * 2 * T::kBytes);
+        if (MASKED && a.causal && k0 > q_wave + 31 + ahead) return;     // no query of this wavefront sees it
+        f32x16 s[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[u][r] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < QM; ++i) {
+                const u32x4 k = *(lds_u4)(buf + k_lane + u * 32 * T::kRow + (k_swz ^ (uint32_t)(i << 5)));
+                s[u] = mma32<F16>(k, q[i], s[u]);
+            }
+        }
+        if constexpr (MASKED) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    s[u][r] = k0 + 32 * u + 8 * (r >> 2) + 4 * g + (r & 3) <= lim ? s[u][r] : -__builtin_inff();
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
+        top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
+        if (__builtin_amdgcn_ballot_w64(top > m_ref + kSlack || (m_ref == -__builtin_inff() && top > m_ref))) {
+            const float m_new = fmaxf(m_ref, top);
+            const float alpha = m_new > m_ref ? exp2_fast(m_ref - m_new) : 1.0f;
+            m_ref = m_new;
+            l *= alpha;
+#pragma unroll
+            for (int m = 0; m < OM; ++m) o[m] *= alpha;
+        }
+        const float m_use = m_ref == -__builtin_inff() ? 0.0f : m_ref;
+        u32x4 p[4];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) {
+                const float x = exp2_fast(fmaf(s[u][r], a.scale_log2, -m_use)), y = exp2_fast(fmaf(s[u][r + 1], a.scale_log2, -m_use));
+                l += x + y;
+                p[2 * u + (r >> 3)][(r >> 1) & 3] = f32x2_to_h16x2<F16>(x, y);
+            }
+        auto v_operand = [&](int c, int m) -> u32x4 {
+            const uint32_t at = buf + v_lane + c * 16 * T::kRow + (v_swz ^ (uint32_t)(m << 6));
+            const u32x2 lo = lds_read_transposed(at), hi = lds_read_transposed(at + 8 * T::kRow);
+            return u32x4{lo[0], lo[1], hi[0], hi[1]};
+        };
+        if constexpr (!MASKED) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int m = 0; m < OM; ++m) o[m] = mma32<F16>(v_operand(c, m), p[c], o[m]);
+        } else {
+            // A key that some query does not see has weight 0 for it, and 0 times what is not finite would be NaN: keys with such
+            // values are taken out of the product and added one by one to the queries that see them.
+            constexpr uint32_t kExp = F16 ? 0x7C007C00u : 0x7F807F80u, kOne = F16 ? 0x04000400u : 0x00800080u;
+            unsigned long long bad = 0ull;                      // bit 16 c + 8 half + slot
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+                uint32_t bits[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+                for (int m = 0; m < OM; ++m) {
+                    const u32x4 v = v_operand(c, m);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) bits[w] |= (v[w] & kExp) + kOne;       // (an exponent of all ones carries into the half's top bit)
+                }
+                if (__builtin_amdgcn_ballot_w64(((bits[0] | bits[1] | bits[2] | bits[3]) & 0x80008000u) != 0u) == 0ull) continue;
+                uint32_t some = 0u;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const unsigned long long lanes = __builtin_amdgcn_ballot_w64((bits[j >> 1] >> (16 * (j & 1) + 15)) & 1u);
+                    some |= ((uint32_t)lanes != 0u ? 1u : 0u) << j | ((uint32_t)(lanes >> 32) != 0u ? 1u : 0u) << (8 + j);
+                }
+                bad |= (unsigned long long)some << (16 * c);
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const uint32_t mine = (uint32_t)(bad >> (16 * c)) >> (8 * g);
+                u32x4 keep;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) keep[w] = ((mine >> (2 * w)) & 1u ? 0u : 0xFFFFu) | ((mine >> (2 * w + 1)) & 1u ? 0u : 0xFFFF0000u);
+#pragma unroll
+                for (int m = 0; m < OM; ++m) o[m] = mma32<F16>(v_operand(c, m) & keep, p[c], o[m]);
+            }
+#pragma unroll 1
+            while (bad) {
+                const int b = __builtin_ctzll(bad), c = b >> 4, half = (b >> 3) & 1, slot = b & 7;
+                bad &= bad - 1;
+                const int row = 16 * c + (slot < 4 ? 4 * half + slot : 4 + 4 * half + slot);
+                uint32_t pair = 0u;
+#pragma unroll
+                for (int x = 0; x < 16; ++x) pair = x == 4 * c + (slot >> 1) ? p[x >> 2][x & 3] : pair;
+                const float mine = slot & 1 ? h16hi_to_f32<F16>(pair) : h16lo_to_f32<F16>(pair), other = __shfl_xor(mine, 32);
+                const float weight = g == half ? mine : other;
+                const bool seen = k0 + row <= lim;
+#pragma unroll
+                for (int m = 0; m < OM; ++m)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const uint32_t piece = (uint32_t)((4 * m + r) ^ T::swizzle_v(row));
+                        const u32x2 v = *(lds_u2)(buf + (uint32_t)T::kBytes + (uint32_t)(row * T::kRow) + 16u * piece + 8u * (uint32_t)g);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float x = e & 1 ? h16hi_to_f32<F16>(v[e >> 1]) : h16lo_to_f32<F16>(v[e >> 1]);
+                            o[m][4 * r + e] = seen ? fmaf(weight, x, o[m][4 * r + e]) : o[m][4 * r + e];
+                        }
+                    }
+            }
+        }
+    };
+    const int whole = min(tiles, max(a.causal ? min(lk, q0 + ahead + 1) : lk, 0) / kKeys);
+    if (tiles > 0) copy(0, 0);
+    for (int t = 0; t < whole; ++t) step(t, std::false_type{});
+    for (int t = whole; t < tiles; ++t) step(t, std::true_type{});
+
+    l += __shfl_xor(l, 32);
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;              // (no key seen: o is 0 as well)
+    if (query < lq) {
+        uint16_t* out = a.out + ((int64_t)(q_at + query) * a.heads + head) * D + 4 * g;
+#pragma unroll
+        for (int m = 0; m < OM; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                *reinterpret_cast<u32x2*>(out + 32 * m + 8 * r) =
+                    u32x2{f32x2_to_h16x2<F16>(o[m][4 * r] * inv, o[m][4 * r + 1] * inv), f32x2_to_h16x2<F16>(o[m][4 * r + 2] * inv, o[m][4 * r + 3] * inv)};
+    }
+}
+
+template <int D, bool F16> hipError_t launch(const Args& a, int64_t blocks, hipStream_t stream) {
+    constexpr auto kernel = attn_prompt_kernel<D, F16>;
+    constexpr int bytes = 4 * Tile<D>::kBytes;
+    if (hipError_t e = ensure_lds<kernel>(bytes); e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), bytes, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_prompt(const PromptArgs& p, hipStream_t stream) {
+    Args a{p.q, p.k, p.v, p.q_starts, p.k_starts, (int)p.q_tokens, (int)p.k_tokens, p.requests, p.heads, p.kv_heads, p.heads / p.kv_heads,
+           p.causal, p.softmax_scale * kLog2e, p.out};
+    // a tile of each request may be short; those that no request has end at once
+    const int64_t places = p.q_tokens / (32 * kWaves) + (p.requests < p.q_tokens ? p.requests : p.q_tokens);
+    const int64_t blocks = places * p.heads;
+    if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (p.head_dim == 128) return p.f16 ? launch<128, true>(a, blocks, stream) : launch<128, false>(a, blocks, stream);
+    return p.f16 ? launch<64, true>(a, blocks, stream) : launch<64, false>(a, blocks, stream);
+}
+
+}  // namespace any4
