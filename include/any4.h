@@ -290,7 +290,7 @@ int any4_gemm_noalloc(const uint16_t* x, const uint32_t* codes, const uint16_t* 
  * With 8 and 4 bits every (token, head) of k and of v is a group of its own, scaled as any4_quantize scales
  * its groups (section 2.5.1, asymmetric): scale = bf16((max - min) / (2^bits - 1)), 1 where that is 0;
  * offset = bf16(min); code = (x - offset) / scale rounded to the nearest integer, ties to even, within 0 ..
- * 2^bits - 1; it stands for scale * code + offset.  A group with a value that is not finite, or whose range
+ * 2^bits - 1; it stands for scale * code + offset (read as fp16: within +- 65504).  A group with a value that is not finite, or whose range
  * is not, has a NaN for scale and offset and reads back as NaN.  scales is bf16 [pages][kv_heads][page_size][4]:
  * k scale, k offset, v scale, v offset.
  * Token s of the cache ("slot") is token s % page_size of page s / page_size.

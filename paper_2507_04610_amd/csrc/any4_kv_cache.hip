@@ -88,7 +88,7 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(Rows k, Rows v, int6
     }
 }
 
-// value = scale * code + offset in fp32 (the product is exact), rounded once
+// value = scale * code + offset in fp32 (the product is exact), rounded once, within the type's range
 template <int BITS, bool F16> __device__ __forceinline__ u32x4 decode(const u32x2& w, uint32_t scale_offset) {
     const float s = bf16lo_to_f32(scale_offset), o = bf16hi_to_f32(scale_offset);
     float x[8];
@@ -96,6 +96,7 @@ template <int BITS, bool F16> __device__ __forceinline__ u32x4 decode(const u32x
     for (int j = 0; j < 8; ++j) {
         const uint32_t c = BITS == 8 ? (w[j >> 2] >> (8 * (j & 3))) & 0xFFu : (w[0] >> (4 * j)) & 0xFu;
         x[j] = fmaf((float)c, s, o);
+        if (F16 && fabsf(x[j]) > 65504.0f) x[j] = copysignf(65504.0f, x[j]);       // (a bf16 offset may lie outside of fp16's range)
     }
     return u32x4{f32x2_to_h16x2<F16>(x[0], x[1]), f32x2_to_h16x2<F16>(x[2], x[3]), f32x2_to_h16x2<F16>(x[4], x[5]),
                  f32x2_to_h16x2<F16>(x[6], x[7])};
