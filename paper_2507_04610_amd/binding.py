@@ -36,12 +36,13 @@ class _KvCache(ctypes.Structure):
 
 _lib = None
 _native_gemm = None          # the native call (_any4_torch.gemm) once the library is loaded
+_native_calls = None         # the native calls of the cache and of attention (_any4_torch), likewise
 
 
 def load_library() -> ctypes.CDLL:
     """Load libany4.so from the package directory (build it with
     `python -m paper_2507_04610_amd.build`); raises if it is not there."""
-    global _lib, _native_gemm
+    global _lib, _native_gemm, _native_calls
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -99,11 +100,12 @@ def load_library() -> ctypes.CDLL:
     lib.any4_version.argtypes = []
     problem = None
     try:
-        from ._any4_torch import gemm
+        from . import _any4_torch as native
+        gemm, calls = native.gemm, native
     except ImportError as e:
         # built for another torch, or not built: the checked calls run the same kernels, only the call costs more
-        gemm, problem = _no_native_gemm, str(e)
-    _native_gemm = gemm
+        gemm, calls, problem = _no_native_gemm, _NoNativeCalls, str(e)
+    _native_gemm, _native_calls = gemm, calls
     _lib = lib                   # last: another thread that sees it finds the call as well
     if problem:
         warnings.warn(f"the torch extension beside {LIB_PATH} does not load ({problem}): GEMM calls go through ctypes; "
@@ -114,6 +116,19 @@ def load_library() -> ctypes.CDLL:
 def _no_native_gemm(*args):
     """in the place of the native call where its extension does not load: never a plain valid call"""
     return None
+
+
+class _NoNativeCalls:
+    """the same for the cache and attention"""
+    kv_write = kv_read = attn_decode = attn_prompt = staticmethod(_no_native_gemm)
+
+
+def _calls():
+    """the native calls (csrc/any4_torch.cpp): each gives its result, None with nothing done where a call is not a plain valid
+    one (the checked call then names what is wrong), or a code from the runtime"""
+    if _native_calls is None:
+        load_library()
+    return _native_calls
 
 
 def _check(rc: int, what: str) -> None:
@@ -439,6 +454,11 @@ def any4_kv_write(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache_k
                   scales: torch.Tensor | None = None, bits: int = 16) -> None:
     """k, v [tokens, kv_heads, head_dim] (bf16 or fp16; slices of a fused projection's rows serve as they are) into slots
     (int64 [tokens]; a slot outside the cache leaves its token out) of the cache, with 8 and 4 bits quantised on the way."""
+    r = _calls().kv_write(k, v, slots, cache_k, cache_v, scales, bits)
+    if r is not None:
+        if r.__class__ is int:
+            _check(r, "any4_kv_write")
+        return
     lib = load_library()
     if not isinstance(k, torch.Tensor):
         raise Any4Error("k must be a tensor in device memory")
@@ -456,6 +476,12 @@ def any4_kv_read(cache_k: torch.Tensor, cache_v: torch.Tensor, slots: torch.Tens
                  dtype: torch.dtype = torch.bfloat16, out: tuple[torch.Tensor, torch.Tensor] | None = None):
     """(k, v) [tokens, kv_heads, head_dim] of slots (int64 [tokens]) of the cache, in dtype (the cache's own with 16 bits); zeros
     for a slot outside the cache."""
+    if dtype is torch.bfloat16 or dtype is torch.float16:
+        r = _calls().kv_read(cache_k, cache_v, slots, scales, bits, dtype is torch.float16, *(out if out is not None else (None, None)))
+        if r is not None:
+            if r.__class__ is int:
+                _check(r, "any4_kv_read")
+            return r
     lib = load_library()
     cache, heads, dim = _cache(cache_k, cache_v, scales, bits, dtype)
     ptr = _dev(slots, torch.int64, "slots")
@@ -481,6 +507,11 @@ def any4_attn_decode(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tens
     """[requests, heads, head_dim]: the newest token of each request (q, of that shape; slices of a fused projection's rows serve as
     they are) attends to the first lengths[r] (int32 [requests]) tokens of its pages (page_table, int32 [requests, table_width]) in
     the cache.  Query head h reads KV head h // (heads // kv_heads); softmax_scale is head_dim ** -0.5 unless given."""
+    r = _calls().attn_decode(q, cache_k, cache_v, page_table, lengths, scales, bits, softmax_scale, out, workspace)
+    if r is not None:
+        if r.__class__ is int:
+            _check(r, "any4_attn_decode")
+        return r
     lib = load_library()
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise Any4Error("q must be a tensor of 3 dimensions: requests, heads, head_dim")
@@ -515,6 +546,11 @@ def any4_attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts
     """[q_tokens, heads, head_dim]: packed prompts, request r in rows q_starts[r] .. q_starts[r + 1] - 1 of q and k_starts[r] .. of k and v
     [k_tokens, kv_heads, head_dim] (int32 [requests + 1]; k_starts None: q_starts).  Where a request has more rows in k, the first
     of them are the context in front of its queries: causal, query i of nq sees keys 0 .. i + nk - nq."""
+    r = _calls().attn_prompt(q, k, v, q_starts, k_starts, causal, softmax_scale, out)
+    if r is not None:
+        if r.__class__ is int:
+            _check(r, "any4_attn_prompt")
+        return r
     lib = load_library()
     for t, name in ((q, "q"), (k, "k"), (v, "v")):
         if not isinstance(t, torch.Tensor) or t.dim() != 3:

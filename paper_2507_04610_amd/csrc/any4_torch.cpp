@@ -1,15 +1,17 @@
-// The GEMM entry points of binding.py for the ordinary, valid call, in native code.
+// The GEMM, cache and attention entry points of binding.py for the ordinary, valid call, in native code.
 //
 // A decode-size GEMM takes the GPU 5 - 10 us; checking shapes and types, asking for the workspace size,
 // allocating the output and calling through ctypes took the host 13 us in Python, so that one call after
 // another was bound by the host (1 x 1024 x 1024: 13.2 us a call, 4.7 us of it on the GPU).  gemm() does
 // the same checks on the tensors themselves and calls the C ABI.  It only ever says yes: whatever is not a
 // plain valid call (a wrong type, shape, device, layout, a combination that does not exist) returns None
-// with nothing done, and binding.py goes through its own checks, which name the mistake.
+// with nothing done, and binding.py goes through its own checks, which name the mistake.  The functions for the cache and for
+// attention are the same for calls whose kernels take 3 - 5 us.
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
 #include <c10/hip/HIPStream.h>
+#include <cmath>
 #include "any4.h"
 
 namespace {
@@ -92,7 +94,173 @@ PyObject* gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// The cache as the C ABI takes it, from tensors [pages, kv_heads, page_size, head_dim (bytes of codes)]; false: not a valid one
+bool kv_cache(const at::Tensor& k, const at::Tensor& v, const at::Tensor* scales, long bits, at::ScalarType ty, any4_kv_cache& c) {
+    const at::ScalarType held = bits == 16 ? ty : at::kByte;
+    if ((bits != 16 && bits != 8 && bits != 4) || (ty != at::kBFloat16 && ty != at::kHalf) || k.dim() != 4) return false;
+    if (!plain(k, held) || !plain(v, held) || v.sizes() != k.sizes() || v.device() != k.device()) return false;
+    const int64_t pages = k.size(0), heads = k.size(1), page = k.size(2), width = k.size(3);
+    if (heads > 0xFFFF || page > 0xFFFF || width > 0xFFFF) return false;
+    c = any4_kv_cache{k.data_ptr(), v.data_ptr(), nullptr, pages, (int)page, (int)heads, (int)(bits == 16 ? width : width * 8 / bits), (int)bits, ty == at::kHalf};
+    if (bits == 16) return true;
+    if (!scales || !plain(*scales, at::kBFloat16) || scales->dim() != 4 || scales->size(0) != pages || scales->size(1) != heads ||
+        scales->size(2) != page || scales->size(3) != 4 || scales->device() != k.device())
+        return false;
+    c.scales = static_cast<uint16_t*>(scales->data_ptr());
+    return true;
+}
+// rows [tokens, heads, head_dim] whose heads' values lie side by side
+bool rows(const at::Tensor& t, at::ScalarType ty, int64_t tokens, int64_t heads, int64_t dim, const at::Tensor& on) {
+    return t.is_cuda() && t.scalar_type() == ty && t.layout() == at::kStrided && t.dim() == 3 && t.size(0) == tokens && t.size(1) == heads &&
+           t.size(2) == dim && t.stride(2) == 1 && t.device() == on.device();
+}
+bool list(const at::Tensor& t, at::ScalarType ty, const at::Tensor& on) { return plain(t, ty) && t.dim() == 1 && t.device() == on.device(); }
+// a tensor, or None; false: something else
+bool optional_tensor(PyObject* o, const at::Tensor*& t) {
+    t = o == Py_None ? nullptr : tensor(o);
+    return o == Py_None || t;
+}
+bool whole(PyObject* o, long& v) {
+    if (!PyLong_CheckExact(o)) return false;
+    v = PyLong_AsLong(o);
+    if (!PyErr_Occurred()) return true;
+    PyErr_Clear();
+    return false;
+}
+// softmax_scale, or None: head_dim ** -0.5
+bool scale_of(PyObject* o, int64_t dim, float& s) {
+    if (o == Py_None) { s = (float)std::pow((double)dim, -0.5); return true; }
+    if (!PyFloat_CheckExact(o)) return false;
+    s = (float)PyFloat_AS_DOUBLE(o);
+    return true;
+}
+PyObject* answer(int rc, PyObject* given, at::Tensor&& made) {
+    if (rc == ANY4_ERR_HIP) return PyLong_FromLong(rc);
+    if (rc != ANY4_OK) Py_RETURN_NONE;
+    if (given != Py_None) { Py_INCREF(given); return given; }
+    return THPVariable_Wrap(std::move(made));
+}
+
+// kv_write(k, v, slots, cache_k, cache_v, scales, bits) -> True; None and an int as gemm's
+PyObject* kv_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 7) Py_RETURN_NONE;
+    const at::Tensor *k = tensor(a[0]), *v = tensor(a[1]), *slots = tensor(a[2]), *ck = tensor(a[3]), *cv = tensor(a[4]), *scales;
+    long bits;
+    any4_kv_cache c;
+    if (!k || !v || !slots || !ck || !cv || !optional_tensor(a[5], scales) || !whole(a[6], bits)) Py_RETURN_NONE;
+    if (!kv_cache(*ck, *cv, scales, bits, k->scalar_type(), c) || !list(*slots, at::kLong, *ck)) Py_RETURN_NONE;
+    const int64_t tokens = slots->size(0);
+    if (!rows(*k, k->scalar_type(), tokens, c.kv_heads, c.head_dim, *ck) || !rows(*v, k->scalar_type(), tokens, c.kv_heads, c.head_dim, *ck)) Py_RETURN_NONE;
+    const int rc = any4_kv_write(u16(*k), k->stride(0), k->stride(1), u16(*v), v->stride(0), v->stride(1), tokens,
+                                 static_cast<const int64_t*>(slots->data_ptr()), &c, c10::hip::getCurrentHIPStream().stream());
+    if (rc == ANY4_OK) Py_RETURN_TRUE;
+    if (rc == ANY4_ERR_HIP) return PyLong_FromLong(rc);
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_read(cache_k, cache_v, slots, scales, bits, f16, out_k, out_v) -> (k, v)
+PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 8) Py_RETURN_NONE;
+    const at::Tensor *ck = tensor(a[0]), *cv = tensor(a[1]), *slots = tensor(a[2]), *scales, *ok, *ov;
+    long bits;
+    any4_kv_cache c;
+    const at::ScalarType ty = a[5] == Py_True ? at::kHalf : at::kBFloat16;
+    if (!ck || !cv || !slots || !optional_tensor(a[3], scales) || !whole(a[4], bits) || !optional_tensor(a[6], ok) || !optional_tensor(a[7], ov)) Py_RETURN_NONE;
+    if (!ok != !ov || !kv_cache(*ck, *cv, scales, bits, ty, c) || !list(*slots, at::kLong, *ck)) Py_RETURN_NONE;
+    const int64_t tokens = slots->size(0);
+    for (const at::Tensor* o : {ok, ov})
+        if (o && !(plain(*o, ty) && o->dim() == 3 && o->size(0) == tokens && o->size(1) == c.kv_heads && o->size(2) == c.head_dim && o->device() == ck->device())) Py_RETURN_NONE;
+    at::Tensor k = ok ? *ok : at::empty({tokens, c.kv_heads, c.head_dim}, ck->options().dtype(ty).requires_grad(false));
+    at::Tensor v = ov ? *ov : at::empty({tokens, c.kv_heads, c.head_dim}, ck->options().dtype(ty).requires_grad(false));
+    const int rc = any4_kv_read(&c, static_cast<const int64_t*>(slots->data_ptr()), tokens, static_cast<uint16_t*>(k.data_ptr()),
+                                static_cast<uint16_t*>(v.data_ptr()), c10::hip::getCurrentHIPStream().stream());
+    if (rc == ANY4_ERR_HIP) return PyLong_FromLong(rc);
+    if (rc != ANY4_OK) Py_RETURN_NONE;
+    PyObject* both = PyTuple_New(2);
+    if (!both) return nullptr;
+    PyTuple_SET_ITEM(both, 0, answer(rc, a[6], std::move(k)));
+    PyTuple_SET_ITEM(both, 1, answer(rc, a[7], std::move(v)));
+    return both;
+    END_HANDLE_TH_ERRORS
+}
+
+// attn_decode(q, cache_k, cache_v, page_table, lengths, scales, bits, softmax_scale, out, workspace)
+PyObject* attn_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 10) Py_RETURN_NONE;
+    const at::Tensor *q = tensor(a[0]), *ck = tensor(a[1]), *cv = tensor(a[2]), *table = tensor(a[3]), *lengths = tensor(a[4]), *scales, *out, *ws;
+    long bits;
+    float scale;
+    any4_kv_cache c;
+    if (!q || !ck || !cv || !table || !lengths || !optional_tensor(a[5], scales) || !whole(a[6], bits) || !optional_tensor(a[8], out) ||
+        !optional_tensor(a[9], ws) || q->dim() != 3)
+        Py_RETURN_NONE;
+    const at::ScalarType ty = q->scalar_type();
+    const int64_t requests = q->size(0), heads = q->size(1);
+    if (!kv_cache(*ck, *cv, scales, bits, ty, c) || !rows(*q, ty, requests, heads, c.head_dim, *ck) || !scale_of(a[7], c.head_dim, scale)) Py_RETURN_NONE;
+    if (heads < 1 || heads > 0xFFFF || c.kv_heads < 1 || heads % c.kv_heads) Py_RETURN_NONE;
+    if (!list(*lengths, at::kInt, *ck) || lengths->size(0) != requests) Py_RETURN_NONE;
+    if (!table->is_cuda() || table->scalar_type() != at::kInt || table->layout() != at::kStrided || table->dim() != 2 || table->size(0) != requests ||
+        table->stride(1) != 1 || table->device() != ck->device())
+        Py_RETURN_NONE;
+    if (out && !(plain(*out, ty) && rows(*out, ty, requests, heads, c.head_dim, *ck))) Py_RETURN_NONE;
+    if (ws && !(ws->layout() == at::kStrided && ws->device() == ck->device() && ws->is_non_overlapping_and_dense())) Py_RETURN_NONE;
+    const int64_t width = table->size(1);
+    at::Tensor o = out ? *out : at::empty({requests, heads, c.head_dim}, q->options().requires_grad(false));
+    at::Tensor scratch;
+    void* wp = nullptr;
+    size_t wbytes = 0;
+    if (ws) {
+        wp = ws->data_ptr();
+        wbytes = (size_t)ws->numel() * ws->element_size();
+    } else if (const size_t need = any4_attn_decode_workspace_bytes(requests, (int)heads, c.kv_heads, c.head_dim, width * c.page_size)) {
+        scratch = at::empty({(int64_t)need}, q->options().dtype(at::kByte).requires_grad(false));
+        wp = scratch.data_ptr();
+        wbytes = need;
+    }
+    const int rc = any4_attn_decode(u16(*q), q->stride(0), q->stride(1), &c, static_cast<const int32_t*>(table->data_ptr()), table->stride(0), width,
+                                    static_cast<const int32_t*>(lengths->data_ptr()), requests, (int)heads, scale, static_cast<uint16_t*>(o.data_ptr()), wp,
+                                    wbytes, c10::hip::getCurrentHIPStream().stream());
+    return answer(rc, a[8], std::move(o));
+    END_HANDLE_TH_ERRORS
+}
+
+// attn_prompt(q, k, v, q_starts, k_starts, causal, softmax_scale, out)
+PyObject* attn_prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 8) Py_RETURN_NONE;
+    const at::Tensor *q = tensor(a[0]), *k = tensor(a[1]), *v = tensor(a[2]), *qs = tensor(a[3]), *ks, *out;
+    float scale;
+    if (!q || !k || !v || !qs || !optional_tensor(a[4], ks) || !optional_tensor(a[7], out) || q->dim() != 3 || k->dim() != 3) Py_RETURN_NONE;
+    if (a[5] != Py_True && a[5] != Py_False) Py_RETURN_NONE;
+    const at::ScalarType ty = q->scalar_type();
+    if (ty != at::kBFloat16 && ty != at::kHalf) Py_RETURN_NONE;
+    const int64_t nq = q->size(0), heads = q->size(1), dim = q->size(2), nk = k->size(0), kv_heads = k->size(1);
+    if (heads < 1 || heads > 0xFFFF || kv_heads < 1 || kv_heads > 0xFFFF || heads % kv_heads || dim > 0xFFFF) Py_RETURN_NONE;
+    if (!rows(*q, ty, nq, heads, dim, *q) || !rows(*k, ty, nk, kv_heads, dim, *q) || !rows(*v, ty, nk, kv_heads, dim, *q)) Py_RETURN_NONE;
+    if (!list(*qs, at::kInt, *q) || qs->size(0) < 1 || (ks && (!list(*ks, at::kInt, *q) || ks->size(0) != qs->size(0)))) Py_RETURN_NONE;
+    if ((!ks && nk != nq) || !scale_of(a[6], dim, scale)) Py_RETURN_NONE;
+    if (out && !(plain(*out, ty) && rows(*out, ty, nq, heads, dim, *q))) Py_RETURN_NONE;
+    at::Tensor o = out ? *out : at::empty({nq, heads, dim}, q->options().requires_grad(false));
+    const int rc = any4_attn_prompt(u16(*q), q->stride(0), q->stride(1), u16(*k), k->stride(0), k->stride(1), u16(*v), v->stride(0), v->stride(1), nq, nk,
+                                    static_cast<const int32_t*>(qs->data_ptr()), static_cast<const int32_t*>((ks ? ks : qs)->data_ptr()), qs->size(0) - 1,
+                                    (int)heads, (int)kv_heads, (int)dim, ty == at::kHalf, a[5] == Py_True, scale, static_cast<uint16_t*>(o.data_ptr()),
+                                    c10::hip::getCurrentHIPStream().stream());
+    return answer(rc, a[7], std::move(o));
+    END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {
+    {"kv_write", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv_write)), METH_FASTCALL, "kv_write(k, v, slots, cache_k, cache_v, scales, bits)"},
+    {"kv_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv_read)), METH_FASTCALL,
+     "kv_read(cache_k, cache_v, slots, scales, bits, f16, out_k, out_v)"},
+    {"attn_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attn_decode)), METH_FASTCALL,
+     "attn_decode(q, cache_k, cache_v, page_table, lengths, scales, bits, softmax_scale, out, workspace)"},
+    {"attn_prompt", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attn_prompt)), METH_FASTCALL,
+     "attn_prompt(q, k, v, q_starts, k_starts, causal, softmax_scale, out)"},
     {"gemm", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(gemm)), METH_FASTCALL,
      "gemm(x, codes, lut, scale, offset, bits, out, workspace, group, repacked)"},
     {nullptr, nullptr, 0, nullptr}};
