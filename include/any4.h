@@ -346,7 +346,7 @@ int any4_kv_read(const any4_kv_cache* cache, const int64_t* slots, int64_t token
  *   workspace   at least any4_attn_decode_workspace_bytes() bytes; may be NULL when that is 0.  What is said of any4_gemm's
  *               holds here too
  * The cache behind a request's last token, up to the end of its page, may hold anything, NaN among it.
- * requests at most 65535, table_width * page_size at most 2^31 - 2048, softmax_scale finite and above 0
+ * requests at most 65535, table_width * page_size at most 2^31 - 2048 (with hundreds of KV heads 2^38 / kv_heads), softmax_scale finite and above 0
  * (ANY4_ERR_SHAPE).  requests = 0 does nothing.
  */
 int any4_attn_decode(const uint16_t* q, int64_t q_request_stride, int64_t q_head_stride, const any4_kv_cache* cache,

@@ -13,6 +13,7 @@ namespace any4 {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -68,11 +69,12 @@ constexpr float kLog2e = 1.44269504088896340736f;
 hipError_t launch_kv_write(const Rows& k, const Rows& v, int64_t tokens, const int64_t* slots, const any4_kv_cache& c, hipStream_t stream);
 hipError_t launch_kv_read(const any4_kv_cache& c, const int64_t* slots, int64_t tokens, uint16_t* k, uint16_t* v, hipStream_t stream);
 
-// How a decode call is cut: `splits` pieces of `chunk` tokens for each (request, KV head, 16 query heads).
+// How a decode call is shared out.
 struct DecodePlan {
-    int shared, head_tiles;   // query heads of a KV head, and in how many blocks of at most 16
-    int splits, chunk;
-    size_t words_bytes, workspace;      // arrival words, and all with the pieces' results (several pieces only)
+    int shared, head_tiles;   // query heads of a KV head, and in how many parts of at most 16
+    int at_once;              // requests of a launch
+    int waves, blocks, cus;   // wavefronts of a block, most blocks, compute units
+    size_t words_bytes, workspace;      // arrival words, and all with the pieces' results
 };
 DecodePlan plan_attn_decode(int64_t requests, int heads, int kv_heads, int head_dim, int64_t max_tokens, int cus);
 hipError_t launch_attn_decode(const Rows& q, const any4_kv_cache& c, const int32_t* table, int64_t table_stride, int64_t table_width,

@@ -15,6 +15,10 @@ constexpr int64_t kMaxStride = (int64_t)1 << 23;             // any4_attn_prompt
 constexpr int kMaxKvHeads = 4095, kMaxHeads = 65535;
 constexpr int64_t kMaxRequests = 65535, kMaxTokens = 0x7FFFFFFF - 2047;
 
+// the units of work of one request are counted in 32 bits
+bool tokens_ok(int64_t max_tokens, int heads, int kv_heads) {
+    return max_tokens >= 1 && max_tokens <= kMaxTokens && (max_tokens / 128 + 1) * kv_heads * ((heads / kv_heads + 15) / 16) <= 0x7FFFFFFF;
+}
 bool heads_ok(int heads, int kv_heads) {
     return kv_heads >= 1 && kv_heads <= kMaxKvHeads && heads >= 1 && heads <= kMaxHeads && heads % kv_heads == 0;
 }
@@ -60,8 +64,8 @@ int any4_kv_read(const any4_kv_cache* cache, const int64_t* slots, int64_t token
 }
 
 size_t any4_attn_decode_workspace_bytes(int64_t requests, int heads, int kv_heads, int head_dim, int64_t max_tokens) {
-    if (requests < 1 || requests > kMaxRequests || !heads_ok(heads, kv_heads) || (head_dim != 64 && head_dim != 128) || max_tokens < 1 ||
-        max_tokens > kMaxTokens)
+    if (requests < 1 || requests > kMaxRequests || !heads_ok(heads, kv_heads) || (head_dim != 64 && head_dim != 128) ||
+        !tokens_ok(max_tokens, heads, kv_heads))
         return 0;
     return plan_attn_decode(requests, heads, kv_heads, head_dim, max_tokens, device_compute_units()).workspace;
 }
@@ -71,7 +75,8 @@ int any4_attn_decode(const uint16_t* q, int64_t q_request_stride, int64_t q_head
                      int heads, float softmax_scale, uint16_t* out, void* workspace, size_t workspace_bytes, void* stream) {
     if (int rc = cache_check(cache)) return rc;
     if (requests < 0 || requests > kMaxRequests || !heads_ok(heads, cache->kv_heads) || !scale_ok(softmax_scale) ||
-        !strides_ok(q_request_stride, q_head_stride) || table_width < 1 || table_width > kMaxTokens / cache->page_size || table_stride < 0)
+        !strides_ok(q_request_stride, q_head_stride) || table_width < 1 || table_width > kMaxTokens / cache->page_size || table_stride < 0 ||
+        !tokens_ok(table_width * cache->page_size, heads, cache->kv_heads))
         return ANY4_ERR_SHAPE;
     if (requests == 0) return ANY4_OK;
     if (!q || !page_table || !lengths || !out) return ANY4_ERR_NULL;

@@ -27,7 +27,11 @@ namespace any4 {
 
 namespace {
 
-constexpr int kWaves = 8, kThreads = 64 * kWaves, kStep = 32;
+constexpr int kStep = 32;                                       // tokens of a wavefront's step
+constexpr int kFewGroups = 64;                                  // below: blocks of 8 wavefronts, one for a compute unit; from there on two or three of 4
+constexpr int kMaxRequests = 2048;                              // of a launch: their units' beginnings lie in LDS
+constexpr int kWholeUnits = 4;                                  // with fewer units a group (on average) no group is cut for the sake of more blocks
+constexpr int kJoin = 16;                                       // pieces whose loads are out at a time
 
 struct DecodeArgs {
     Rows q;
@@ -36,28 +40,61 @@ struct DecodeArgs {
     int64_t table_stride;
     int table_width;
     const int32_t* lengths;
-    int heads, shared, head_tiles;
+    int requests, heads, shared, head_tiles;
     float scale_log2;                  // softmax scale * log2(e)
     uint16_t* out;
-    int splits, chunk;
-    float* partial;                    // [request][KV head][head tile][split][query head][D + 2]: sums, then maximum and sum of weights
-    uint8_t* words;
+    float* partial;                    // [block][2][query head][D + 2]: sums, then maximum and sum of weights of every head
+    uint8_t* words;                    // an arrival word for each (request, KV head, head tile)
 };
+
+// One arrival at a word; true if it is the last of `pieces` (at most 2^16 - 1).  As arrive_one(), with 16 bits to count in.
+__device__ __forceinline__ bool arrive_piece(unsigned long long* word, int pieces) {
+    constexpr unsigned long long kTag = 0xA4C0DEDECull << 16;
+    auto own = [&](unsigned long long v) -> bool { return (v >> 16) == (kTag >> 16) && (int)(v & 0xFFFFull) < pieces; };
+    unsigned long long old = __hip_atomic_fetch_add(word, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), count;
+    if (own(old)) {
+        count = (old & 0xFFFFull) + 1ull;
+    } else {
+        old += 1ull;                                            // the add went into a foreign word and is dropped with it
+        for (;;) {
+            count = own(old) ? (old & 0xFFFFull) + 1ull : 1ull;
+            if (__hip_atomic_compare_exchange_strong(word, &old, kTag | count, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) break;
+        }
+    }
+    const bool last = (int)count == pieces;
+    if (last) __hip_atomic_store(word, kTag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return last;
+}
+
+// two floats between blocks, as splitk_store() and splitk_load()
+__device__ __forceinline__ void store_pair(float* p, f32x2 v) {
+    __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), __builtin_bit_cast(unsigned long long, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x2 load_pair(const float* p) {
+    return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// What a kernel only reads, at an address that all lanes share: scalar loads, which do not queue behind the vector loads.
+typedef const __attribute__((address_space(4))) int32_t* scalar_i32;
+__device__ __forceinline__ scalar_i32 scalar(const int32_t* p) { return (scalar_i32)reinterpret_cast<uintptr_t>(p); }
+
+// The cache is read once: loads that leave nothing behind in L2.
+template <class V> __device__ __forceinline__ V load_once(const void* p) { return __builtin_nontemporal_load(static_cast<const V*>(p)); }
 
 template <int N> __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[N]) {
     if constexpr (N >= 4) {
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) {
-            const u32x4 x = reinterpret_cast<const u32x4*>(p)[i];
+            const u32x4 x = load_once<u32x4>(p + 16 * i);
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[4 * i + j] = x[j];
         }
     } else if constexpr (N == 2) {
-        const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+        const u32x2 x = load_once<u32x2>(p);
         w[0] = x[0];
         w[1] = x[1];
     } else {
-        w[0] = *reinterpret_cast<const uint32_t*>(p);
+        w[0] = load_once<uint32_t>(p);
     }
 }
 
@@ -108,57 +145,121 @@ template <int BITS, bool F16, int N> __device__ __forceinline__ uint32_t v_pair(
     }
 }
 
-// over the four lanes that hold a head's tokens
-template <class F> __device__ __forceinline__ float head_reduce(float v, F f) {
-    v = f(v, __shfl_xor(v, 16));
-    return f(v, __shfl_xor(v, 32));
+// units of UNIT tokens of a request; one without tokens has one, in which its zeros are written
+template <int UNIT> __device__ __forceinline__ int units_of(int length, int64_t capacity) {
+    return (int)max((min((int64_t)length, capacity) + UNIT - 1) / UNIT, (int64_t)1);
 }
 
-template <int BITS, int D, bool F16>
-__global__ __launch_bounds__(kThreads) void attn_decode_kernel(DecodeArgs a) {
+// each lane gets the sum of the lanes up to its own
+__device__ __forceinline__ int lanes_scan(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111 /*row_shr:1*/, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112 /*row_shr:2*/, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114 /*row_shr:4*/, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118 /*row_shr:8*/, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142 /*row_bcast:15*/, 0xA, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143 /*row_bcast:31*/, 0xC, 0xF, false);
+    return v;
+}
+
+// over the four lanes that hold a head's tokens
+template <class F> __device__ __forceinline__ float head_reduce(float v, F f) {
+    u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+    v = f(__uint_as_float(x[0]), __uint_as_float(x[1]));
+    x = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+    return f(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+// over all lanes of a wavefront
+template <class F> __device__ __forceinline__ float wave_reduce(float v, F f) { return head_reduce(lanes_reduce<16>(v, f), f); }
+
+template <int BITS, int D, bool F16, int WAVES, bool AHEAD>
+__global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(DecodeArgs a) {
     using C = Codes<BITS, F16>;
+    constexpr int THREADS = 64 * WAVES, UNIT = kStep * WAVES;
     constexpr int KM = D / 32, VM = D / 16;                     // matrix instructions of S^T (16 tokens) and of O^T (32 tokens)
     constexpr int ROW = D * BITS / 8;                           // bytes of a token
     constexpr int KW = D * BITS / 128;                          // words of a lane: k of one token
     constexpr int VB = VM * BITS / 8, VW = VB < 4 ? 1 : VB / 4; // bytes and words of a lane: v of one token
     constexpr bool QUANT = BITS != 16;
+    constexpr int PAD = D + 4;                                  // a head's sums in LDS: 16 heads' pieces in different banks
     extern __shared__ float lds[];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
-    const int split = blockIdx.x, request = blockIdx.z;
-    const int kv_head = a.head_tiles == 1 ? (int)blockIdx.y : (int)blockIdx.y / a.head_tiles;
-    const int head_tile = (int)blockIdx.y - kv_head * a.head_tiles;
-    const int first_head = kv_head * a.shared + head_tile * 16, here = min(16, a.shared - head_tile * 16);
+    const int most = min(16, a.shared), room = most * (D + 2);  // query heads of a full head tile; floats of a piece's result
+    const int64_t capacity = (int64_t)a.table_width << a.c.page_shift;
 
-    int len = max(a.lengths[request], 0);
-    if ((int64_t)len > (int64_t)a.table_width << a.c.page_shift) len = (int)((int64_t)a.table_width << a.c.page_shift);
-    const int active = max(1, (int)(((int64_t)len + a.chunk - 1) / a.chunk));
-    if (split >= active) return;
-    const int t0 = split * a.chunk, t1 = (int)min((int64_t)len, (int64_t)t0 + a.chunk);
-    const int32_t* table = a.table + (int64_t)request * a.table_stride;
-
-    // Q^T, columns past `here` are zeros
-    u32x4 q[KM];
-    float sum_q = 0.0f;
+    // Where the requests' units begin: with up to 64 requests in the lanes, with more in LDS behind the wavefronts' sums or the
+    // pieces' factors and parts.
+    const bool many = a.requests > 64;
+    int* begins = reinterpret_cast<int*>(lds + max(WAVES * most * (PAD + 2), most * (int)gridDim.x + 2 * THREADS));
+    int lane_begin, lane_end, units_of_all;
+    if (!many) {
+        const int r = min(lane, a.requests - 1);
+        const int units = lane < a.requests ? units_of<UNIT>(a.lengths[r], capacity) : 0;
+        lane_end = lanes_scan(units);
+        lane_begin = lane_end - units;
+        units_of_all = __builtin_amdgcn_readlane(lane_end, 63);
+    } else {
+        int* sums = begins + a.requests + 1;
+        int before = 0;
+        for (int r0 = 0; r0 < a.requests; r0 += THREADS) {
+            const int r = r0 + (int)threadIdx.x;
+            const int sum = lanes_scan(r < a.requests ? units_of<UNIT>(a.lengths[r], capacity) : 0);
+            if (lane == 63) sums[wave] = sum;
+            __syncthreads();
+            int here = before;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                if (w < wave) here += sums[w];
+                before += sums[w];
+            }
+            if (r < a.requests) begins[r + 1] = here + sum;
+            if (r == 0) begins[0] = 0;
+            __syncthreads();
+        }
+        lane_begin = lane_end = 0;
+        units_of_all = __builtin_amdgcn_readfirstlane(before);
+    }
+    // That many units there are for each of `groups` (KV head, head tile), a request's groups one behind the other, and `blocks` blocks
+    // share them evenly, the first `longer` of them with one more than `each`.  (The host sees to it that they are fewer than 2^31.)
+    const unsigned groups = (unsigned)(a.c.kv_heads * a.head_tiles), all = (unsigned)units_of_all * groups;
+    const unsigned blocks = min(gridDim.x, all < kWholeUnits * (unsigned)a.requests * groups ? (unsigned)a.requests * groups : all);
+    if (blockIdx.x >= blocks) return;
+    const unsigned each = all / blocks, longer = all - each * blocks;
+    unsigned at = blockIdx.x * each + min(blockIdx.x, longer);
+    const unsigned end = at + each + (blockIdx.x < longer ? 1u : 0u);
+    auto block_of = [&](unsigned unit) -> int {
+        return (int)(unit < longer * (each + 1) ? unit / (each + 1) : longer + (unit - longer * (each + 1)) / each);
+    };
+    int request;
     {
-        const uint16_t* qp = a.q.p + (int64_t)request * a.q.token + (int64_t)(first_head + min(col, here - 1)) * a.q.head;
-#pragma unroll
-        for (int i = 0; i < KM; ++i) {
-            q[i] = *reinterpret_cast<const u32x4*>(qp + (QUANT ? (D / 4) * g + 8 * i : 32 * i + 8 * g));
-            if (col >= here) q[i] = u32x4{0u, 0u, 0u, 0u};
-            if constexpr (QUANT) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sum_q += h16lo_to_f32<F16>(q[i][j]) + h16hi_to_f32<F16>(q[i][j]);
+        const int y = (int)(at / groups);                       // the last request that begins at or before y
+        if (!many) {
+            request = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(lane < a.requests && lane_begin <= y));
+        } else {
+            int lo = 0;
+            for (int hi = a.requests - 1; lo < hi;) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (__builtin_amdgcn_readfirstlane(begins[mid]) <= y) lo = mid;
+                else hi = mid - 1;
             }
-            if constexpr (BITS == 4) {                          // pairs (x, x + 4), as the codes come
-                const u32x4 r = q[i];
-                q[i] = u32x4{__builtin_amdgcn_perm(r[2], r[0], 0x05040100u), __builtin_amdgcn_perm(r[2], r[0], 0x07060302u),
-                             __builtin_amdgcn_perm(r[3], r[1], 0x05040100u), __builtin_amdgcn_perm(r[3], r[1], 0x07060302u)};
-            }
+            request = lo;
         }
     }
-    if constexpr (QUANT) sum_q = head_reduce(sum_q, [](float x, float y) { return x + y; }) * a.scale_log2;
+    for (; at < end; ++request) {
+    const int len = (int)min((int64_t)max(scalar(a.lengths)[request], 0), capacity);
+    const scalar_i32 table = scalar(a.table + (int64_t)request * a.table_stride);
+    const unsigned begin = many ? __builtin_amdgcn_readfirstlane(begins[request]) : __builtin_amdgcn_readlane(lane_begin, request & 63);
+    const unsigned units = (many ? __builtin_amdgcn_readfirstlane(begins[request + 1]) : __builtin_amdgcn_readlane(lane_end, request & 63)) - begin;
+    const unsigned request_at = begin * groups;
+    for (int group = (int)((at - request_at) / units); group < (int)groups && at < end; ++group) {
+    const unsigned group_at = request_at + (unsigned)group * units;
+    const int from = (int)(at - group_at), to = (int)min(units, end - group_at);
+    at = group_at + (unsigned)to;
+    const int kv_head = a.head_tiles == 1 ? group : group / a.head_tiles;
+    const int head_tile = group - kv_head * a.head_tiles;
+    const int first_head = kv_head * a.shared + head_tile * 16, here = min(16, a.shared - head_tile * 16);
+    const int t0 = from * UNIT, t1 = min(len, to * UNIT);
 
     float m_ref = -__builtin_inff(), l = 0.0f, vo_sum = 0.0f;
     f32x4 o[VM], ones_sum = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -167,44 +268,95 @@ __global__ __launch_bounds__(kThreads) void attn_decode_kernel(DecodeArgs a) {
     // fp16 weights p * vs: held as p * (vs * 2^-exponent), with the largest vs so far between 1 and 2, or small scales would leave fp16's range
     int exponent = -126;
 
-    const int page_mask = (1 << a.c.page_shift) - 1;
-    for (int t = t0 + kStep * wave; t < t1; t += kStep * kWaves) {
-        // tokens of the two 16s that exist; a page that does not has none
+    // One step's tokens: which of the two 16s' exist, and what the lanes load of them.
+    struct Step {
         int there[2];
+        uint32_t kw[2][KW], vw[8][VW];
+        u32x4 so[2][2];
+    };
+    const int page_mask = (1 << a.c.page_shift) - 1;
+    // the pages of a step at t (its own, again, past the end)
+    auto pages_of = [&](int t, int (&page)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int th = t + 16 * h < t1 ? t + 16 * h : t < t1 ? t : t0;
+            page[h] = table[th >> a.c.page_shift];
+        }
+    };
+    auto load = [&](int t, const int (&page)[2], Step& st) {
         int64_t tok[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int th = t + 16 * h < len ? t + 16 * h : t;
-            const int page = __builtin_amdgcn_readfirstlane(table[th >> a.c.page_shift]);
-            const bool ok = page >= 0 && page < a.c.pages;
-            there[h] = ok ? min(max(len - (t + 16 * h), 0), 16) : 0;
-            tok[h] = a.c.first_token(ok ? page : 0, kv_head) + (th & page_mask);
-        }
-        uint32_t kw[2][KW], vw[8][VW];
-        u32x4 so[2][2 * 2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
+            const int th = t + 16 * h < t1 ? t + 16 * h : t;
+            const bool ok = page[h] >= 0 && page[h] < a.c.pages;           // a page that does not exist has no tokens
+            st.there[h] = ok ? min(max(len - (t + 16 * h), 0), 16) : 0;
+            tok[h] = a.c.first_token(ok ? page[h] : 0, kv_head) + (th & page_mask);
             const uint8_t* kp = a.c.k + tok[h] * ROW;
             if constexpr (BITS == 16) {
 #pragma unroll
                 for (int i = 0; i < KM; ++i) {
-                    const u32x4 x = *reinterpret_cast<const u32x4*>(kp + col * ROW + 64 * i + 16 * g);
+                    const u32x4 x = load_once<u32x4>(kp + (uint32_t)(col * ROW + 64 * i + 16 * g));
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) kw[h][4 * i + j] = x[j];
+                    for (int j = 0; j < 4; ++j) st.kw[h][4 * i + j] = x[j];
                 }
             } else {
-                load_words(kp + col * ROW + (ROW / 4) * g, kw[h]);
-                const u32x4* sp = reinterpret_cast<const u32x4*>(a.c.scales + tok[h] * 4) + 2 * g;
-                so[h][0] = sp[0];
-                so[h][1] = sp[1];
+                load_words(kp + (uint32_t)(col * ROW + (ROW / 4) * g), st.kw[h]);
+                const uint8_t* sp = reinterpret_cast<const uint8_t*>(a.c.scales + tok[h] * 4) + (uint32_t)(32 * g);
+                st.so[h][0] = load_once<u32x4>(sp);
+                st.so[h][1] = load_once<u32x4>(sp + 16);
             }
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const uint8_t* vp = a.c.v + tok[j >> 2] * ROW + (4 * g + (j & 3)) * ROW + VB * col;
-            if constexpr (VB == 2) vw[j][0] = *reinterpret_cast<const uint16_t*>(vp);
-            else load_words(vp, vw[j]);
+            const uint8_t* vp = a.c.v + tok[j >> 2] * ROW + (uint32_t)((4 * g + (j & 3)) * ROW + VB * col);
+            if constexpr (VB == 2) st.vw[j][0] = load_once<uint16_t>(vp);
+            else load_words(vp, st.vw[j]);
         }
+    };
+
+    // A step's loads are out before the step in front of it is worked on, its pages' numbers one step earlier.
+    Step st;
+    int page[2];
+    const int first = t0 + kStep * wave;
+    pages_of(first, page);
+    u32x4 q[KM];
+    {
+        int q_lane = lane;
+        asm volatile("" : "+v"(q_lane));
+        const int col = q_lane & 15, g = q_lane >> 4;
+        const uint16_t* qp = a.q.p + (int64_t)request * a.q.token + (int64_t)(first_head + min(col, here - 1)) * a.q.head;
+#pragma unroll
+        for (int i = 0; i < KM; ++i) q[i] = *reinterpret_cast<const u32x4*>(qp + (QUANT ? (D / 4) * g + 8 * i : 32 * i + 8 * g));
+    }
+    if (AHEAD && first < t1) load(first, page, st);
+    if (AHEAD) pages_of(first + UNIT, page);
+    __builtin_amdgcn_sched_barrier(0);
+    // Q^T, columns past `here` are zeros
+    float sum_q = 0.0f;
+#pragma unroll
+    for (int i = 0; i < KM; ++i) {
+        if (col >= here) q[i] = u32x4{0u, 0u, 0u, 0u};
+        if constexpr (QUANT) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum_q += h16lo_to_f32<F16>(q[i][j]) + h16hi_to_f32<F16>(q[i][j]);
+        }
+        if constexpr (BITS == 4) {                              // pairs (x, x + 4), as the codes come
+            const u32x4 r = q[i];
+            q[i] = u32x4{__builtin_amdgcn_perm(r[2], r[0], 0x05040100u), __builtin_amdgcn_perm(r[2], r[0], 0x07060302u),
+                         __builtin_amdgcn_perm(r[3], r[1], 0x05040100u), __builtin_amdgcn_perm(r[3], r[1], 0x07060302u)};
+        }
+    }
+    if constexpr (QUANT) sum_q = head_reduce(sum_q, [](float x, float y) { return x + y; }) * a.scale_log2;
+    for (int t = first; t < t1; t += UNIT) {
+        Step next;
+        if (!AHEAD) load(t, page, st);
+        if (AHEAD && t + UNIT < t1) load(t + UNIT, page, next);
+        pages_of(t + (AHEAD ? 2 : 1) * UNIT, page);
+        __builtin_amdgcn_sched_barrier(0);                      // (left alone, the loads sink to where their values are used)
+        auto& kw = st.kw;
+        auto& vw = st.vw;
+        auto& so = st.so;
+        const int there[2] = {st.there[0], st.there[1]};
 
         f32x4 s[2];
 #pragma unroll
@@ -295,116 +447,181 @@ __global__ __launch_bounds__(kThreads) void attn_decode_kernel(DecodeArgs a) {
             for (int j = 0; j < 4; ++j) v[j] = v_pair<BITS, F16>(vw[2 * j], vw[2 * j + 1], m);
             o[m] = mma16<F16>(v, p, o[m]);
         }
+        if (AHEAD) st = next;
     }
 
-    // The wavefronts' results meet in LDS: [wave][head][D], then [wave][head] maximum and sum of weights.
+    // (the lane's number anew: what follows from it below is not to take registers from the loop above)
+    int thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));
+    const int col_e = thread & 15, g_e = (thread >> 4) & 3;
+    // The wavefronts' results meet in LDS: [wave][head][PAD], then [wave][head] maximum and sum of weights.
     auto add = [](float u, float v) { return u + v; };
     l = head_reduce(l, add);
     if constexpr (QUANT) vo_sum = head_reduce(vo_sum, add);
-    float* ml = lds + kWaves * here * D;
-    if (col < here) {
+    float* ml = lds + WAVES * here * PAD;
+    __syncthreads();                                            // (nobody reads what another piece left there)
+    if (col_e < here) {
         const float back = QUANT && F16 ? __builtin_ldexpf(1.0f, exponent) : 1.0f;
-        float* to = lds + (wave * here + col) * D;
+        float* to_lds = lds + (wave * here + col_e) * PAD;
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int m = 0; m < VM; ++m) {
-                float v = o[m][r];
-                if constexpr (QUANT) v = fmaf(back, v - (float)(C::kBias + C::kCentre) * ones_sum[0], vo_sum);
-                to[VM * (4 * g + r) + m] = v;
+            for (int m = 0; m < VM; m += 4) {
+                f32x4 v = {o[m][r], o[m + 1][r], o[m + 2][r], o[m + 3][r]};
+                if constexpr (QUANT) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = fmaf(back, v[j] - (float)(C::kBias + C::kCentre) * ones_sum[0], vo_sum);
+                }
+                *reinterpret_cast<f32x4*>(to_lds + VM * (4 * g_e + r) + m) = v;
             }
-        if (g == 0) {
-            ml[2 * (wave * here + col)] = m_ref;
-            ml[2 * (wave * here + col) + 1] = l;
+        if (g_e == 0) {
+            ml[2 * (wave * here + col_e)] = m_ref;
+            ml[2 * (wave * here + col_e) + 1] = l;
         }
     }
     __syncthreads();
-    const int64_t pair = ((int64_t)request * gridDim.y + blockIdx.y);
     uint16_t* out = a.out + ((int64_t)request * a.heads + first_head) * D;
-    const int room = min(16, a.shared) * (D + 2);               // of a piece (the last head tile may have fewer heads)
-    float* mine = a.partial + (pair * a.splits + split) * room;
-    for (int i = threadIdx.x; i < here * D; i += kThreads) {
-        const int n = i / D;
+    const bool split = from > 0 || to < units;
+    // A block has at most two groups that it shares with others: one that begins in front of it, one that goes on behind it.
+    float* mine = a.partial + ((int64_t)blockIdx.x * 2 + (from > 0 ? 0 : 1)) * room;
+    for (int i = thread; i < here * D / 2; i += THREADS) {      // two places of a head each
+        const int n = i / (D / 2), d = 2 * i - n * D;
         float top = -__builtin_inff();
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[2 * (w * here + n)]);
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ml[2 * (w * here + n)]);
         const float use = top == -__builtin_inff() ? 0.0f : top;
-        float sum = 0.0f, v = 0.0f;
+        float sum = 0.0f;
+        f32x2 v = {0.0f, 0.0f};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const float f = exp2_fast(ml[2 * (w * here + n)] - use);
             sum = fmaf(f, ml[2 * (w * here + n) + 1], sum);
-            v = fmaf(f, lds[w * here * D + i], v);
+            const f32x2 x = *reinterpret_cast<const f32x2*>(lds + (w * here + n) * PAD + d);
+            v = f32x2{fmaf(f, x[0], v[0]), fmaf(f, x[1], v[1])};
         }
-        if (active == 1) {
-            out[i] = (uint16_t)f32_to_h16<F16>(sum == 0.0f ? 0.0f : v / sum);
+        if (!split) {
+            reinterpret_cast<uint32_t*>(out)[i] = sum == 0.0f ? 0u : f32x2_to_h16x2<F16>(v[0] / sum, v[1] / sum);
         } else {
-            splitk_store(mine + i, v);
-            if (i - n * D < 2) splitk_store(mine + here * D + 2 * n + (i - n * D), i == n * D ? top : sum);
+            store_pair(mine + 2 * i, v);
+            if (d == 0) store_pair(mine + here * D + 2 * n, f32x2{top, sum});
         }
     }
-    if (active == 1) return;
+    if (!split) continue;
 
-    // The last piece of a request and head to come adds all of them, in their order.
+    // The last piece of a group to come adds all of them: first the pieces' factors, a wavefront for a head and a lane for a piece,
+    // then the sums in the pieces' order, with the pieces dealt out to as many threads as there are for each two places.  (One compute
+    // unit reads what the others wrote: all its loads are out at once, or this takes longer than the rest of a short call.)
+    const int first_block = block_of(group_at), pieces = block_of(group_at + units - 1) - first_block + 1;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     int* last = reinterpret_cast<int*>(lds);
-    if (threadIdx.x == 0) *last = arrive_one(reinterpret_cast<unsigned long long*>(a.words + pair * kWordBytes), active);
+    if (thread == 0)
+        *last = arrive_piece(reinterpret_cast<unsigned long long*>(a.words + ((int64_t)request * groups + group) * kWordBytes), pieces);
     __syncthreads();
     const bool joins = *last != 0;
     __syncthreads();
-    if (!joins) return;
-    const float* all = a.partial + pair * a.splits * room;
-    for (int i = threadIdx.x; i < active * here * 2; i += kThreads) {
-        const int w = i / (here * 2);
-        lds[i] = splitk_load(all + (int64_t)w * room + here * D + (i - w * here * 2));
+    if (!joins) continue;
+    // (the first piece lies in its block's second place, the others in their blocks' first)
+    const float* base = a.partial + (int64_t)first_block * 2 * room;
+    auto piece_at = [&](int w) -> const float* { return base + (w == 0 ? room : w * 2 * room); };
+    const int items = here * D / 2, slices = max(THREADS / items, 1), span = (pieces + slices - 1) / slices;
+    const int slice = thread / items, w_first = slice * span, w_end = slice < slices ? min(pieces, w_first + span) : 0;
+    float* factor = lds;                                        // [head][pieces]
+    float* parts = lds + here * pieces;                         // [slice][items][2], behind the factors
+    f32x2 x[kJoin];
+    auto load_parts = [&](int w0, int i) {
+#pragma unroll
+        for (int w = 0; w < kJoin; ++w)
+            x[w] = w0 + w < w_end && i < items ? load_pair(piece_at(w0 + w) + 2 * i) : f32x2{0.0f, 0.0f};
+    };
+    auto load_ml = [&](int w, int n) -> f32x2 {
+        return w < pieces && n < here ? load_pair(piece_at(w) + here * D + 2 * n) : f32x2{-__builtin_inff(), 0.0f};
+    };
+    const int lane_e = thread & 63;
+    f32x2 ml_of = load_ml(lane_e, wave);
+    load_parts(w_first, thread - slice * items);                // (on their way while the factors are made)
+    for (int n = wave; n < here; n += WAVES) {
+        if (n != wave) ml_of = load_ml(lane_e, n);
+        float top = -__builtin_inff(), sum = 0.0f;
+        for (int w = lane_e; w < pieces; w += 64) {
+            if (w >= 64) ml_of = load_ml(w, n);
+            factor[n * pieces + w] = ml_of[0];
+            const float higher = fmaxf(top, ml_of[0]), use = higher == -__builtin_inff() ? 0.0f : higher;
+            sum = fmaf(exp2_fast(top - use), sum, exp2_fast(ml_of[0] - use) * ml_of[1]);
+            top = higher;
+        }
+        const float own_top = top;
+        top = wave_reduce(top, [](float u, float v) { return fmaxf(u, v); });
+        const float use = top == -__builtin_inff() ? 0.0f : top;
+        sum = wave_reduce(sum * exp2_fast(own_top - use), add);
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        for (int w = lane_e; w < pieces; w += 64) factor[n * pieces + w] = exp2_fast(factor[n * pieces + w] - use) * inv;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < here * D; i += kThreads) {
-        const int n = i / D;
-        float top = -__builtin_inff(), sum = 0.0f, v = 0.0f;
-        for (int w = 0; w < active; ++w) top = fmaxf(top, lds[2 * (w * here + n)]);
-        const float use = top == -__builtin_inff() ? 0.0f : top;
-#pragma unroll 8
-        for (int w = 0; w < active; ++w) {
-            const float f = exp2_fast(lds[2 * (w * here + n)] - use);
-            sum = fmaf(f, lds[2 * (w * here + n) + 1], sum);
-            v = fmaf(f, splitk_load(all + (int64_t)w * room + i), v);
+    for (int i0 = 0; i0 < items; i0 += THREADS) {
+        const int i = i0 + thread - slice * items, n = min(i / (D / 2), here - 1);
+        if (i0 > 0) load_parts(w_first, i);
+        f32x2 v = {0.0f, 0.0f};
+        for (int w0 = w_first; w0 < w_end; w0 += kJoin) {
+            if (w0 > w_first) load_parts(w0, i);
+#pragma unroll
+            for (int w = 0; w < kJoin; ++w)
+                if (w0 + w < w_end) {
+                    const float f = factor[n * pieces + w0 + w];
+                    v = f32x2{fmaf(f, x[w][0], v[0]), fmaf(f, x[w][1], v[1])};
+                }
         }
-        out[i] = (uint16_t)f32_to_h16<F16>(sum == 0.0f ? 0.0f : v / sum);
+        if (slices > 1) {
+            if (slice < slices) reinterpret_cast<f32x2*>(parts)[thread] = v;
+            __syncthreads();
+            if (slice == 0)
+                for (int s = 1; s < slices; ++s) {
+                    const f32x2 other = reinterpret_cast<const f32x2*>(parts)[s * items + i];
+                    v = f32x2{v[0] + other[0], v[1] + other[1]};
+                }
+        }
+        if (i < items && slice == 0) reinterpret_cast<uint32_t*>(out)[i] = f32x2_to_h16x2<F16>(v[0], v[1]);
+    }
+    }
     }
 }
 
-template <int BITS, int D, bool F16> hipError_t launch(const DecodeArgs& a, const dim3& grid, int here, hipStream_t stream) {
-    constexpr auto kernel = attn_decode_kernel<BITS, D, F16>;
-    const int most = kWaves * 16 * (D + 2) * (int)sizeof(float);
-    if (hipError_t e = ensure_lds<kernel>(most); e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), kWaves * here * (D + 2) * sizeof(float), stream, a);
+template <int BITS, int D, bool F16, int WAVES> hipError_t launch(const DecodeArgs& a, const DecodePlan& pl, hipStream_t stream) {
+    constexpr auto kernel = attn_decode_kernel<BITS, D, F16, WAVES, BITS == 16 || WAVES == 8>;
+    auto bytes = [](int heads, int requests, int blocks) {
+        const int own = WAVES * heads * (D + 6), join = heads * blocks + 128 * WAVES;
+        return (int)sizeof(float) * ((own > join ? own : join) + requests + 1 + WAVES);
+    };
+    if (hipError_t e = ensure_lds<kernel>(bytes(16, kMaxRequests, 1024)); e != hipSuccess) return e;
+    const int most = pl.shared < 16 ? pl.shared : 16;
+    // blocks of 4 wavefronts: two for a compute unit, with 4 bits three (64 requests of up to 2048 tokens: 33 -> 27 us; 8 bits and 32 of up to
+    // 4096: 34 -> 36)
+    const int fill = pl.cus * (WAVES == 8 ? 1 : BITS == 4 ? 3 : 2), blocks = pl.blocks < fill ? pl.blocks : fill;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * WAVES), bytes(most, a.requests, blocks), stream, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-constexpr int kMaxSplits = 128, kMinChunk = kStep * kWaves, kMaxChunk = 2048;
-
 DecodePlan plan_attn_decode(int64_t requests, int heads, int kv_heads, int head_dim, int64_t max_tokens, int cus) {
     DecodePlan p{};
+    p.cus = cus;
     p.shared = heads / kv_heads;
     p.head_tiles = (p.shared + 15) / 16;
-    const int64_t pairs = requests * kv_heads * p.head_tiles;
-    const int64_t want = pairs > 0 ? (2 * (int64_t)cus + pairs - 1) / pairs : 1;
-    int64_t chunk = (max_tokens + want - 1) / want;
-    if (chunk > kMaxChunk) chunk = kMaxChunk;
-    if (chunk < kMinChunk) chunk = kMinChunk;
-    if (chunk * kMaxSplits < max_tokens) chunk = (max_tokens + kMaxSplits - 1) / kMaxSplits;
-    chunk = (chunk + kStep - 1) / kStep * kStep;
-    p.chunk = (int)chunk;
-    p.splits = (int)((max_tokens + chunk - 1) / chunk);
-    if (p.splits < 1) p.splits = 1;
-    if (p.splits > 1) {
-        const int here = p.shared < 16 ? p.shared : 16;
-        p.words_bytes = (size_t)pairs * kWordBytes;
-        p.workspace = p.words_bytes + (size_t)pairs * p.splits * here * (head_dim + 2) * sizeof(float);
+    // (units are counted in 32 bits)
+    const int64_t longest = (max_tokens + kStep * 4 - 1) / (kStep * 4) * kv_heads * p.head_tiles;
+    p.at_once = (int)(0x7FFFFFFF / longest < kMaxRequests ? 0x7FFFFFFF / longest : kMaxRequests);
+    if (p.at_once < 1) p.at_once = 1;
+    const int64_t groups = (requests < p.at_once ? requests : p.at_once) * kv_heads * p.head_tiles;
+    p.waves = groups < kFewGroups ? 8 : 4;
+    const int64_t unit = kStep * p.waves, most_blocks = (int64_t)cus * (p.waves == 8 ? 1 : 3);
+    // no more blocks than there are groups, or units if all requests are as long as they may be
+    const int64_t units = (max_tokens + unit - 1) / unit, useful = units < kWholeUnits ? groups : groups * units;
+    p.blocks = (int)(useful < most_blocks ? useful : most_blocks);
+    if (max_tokens > unit) {
+        const int most = p.shared < 16 ? p.shared : 16;
+        p.words_bytes = (size_t)groups * kWordBytes;
+        p.workspace = p.words_bytes + (size_t)p.blocks * 2 * most * (head_dim + 2) * sizeof(float);
     }
     return p;
 }
@@ -412,17 +629,27 @@ DecodePlan plan_attn_decode(int64_t requests, int heads, int kv_heads, int head_
 hipError_t launch_attn_decode(const Rows& q, const any4_kv_cache& c, const int32_t* table, int64_t table_stride, int64_t table_width,
                               const int32_t* lengths, int64_t requests, int heads, float softmax_scale, uint16_t* out, const DecodePlan& pl,
                               void* workspace, hipStream_t stream) {
-    DecodeArgs a{q, kv_pages(c), table, table_stride, (int)table_width, lengths, heads, pl.shared, pl.head_tiles, softmax_scale * kLog2e, out,
-                 pl.splits, pl.chunk, nullptr, static_cast<uint8_t*>(workspace)};
+    DecodeArgs a{q, kv_pages(c), table, table_stride, (int)table_width, lengths, 0, heads, pl.shared, pl.head_tiles, softmax_scale * kLog2e, out,
+                 nullptr, static_cast<uint8_t*>(workspace)};
     a.partial = reinterpret_cast<float*>(a.words + pl.words_bytes);
-    const dim3 grid((unsigned)pl.splits, (unsigned)(c.kv_heads * pl.head_tiles), (unsigned)requests);
-    const int here = pl.shared < 16 ? pl.shared : 16;
+    auto waves = [&](auto bits, auto f16, auto dim) {
+        return pl.waves == 8 ? launch<decltype(bits)::value, decltype(dim)::value, decltype(f16)::value, 8>(a, pl, stream)
+                             : launch<decltype(bits)::value, decltype(dim)::value, decltype(f16)::value, 4>(a, pl, stream);
+    };
     auto dims = [&](auto bits, auto f16) {
-        return c.head_dim == 128 ? launch<decltype(bits)::value, 128, decltype(f16)::value>(a, grid, here, stream)
-                                 : launch<decltype(bits)::value, 64, decltype(f16)::value>(a, grid, here, stream);
+        return c.head_dim == 128 ? waves(bits, f16, std::integral_constant<int, 128>{}) : waves(bits, f16, std::integral_constant<int, 64>{});
     };
     auto types = [&](auto bits) { return c.f16 ? dims(bits, std::true_type{}) : dims(bits, std::false_type{}); };
-    return c.bits == 16 ? types(std::integral_constant<int, 16>{}) : c.bits == 8 ? types(std::integral_constant<int, 8>{}) : types(std::integral_constant<int, 4>{});
+    hipError_t e = hipSuccess;
+    for (int64_t r = 0; r < requests && e == hipSuccess; r += pl.at_once) {           // (one launch, but for thousands)
+        a.requests = (int)(requests - r < pl.at_once ? requests - r : pl.at_once);
+        a.q.p = q.p + r * q.token;
+        a.table = table + r * table_stride;
+        a.lengths = lengths + r;
+        a.out = out + r * heads * c.head_dim;
+        e = c.bits == 16 ? types(std::integral_constant<int, 16>{}) : c.bits == 8 ? types(std::integral_constant<int, 8>{}) : types(std::integral_constant<int, 4>{});
+    }
+    return e;
 }
 
 }  // namespace any4
