@@ -106,69 +106,79 @@ __global__ __launch_bounds__(kThreads, 2) void attn_prompt_kernel(Args a) {
         for (int i = 0; i < QM; ++i) q[i] = *reinterpret_cast<const u32x4*>(qp + 16 * i);
     }
 
-    // copies: lane -> row and piece of each instruction; LDS has piece c of row r at c ^ swizzle(r)
+    // copies: lane -> row and piece of each instruction; LDS has piece c of row r at c ^ swizzle(r).  LDS: two tiles of k, two of v.
     const char* k_base = reinterpret_cast<const char*>(a.k.p + (int64_t)k_at * a.k.token + (int64_t)kv_head * a.k.head);
     const char* v_base = reinterpret_cast<const char*>(a.v.p + (int64_t)k_at * a.v.token + (int64_t)kv_head * a.v.head);
     const uint32_t k_step = (uint32_t)a.k.token * 2u, v_step = (uint32_t)a.v.token * 2u;
-    auto copy = [&](int t, int buffer) {
+    const int copy_row = T::kCopies * wave * T::kRows + lane / T::kPieces, copy_piece = lane % T::kPieces;
+    uint32_t k_from[T::kCopies], v_from[T::kCopies];
+#pragma unroll
+    for (int j = 0; j < T::kCopies; ++j) {
+        const int row = copy_row + j * T::kRows;
+        k_from[j] = (uint32_t)row * k_step + 16u * (uint32_t)(copy_piece ^ T::swizzle_k(row));
+        v_from[j] = (uint32_t)row * v_step + 16u * (uint32_t)(copy_piece ^ T::swizzle_v(row));
+    }
+    auto copy_rows = [&](const char* base, uint32_t step, const uint32_t (&from)[T::kCopies], int t, uint32_t to) {
         const int k0 = t * kKeys;
-        const char* kb = k_base + (int64_t)k0 * k_step;
-        const char* vb = v_base + (int64_t)k0 * v_step;
+        const char* tile_base = base + (int64_t)k0 * step;
 #pragma unroll
         for (int j = 0; j < T::kCopies; ++j) {
-            const int at = T::kCopies * wave + j, row = at * T::kRows + lane / T::kPieces, piece = lane % T::kPieces;
-            const uint32_t from = (uint32_t)min(row, lk - 1 - k0);          // (rows past the last are copies of it; they are masked)
-            copy_to_lds(buffer * 2 * T::kBytes + at * 1024, kb, from * k_step + 16u * (uint32_t)(piece ^ T::swizzle_k(row)));
-            copy_to_lds(buffer * 2 * T::kBytes + T::kBytes + at * 1024, vb, from * v_step + 16u * (uint32_t)(piece ^ T::swizzle_v(row)));
+            uint32_t off = from[j];
+            // (rows past the last are copies of it; they are masked)
+            if (k0 + kKeys > lk) off -= (uint32_t)max(copy_row + j * T::kRows - (lk - 1 - k0), 0) * step;
+            copy_to_lds(to + (uint32_t)(T::kCopies * wave + j) * 1024u, tile_base, off);
         }
     };
+    auto copy_k = [&](int t, uint32_t parity) { copy_rows(k_base, k_step, k_from, t, parity * T::kBytes); };
+    auto copy_v = [&](int t, uint32_t parity) { copy_rows(v_base, v_step, v_from, t, (2 + parity) * T::kBytes); };
 
-    // operand addresses within a buffer
-    const uint32_t k_lane = (uint32_t)(n * T::kRow), k_swz = (uint32_t)((g ^ T::swizzle_k(n)) << 4);
-    const int i16 = lane & 15, v_row = 4 * g + (i16 >> 2);
-    const uint32_t v_lane = (uint32_t)(T::kBytes + v_row * T::kRow + 8 * (i16 & 1)),
-                   v_swz = (uint32_t)(((2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1)) ^ T::swizzle_v(v_row)) << 4);
+    // operand addresses within a tile
+    uint32_t k_lane[QM], v_lane[OM];
+    {
+        const int i16 = lane & 15, v_row = 4 * g + (i16 >> 2);
+#pragma unroll
+        for (int i = 0; i < QM; ++i) k_lane[i] = (uint32_t)(n * T::kRow + (((2 * i + g) ^ T::swizzle_k(n)) << 4));
+#pragma unroll
+        for (int m = 0; m < OM; ++m)
+            v_lane[m] = (uint32_t)(2 * T::kBytes + v_row * T::kRow + 8 * (i16 & 1) +
+                                   (((4 * m + 2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1)) ^ T::swizzle_v(v_row)) << 4));
+    }
 
     float m_ref = -__builtin_inff(), l = 0.0f;
-    f32x16 o[OM];
+    f32x16 o[OM], s[2];
 #pragma unroll
     for (int m = 0; m < OM; ++m)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[m][r] = 0.0f;
 
-    // MASKED: some query of the block may not see some key of the tile
-    auto step = [&](int t, auto masked_tile) {
-        constexpr bool MASKED = decltype(masked_tile)::value;
-        loads_left<0>();
-        lds_barrier();                                          // tile t is there, and nobody reads the other buffer any more
-        if (t + 1 < tiles) copy(t + 1, (t + 1) & 1);
-        const int k0 = t * kKeys;
-        const uint32_t buf = (uint32_t)((t & 1) * 2 * T::kBytes);
-        if (MASKED && a.causal && k0 > q_wave + 31 + ahead) return;     // no query of this wavefront sees it
-        f32x16 s[2];
+    auto scores = [&](uint32_t buf, f32x16 (&to)[2]) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[u][r] = 0.0f;
+            for (int r = 0; r < 16; ++r) to[u][r] = 0.0f;
 #pragma unroll
             for (int i = 0; i < QM; ++i) {
-                const u32x4 k = *(lds_u4)(buf + k_lane + u * 32 * T::kRow + (k_swz ^ (uint32_t)(i << 5)));
-                s[u] = mma32<F16>(k, q[i], s[u]);
+                const u32x4 k = *(lds_u4)(k_lane[i] + (buf + (uint32_t)(u * 32 * T::kRow)));
+                to[u] = mma32<F16>(k, q[i], to[u]);
             }
         }
-        if constexpr (MASKED) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    s[u][r] = k0 + 32 * u + 8 * (r >> 2) + 4 * g + (r & 3) <= lim ? s[u][r] : -__builtin_inff();
-        }
-        float top = s[0][0];
+    };
+    auto mask = [&](int t, f32x16 (&x)[2]) {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
-        top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
+            for (int r = 0; r < 16; ++r) x[u][r] = t * kKeys + 32 * u + 8 * (r >> 2) + 4 * g + (r & 3) <= lim ? x[u][r] : -__builtin_inff();
+    };
+    auto highest = [&](const f32x16 (&x)[2]) -> float {
+        float top = x[0][0];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, x[u][r]);
+        const u32x2 both = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false));
+        return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * a.scale_log2;
+    };
+    auto raise = [&](float top) {
         if (__builtin_amdgcn_ballot_w64(top > m_ref + kSlack || (m_ref == -__builtin_inff() && top > m_ref))) {
             const float m_new = fmaxf(m_ref, top);
             const float alpha = m_new > m_ref ? exp2_fast(m_ref - m_new) : 1.0f;
@@ -177,27 +187,54 @@ __global__ __launch_bounds__(kThreads, 2) void attn_prompt_kernel(Args a) {
 #pragma unroll
             for (int m = 0; m < OM; ++m) o[m] *= alpha;
         }
+    };
+    auto weigh = [&](const f32x16 (&x)[2], u32x4 (&p)[4]) {
         const float m_use = m_ref == -__builtin_inff() ? 0.0f : m_ref;
-        u32x4 p[4];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int r = 0; r < 16; r += 2) {
-                const float x = exp2_fast(fmaf(s[u][r], a.scale_log2, -m_use)), y = exp2_fast(fmaf(s[u][r + 1], a.scale_log2, -m_use));
-                l += x + y;
-                p[2 * u + (r >> 3)][(r >> 1) & 3] = f32x2_to_h16x2<F16>(x, y);
+                const float e = exp2_fast(fmaf(x[u][r], a.scale_log2, -m_use)), f = exp2_fast(fmaf(x[u][r + 1], a.scale_log2, -m_use));
+                l += e + f;
+                p[2 * u + (r >> 3)][(r >> 1) & 3] = f32x2_to_h16x2<F16>(e, f);
             }
-        auto v_operand = [&](int c, int m) -> u32x4 {
-            const uint32_t at = buf + v_lane + c * 16 * T::kRow + (v_swz ^ (uint32_t)(m << 6));
-            const u32x2 lo = lds_read_transposed(at), hi = lds_read_transposed(at + 8 * T::kRow);
-            return u32x4{lo[0], lo[1], hi[0], hi[1]};
-        };
-        if constexpr (!MASKED) {
+    };
+    auto v_operand = [&](uint32_t buf, int c, int m) -> u32x4 {
+        const uint32_t at = v_lane[m] + (buf + (uint32_t)(c * 16 * T::kRow));
+        const u32x2 lo = lds_read_transposed(at), hi = lds_read_transposed(at + 8 * T::kRow);
+        return u32x4{lo[0], lo[1], hi[0], hi[1]};
+    };
+
+    // Tile t, whose scores are there: its weights and its part of o, while the matrix cores make the next tile's scores.  THIS, NEXT: its
+    // parity, the next one's.  All queries see all keys of both tiles.
+    auto step = [&](int t, uint32_t even) {
+        loads_left<0>();
+        lds_barrier();                                          // k of t + 1 and v of t are there, and nobody reads the other tiles any more
+        if (t + 2 < tiles) copy_k(t + 2, even);
+        copy_v(t + 1, even ^ 1u);
+        f32x16 next[2];
+        u32x4 p[4];
+        scores((even ^ 1u) * T::kBytes, next);
+        weigh(s, p);
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+        for (int c = 0; c < 4; ++c)
 #pragma unroll
-                for (int m = 0; m < OM; ++m) o[m] = mma32<F16>(v_operand(c, m), p[c], o[m]);
-        } else {
+            for (int m = 0; m < OM; ++m) o[m] = mma32<F16>(v_operand(even * T::kBytes, c, m), p[c], o[m]);
+        s[0] = next[0];
+        s[1] = next[1];
+        raise(highest(s));
+    };
+    // The same where some query may not see some key of t or t + 1, or t is the last.
+    auto last_step = [&](int t, uint32_t even) {
+        const int k0 = t * kKeys;
+        const uint32_t buf = even * T::kBytes;
+        loads_left<0>();
+        lds_barrier();
+        if (t + 2 < tiles) copy_k(t + 2, even);
+        if (t + 1 < tiles) copy_v(t + 1, even ^ 1u);
+        if (!(a.causal && k0 > q_wave + 31 + ahead)) {          // (else no query of this wavefront sees a key of t or behind it)
+            u32x4 p[4];
+            weigh(s, p);
             // A key that some query does not see has weight 0 for it, and 0 times what is not finite would be NaN: keys with such
             // values are taken out of the product and added one by one to the queries that see them.
             constexpr uint32_t kExp = F16 ? 0x7C007C00u : 0x7F807F80u, kOne = F16 ? 0x04000400u : 0x00800080u;
@@ -207,7 +244,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_prompt_kernel(Args a) {
                 uint32_t bits[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
                 for (int m = 0; m < OM; ++m) {
-                    const u32x4 v = v_operand(c, m);
+                    const u32x4 v = v_operand(buf, c, m);
 #pragma unroll
                     for (int w = 0; w < 4; ++w) bits[w] |= (v[w] & kExp) + kOne;       // (an exponent of all ones carries into the half's top bit)
                 }
@@ -227,7 +264,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_prompt_kernel(Args a) {
 #pragma unroll
                 for (int w = 0; w < 4; ++w) keep[w] = ((mine >> (2 * w)) & 1u ? 0u : 0xFFFFu) | ((mine >> (2 * w + 1)) & 1u ? 0u : 0xFFFF0000u);
 #pragma unroll
-                for (int m = 0; m < OM; ++m) o[m] = mma32<F16>(v_operand(c, m) & keep, p[c], o[m]);
+                for (int m = 0; m < OM; ++m) o[m] = mma32<F16>(v_operand(buf, c, m) & keep, p[c], o[m]);
             }
 #pragma unroll 1
             while (bad) {
@@ -245,7 +282,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_prompt_kernel(Args a) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const uint32_t piece = (uint32_t)((4 * m + r) ^ T::swizzle_v(row));
-                        const u32x2 v = *(lds_u2)(buf + (uint32_t)T::kBytes + (uint32_t)(row * T::kRow) + 16u * piece + 8u * (uint32_t)g);
+                        const u32x2 v = *(lds_u2)(buf + 2u * T::kBytes + (uint32_t)(row * T::kRow) + 16u * piece + 8u * (uint32_t)g);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const float x = e & 1 ? h16hi_to_f32<F16>(v[e >> 1]) : h16lo_to_f32<F16>(v[e >> 1]);
@@ -253,12 +290,31 @@ __global__ __launch_bounds__(kThreads, 2) void attn_prompt_kernel(Args a) {
                         }
                     }
             }
+            if (t + 1 < tiles) {
+                scores((even ^ 1u) * T::kBytes, s);
+                mask(t + 1, s);
+                raise(highest(s));
+            }
         }
     };
-    const int whole = min(tiles, max(a.causal ? min(lk, q0 + ahead + 1) : lk, 0) / kKeys);
-    if (tiles > 0) copy(0, 0);
-    for (int t = 0; t < whole; ++t) step(t, std::false_type{});
-    for (int t = whole; t < tiles; ++t) step(t, std::true_type{});
+    const int whole = min(tiles, max(a.causal ? min(lk, q0 + ahead + 1) : lk, 0) / kKeys);      // tiles of which all queries see all keys
+    if (tiles > 0) {
+        copy_k(0, 0);
+        copy_v(0, 0);
+        if (tiles > 1) copy_k(1, 1);
+        loads_left<0>();
+        lds_barrier();
+        scores(0, s);
+        if (whole == 0) mask(0, s);
+        raise(highest(s));
+    }
+    int t = 0;
+    for (; t + 2 < whole; t += 2) {
+        step(t, 0u);
+        step(t + 1, 1u);
+    }
+#pragma unroll 1
+    for (; t < tiles; ++t) last_step(t, (uint32_t)(t & 1));
 
     l += __shfl_xor(l, 32);
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;              // (no key seen: o is 0 as well)
