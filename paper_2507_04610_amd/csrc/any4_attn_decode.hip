@@ -19,6 +19,21 @@
 // rounded weights, so that their rounding meets values around 0 as it does without codes.
 //
 // Rounding: scores, maxima, sums and accumulators are fp32; p (times vs) is rounded to 16 bits for the matrix cores, once.
+//
+// Who does what.  Lengths are the device's, so each block finds its share itself: a request has units of 32 tokens a wavefront (128 or
+// 256 tokens a block), all units of all requests and KV heads stand in one line, and the blocks that fit the chip take equal parts
+// of it.  However ragged the lengths, all blocks end together; a block cuts at most two groups (request, KV head), whose
+// pieces' sums and maxima go to the workspace, and the last of a group's pieces to come joins them in the same launch.  (A fixed
+// piece length had a block for each piece: 5 us of beginning and end for every one, 64 requests of 2048 .. 8192 tokens took 305 us with
+// 2048 tokens a piece and 441 with 512.)  Groups with fewer than kWholeUnits units on average are not cut for the sake of more blocks:
+// the join costs as much as four steps.
+//
+// Measured, 8 KV heads of 128, us (bytes of the cache / time):
+//     16 bits, 64 requests of 2048 .. 8192 tokens, 32 query heads          208   (6.5 TB/s; a copy reaches 4.9 read and written)
+//     8 bits, 32 requests of 1 .. 4096 tokens, 32 query heads               33   (4.2 TB/s)
+//     4 bits, one request of 131071 tokens, 64 query heads                  37   (3.8 TB/s: 24 us of streaming at 6 TB/s, 3 until the first
+//                                                                                bytes are asked for, 6 for the join of 32 pieces)
+//     16 bits, one request of 333 tokens, 32 query heads                     8.3 (loads that wait for each other: length, page, k and v)
 #include "any4_attn.h"
 #include "any4_internal.h"
 #include "any4_splitk.h"
@@ -171,6 +186,10 @@ template <class F> __device__ __forceinline__ float head_reduce(float v, F f) {
 // over all lanes of a wavefront
 template <class F> __device__ __forceinline__ float wave_reduce(float v, F f) { return head_reduce(lanes_reduce<16>(v, f), f); }
 
+// WAVES 8: one block for a compute unit, for few groups, whose pieces are then few to join (131071 tokens, 8 groups: 37 us, with 4 wavefronts
+// 45); WAVES 4: two or three, whose beginnings and ends overlap (32 requests, 256 groups: 33 us against 42).  AHEAD: a step's loads are out
+// before the step in front of it is worked on; otherwise the other wavefronts of the SIMD cover for it (8 bits and 4 wavefronts: 33.8 us against
+// 35.3 with, as more blocks fit).
 template <int BITS, int D, bool F16, int WAVES, bool AHEAD>
 __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(DecodeArgs a) {
     using C = Codes<BITS, F16>;
@@ -247,342 +266,342 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
         }
     }
     for (; at < end; ++request) {
-    const int len = (int)min((int64_t)max(scalar(a.lengths)[request], 0), capacity);
-    const scalar_i32 table = scalar(a.table + (int64_t)request * a.table_stride);
-    const unsigned begin = many ? __builtin_amdgcn_readfirstlane(begins[request]) : __builtin_amdgcn_readlane(lane_begin, request & 63);
-    const unsigned units = (many ? __builtin_amdgcn_readfirstlane(begins[request + 1]) : __builtin_amdgcn_readlane(lane_end, request & 63)) - begin;
-    const unsigned request_at = begin * groups;
-    for (int group = (int)((at - request_at) / units); group < (int)groups && at < end; ++group) {
-    const unsigned group_at = request_at + (unsigned)group * units;
-    const int from = (int)(at - group_at), to = (int)min(units, end - group_at);
-    at = group_at + (unsigned)to;
-    const int kv_head = a.head_tiles == 1 ? group : group / a.head_tiles;
-    const int head_tile = group - kv_head * a.head_tiles;
-    const int first_head = kv_head * a.shared + head_tile * 16, here = min(16, a.shared - head_tile * 16);
-    const int t0 = from * UNIT, t1 = min(len, to * UNIT);
+        const int len = (int)min((int64_t)max(scalar(a.lengths)[request], 0), capacity);
+        const scalar_i32 table = scalar(a.table + (int64_t)request * a.table_stride);
+        const unsigned begin = many ? __builtin_amdgcn_readfirstlane(begins[request]) : __builtin_amdgcn_readlane(lane_begin, request & 63);
+        const unsigned units = (many ? __builtin_amdgcn_readfirstlane(begins[request + 1]) : __builtin_amdgcn_readlane(lane_end, request & 63)) - begin;
+        const unsigned request_at = begin * groups;
+        for (int group = (int)((at - request_at) / units); group < (int)groups && at < end; ++group) {
+            const unsigned group_at = request_at + (unsigned)group * units;
+            const int from = (int)(at - group_at), to = (int)min(units, end - group_at);
+            at = group_at + (unsigned)to;
+            const int kv_head = a.head_tiles == 1 ? group : group / a.head_tiles;
+            const int head_tile = group - kv_head * a.head_tiles;
+            const int first_head = kv_head * a.shared + head_tile * 16, here = min(16, a.shared - head_tile * 16);
+            const int t0 = from * UNIT, t1 = min(len, to * UNIT);
 
-    float m_ref = -__builtin_inff(), l = 0.0f, vo_sum = 0.0f;
-    f32x4 o[VM], ones_sum = {0.0f, 0.0f, 0.0f, 0.0f};
+            float m_ref = -__builtin_inff(), l = 0.0f, vo_sum = 0.0f;
+            f32x4 o[VM], ones_sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int m = 0; m < VM; ++m) o[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    // fp16 weights p * vs: held as p * (vs * 2^-exponent), with the largest vs so far between 1 and 2, or small scales would leave fp16's range
-    int exponent = -126;
+            for (int m = 0; m < VM; ++m) o[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            // fp16 weights p * vs: held as p * (vs * 2^-exponent), with the largest vs so far between 1 and 2, or small scales would leave fp16's range
+            int exponent = -126;
 
-    // One step's tokens: which of the two 16s' exist, and what the lanes load of them.
-    struct Step {
-        int there[2];
-        uint32_t kw[2][KW], vw[8][VW];
-        u32x4 so[2][2];
-    };
-    const int page_mask = (1 << a.c.page_shift) - 1;
-    // the pages of a step at t (its own, again, past the end)
-    auto pages_of = [&](int t, int (&page)[2]) {
+            // One step's tokens: which of the two 16s' exist, and what the lanes load of them.
+            struct Step {
+                int there[2];
+                uint32_t kw[2][KW], vw[8][VW];
+                u32x4 so[2][2];
+            };
+            const int page_mask = (1 << a.c.page_shift) - 1;
+            // the pages of a step at t (its own, again, past the end)
+            auto pages_of = [&](int t, int (&page)[2]) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int th = t + 16 * h < t1 ? t + 16 * h : t < t1 ? t : t0;
-            page[h] = table[th >> a.c.page_shift];
-        }
-    };
-    auto load = [&](int t, const int (&page)[2], Step& st) {
-        int64_t tok[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int th = t + 16 * h < t1 ? t + 16 * h : t;
-            const bool ok = page[h] >= 0 && page[h] < a.c.pages;           // a page that does not exist has no tokens
-            st.there[h] = ok ? min(max(len - (t + 16 * h), 0), 16) : 0;
-            tok[h] = a.c.first_token(ok ? page[h] : 0, kv_head) + (th & page_mask);
-            const uint8_t* kp = a.c.k + tok[h] * ROW;
-            if constexpr (BITS == 16) {
-#pragma unroll
-                for (int i = 0; i < KM; ++i) {
-                    const u32x4 x = load_once<u32x4>(kp + (uint32_t)(col * ROW + 64 * i + 16 * g));
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) st.kw[h][4 * i + j] = x[j];
+                for (int h = 0; h < 2; ++h) {
+                    const int th = t + 16 * h < t1 ? t + 16 * h : t < t1 ? t : t0;
+                    page[h] = table[th >> a.c.page_shift];
                 }
-            } else {
-                load_words(kp + (uint32_t)(col * ROW + (ROW / 4) * g), st.kw[h]);
-                const uint8_t* sp = reinterpret_cast<const uint8_t*>(a.c.scales + tok[h] * 4) + (uint32_t)(32 * g);
-                st.so[h][0] = load_once<u32x4>(sp);
-                st.so[h][1] = load_once<u32x4>(sp + 16);
-            }
-        }
+            };
+            auto load = [&](int t, const int (&page)[2], Step& st) {
+                int64_t tok[2];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint8_t* vp = a.c.v + tok[j >> 2] * ROW + (uint32_t)((4 * g + (j & 3)) * ROW + VB * col);
-            if constexpr (VB == 2) st.vw[j][0] = load_once<uint16_t>(vp);
-            else load_words(vp, st.vw[j]);
-        }
-    };
-
-    // A step's loads are out before the step in front of it is worked on, its pages' numbers one step earlier.
-    Step st;
-    int page[2];
-    const int first = t0 + kStep * wave;
-    pages_of(first, page);
-    u32x4 q[KM];
-    {
-        int q_lane = lane;
-        asm volatile("" : "+v"(q_lane));
-        const int col = q_lane & 15, g = q_lane >> 4;
-        const uint16_t* qp = a.q.p + (int64_t)request * a.q.token + (int64_t)(first_head + min(col, here - 1)) * a.q.head;
+                for (int h = 0; h < 2; ++h) {
+                    const int th = t + 16 * h < t1 ? t + 16 * h : t;
+                    const bool ok = page[h] >= 0 && page[h] < a.c.pages;           // a page that does not exist has no tokens
+                    st.there[h] = ok ? min(max(len - (t + 16 * h), 0), 16) : 0;
+                    tok[h] = a.c.first_token(ok ? page[h] : 0, kv_head) + (th & page_mask);
+                    const uint8_t* kp = a.c.k + tok[h] * ROW;
+                    if constexpr (BITS == 16) {
 #pragma unroll
-        for (int i = 0; i < KM; ++i) q[i] = *reinterpret_cast<const u32x4*>(qp + (QUANT ? (D / 4) * g + 8 * i : 32 * i + 8 * g));
-    }
-    if (AHEAD && first < t1) load(first, page, st);
-    if (AHEAD) pages_of(first + UNIT, page);
-    __builtin_amdgcn_sched_barrier(0);
-    // Q^T, columns past `here` are zeros
-    float sum_q = 0.0f;
+                        for (int i = 0; i < KM; ++i) {
+                            const u32x4 x = load_once<u32x4>(kp + (uint32_t)(col * ROW + 64 * i + 16 * g));
 #pragma unroll
-    for (int i = 0; i < KM; ++i) {
-        if (col >= here) q[i] = u32x4{0u, 0u, 0u, 0u};
-        if constexpr (QUANT) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sum_q += h16lo_to_f32<F16>(q[i][j]) + h16hi_to_f32<F16>(q[i][j]);
-        }
-        if constexpr (BITS == 4) {                              // pairs (x, x + 4), as the codes come
-            const u32x4 r = q[i];
-            q[i] = u32x4{__builtin_amdgcn_perm(r[2], r[0], 0x05040100u), __builtin_amdgcn_perm(r[2], r[0], 0x07060302u),
-                         __builtin_amdgcn_perm(r[3], r[1], 0x05040100u), __builtin_amdgcn_perm(r[3], r[1], 0x07060302u)};
-        }
-    }
-    if constexpr (QUANT) sum_q = head_reduce(sum_q, [](float x, float y) { return x + y; }) * a.scale_log2;
-    for (int t = first; t < t1; t += UNIT) {
-        Step next;
-        if (!AHEAD) load(t, page, st);
-        if (AHEAD && t + UNIT < t1) load(t + UNIT, page, next);
-        pages_of(t + (AHEAD ? 2 : 1) * UNIT, page);
-        __builtin_amdgcn_sched_barrier(0);                      // (left alone, the loads sink to where their values are used)
-        auto& kw = st.kw;
-        auto& vw = st.vw;
-        auto& so = st.so;
-        const int there[2] = {st.there[0], st.there[1]};
-
-        f32x4 s[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            s[h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int i = 0; i < KM; ++i) s[h] = mma16<F16>(k_operand<BITS, F16>(kw[h], i), q[i], s[h]);
-        }
-        float x[8], vs[8], vo[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int h = j >> 2, r = j & 3;
-            if constexpr (QUANT) {
-                const uint32_t kk = so[h][r >> 1][2 * (r & 1)], vv = so[h][r >> 1][2 * (r & 1) + 1];
-                const float u = fmaf(s[h][r], a.scale_log2, -(float)C::kBias * sum_q);
-                x[j] = fmaf(bf16lo_to_f32(kk), u, bf16hi_to_f32(kk) * sum_q);
-                vs[j] = bf16lo_to_f32(vv);
-                vo[j] = fmaf((float)C::kCentre, vs[j], bf16hi_to_f32(vv));
-            } else {
-                x[j] = s[h][r] * a.scale_log2;
-            }
-        }
-        if (there[0] + there[1] < 32) {
-            // what lies behind the last token, or in a page that does not exist, may be anything: none of it comes near a sum
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bool ok = 4 * g + (j & 3) < there[j >> 2];
-                x[j] = ok ? x[j] : -__builtin_inff();
-                if constexpr (QUANT) {
-                    vs[j] = ok ? vs[j] : 0.0f;
-                    vo[j] = ok ? vo[j] : 0.0f;
-                } else {
-#pragma unroll
-                    for (int w = 0; w < VW; ++w) vw[j][w] = ok ? vw[j][w] : 0u;
+                            for (int j = 0; j < 4; ++j) st.kw[h][4 * i + j] = x[j];
+                        }
+                    } else {
+                        load_words(kp + (uint32_t)(col * ROW + (ROW / 4) * g), st.kw[h]);
+                        const uint8_t* sp = reinterpret_cast<const uint8_t*>(a.c.scales + tok[h] * 4) + (uint32_t)(32 * g);
+                        st.so[h][0] = load_once<u32x4>(sp);
+                        st.so[h][1] = load_once<u32x4>(sp + 16);
+                    }
                 }
-            }
-        }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint8_t* vp = a.c.v + tok[j >> 2] * ROW + (uint32_t)((4 * g + (j & 3)) * ROW + VB * col);
+                    if constexpr (VB == 2) st.vw[j][0] = load_once<uint16_t>(vp);
+                    else load_words(vp, st.vw[j]);
+                }
+            };
 
-        float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-        top = head_reduce(top, [](float u, float v) { return fmaxf(u, v); });
-        float factor = 1.0f;
-        bool moved = top > m_ref;
-        if constexpr (QUANT && F16) {
-            float big = 0.0f;
+            // A step's loads are out before the step in front of it is worked on, its pages' numbers one step earlier.
+            Step st;
+            int page[2];
+            const int first = t0 + kStep * wave;
+            pages_of(first, page);
+            u32x4 q[KM];
+            {
+                int q_lane = lane;
+                asm volatile("" : "+v"(q_lane));
+                const int col = q_lane & 15, g = q_lane >> 4;
+                const uint16_t* qp = a.q.p + (int64_t)request * a.q.token + (int64_t)(first_head + min(col, here - 1)) * a.q.head;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) big = fmaxf(big, fabsf(vs[j]));
-            big = head_reduce(big, [](float u, float v) { return fmaxf(u, v); });
-            const int e = min(max((int)(__float_as_uint(big) >> 23) - 127, -126), 126);
-            if (e > exponent) {
-                factor = __builtin_ldexpf(1.0f, max(exponent - e, -126));
-                exponent = e;
-                moved = true;
+                for (int i = 0; i < KM; ++i) q[i] = *reinterpret_cast<const u32x4*>(qp + (QUANT ? (D / 4) * g + 8 * i : 32 * i + 8 * g));
             }
-        }
-        if (__builtin_amdgcn_ballot_w64(moved)) {
-            const float m_new = fmaxf(m_ref, top);
-            const float alpha = m_new > m_ref ? exp2_fast(m_ref - m_new) : 1.0f;
-            m_ref = m_new;
-            l *= alpha;
-            vo_sum *= alpha;
-            const float f = alpha * factor;
-            ones_sum *= f;
+            if (AHEAD && first < t1) load(first, page, st);
+            if (AHEAD) pages_of(first + UNIT, page);
+            __builtin_amdgcn_sched_barrier(0);
+            // Q^T, columns past `here` are zeros
+            float sum_q = 0.0f;
 #pragma unroll
-            for (int m = 0; m < VM; ++m) o[m] *= f;
-        }
-        const float m_use = m_ref == -__builtin_inff() ? 0.0f : m_ref;
-        const float unit = __builtin_ldexpf(1.0f, -exponent);
-        u32x4 p;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            x[j] = exp2_fast(x[j] - m_use);
-            l += x[j];
-            if constexpr (QUANT) {
-                vo_sum = fmaf(x[j], vo[j], vo_sum);
-                x[j] *= F16 ? vs[j] * unit : vs[j];
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) p[j] = f32x2_to_h16x2<F16>(x[2 * j], x[2 * j + 1]);
-        if constexpr (QUANT) {
-            constexpr uint32_t kOnes = F16 ? 0x3C003C00u : 0x3F803F80u;
-            ones_sum = mma16<F16>(u32x4{kOnes, kOnes, kOnes, kOnes}, p, ones_sum);
-        }
-#pragma unroll
-        for (int m = 0; m < VM; ++m) {
-            u32x4 v;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = v_pair<BITS, F16>(vw[2 * j], vw[2 * j + 1], m);
-            o[m] = mma16<F16>(v, p, o[m]);
-        }
-        if (AHEAD) st = next;
-    }
-
-    // (the lane's number anew: what follows from it below is not to take registers from the loop above)
-    int thread = threadIdx.x;
-    asm volatile("" : "+v"(thread));
-    const int col_e = thread & 15, g_e = (thread >> 4) & 3;
-    // The wavefronts' results meet in LDS: [wave][head][PAD], then [wave][head] maximum and sum of weights.
-    auto add = [](float u, float v) { return u + v; };
-    l = head_reduce(l, add);
-    if constexpr (QUANT) vo_sum = head_reduce(vo_sum, add);
-    float* ml = lds + WAVES * here * PAD;
-    __syncthreads();                                            // (nobody reads what another piece left there)
-    if (col_e < here) {
-        const float back = QUANT && F16 ? __builtin_ldexpf(1.0f, exponent) : 1.0f;
-        float* to_lds = lds + (wave * here + col_e) * PAD;
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int m = 0; m < VM; m += 4) {
-                f32x4 v = {o[m][r], o[m + 1][r], o[m + 2][r], o[m + 3][r]};
+            for (int i = 0; i < KM; ++i) {
+                if (col >= here) q[i] = u32x4{0u, 0u, 0u, 0u};
                 if constexpr (QUANT) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = fmaf(back, v[j] - (float)(C::kBias + C::kCentre) * ones_sum[0], vo_sum);
+                    for (int j = 0; j < 4; ++j) sum_q += h16lo_to_f32<F16>(q[i][j]) + h16hi_to_f32<F16>(q[i][j]);
                 }
-                *reinterpret_cast<f32x4*>(to_lds + VM * (4 * g_e + r) + m) = v;
+                if constexpr (BITS == 4) {                              // pairs (x, x + 4), as the codes come
+                    const u32x4 r = q[i];
+                    q[i] = u32x4{__builtin_amdgcn_perm(r[2], r[0], 0x05040100u), __builtin_amdgcn_perm(r[2], r[0], 0x07060302u),
+                                 __builtin_amdgcn_perm(r[3], r[1], 0x05040100u), __builtin_amdgcn_perm(r[3], r[1], 0x07060302u)};
+                }
             }
-        if (g_e == 0) {
-            ml[2 * (wave * here + col_e)] = m_ref;
-            ml[2 * (wave * here + col_e) + 1] = l;
-        }
-    }
-    __syncthreads();
-    uint16_t* out = a.out + ((int64_t)request * a.heads + first_head) * D;
-    const bool split = from > 0 || to < units;
-    // A block has at most two groups that it shares with others: one that begins in front of it, one that goes on behind it.
-    float* mine = a.partial + ((int64_t)blockIdx.x * 2 + (from > 0 ? 0 : 1)) * room;
-    for (int i = thread; i < here * D / 2; i += THREADS) {      // two places of a head each
-        const int n = i / (D / 2), d = 2 * i - n * D;
-        float top = -__builtin_inff();
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ml[2 * (w * here + n)]);
-        const float use = top == -__builtin_inff() ? 0.0f : top;
-        float sum = 0.0f;
-        f32x2 v = {0.0f, 0.0f};
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            const float f = exp2_fast(ml[2 * (w * here + n)] - use);
-            sum = fmaf(f, ml[2 * (w * here + n) + 1], sum);
-            const f32x2 x = *reinterpret_cast<const f32x2*>(lds + (w * here + n) * PAD + d);
-            v = f32x2{fmaf(f, x[0], v[0]), fmaf(f, x[1], v[1])};
-        }
-        if (!split) {
-            reinterpret_cast<uint32_t*>(out)[i] = sum == 0.0f ? 0u : f32x2_to_h16x2<F16>(v[0] / sum, v[1] / sum);
-        } else {
-            store_pair(mine + 2 * i, v);
-            if (d == 0) store_pair(mine + here * D + 2 * n, f32x2{top, sum});
-        }
-    }
-    if (!split) continue;
+            if constexpr (QUANT) sum_q = head_reduce(sum_q, [](float x, float y) { return x + y; }) * a.scale_log2;
+            for (int t = first; t < t1; t += UNIT) {
+                Step next;
+                if (!AHEAD) load(t, page, st);
+                if (AHEAD && t + UNIT < t1) load(t + UNIT, page, next);
+                pages_of(t + (AHEAD ? 2 : 1) * UNIT, page);
+                __builtin_amdgcn_sched_barrier(0);                      // (left alone, the loads sink to where their values are used)
+                auto& kw = st.kw;
+                auto& vw = st.vw;
+                auto& so = st.so;
+                const int there[2] = {st.there[0], st.there[1]};
 
-    // The last piece of a group to come adds all of them: first the pieces' factors, a wavefront for a head and a lane for a piece,
-    // then the sums in the pieces' order, with the pieces dealt out to as many threads as there are for each two places.  (One compute
-    // unit reads what the others wrote: all its loads are out at once, or this takes longer than the rest of a short call.)
-    const int first_block = block_of(group_at), pieces = block_of(group_at + units - 1) - first_block + 1;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    int* last = reinterpret_cast<int*>(lds);
-    if (thread == 0)
-        *last = arrive_piece(reinterpret_cast<unsigned long long*>(a.words + ((int64_t)request * groups + group) * kWordBytes), pieces);
-    __syncthreads();
-    const bool joins = *last != 0;
-    __syncthreads();
-    if (!joins) continue;
-    // (the first piece lies in its block's second place, the others in their blocks' first)
-    const float* base = a.partial + (int64_t)first_block * 2 * room;
-    auto piece_at = [&](int w) -> const float* { return base + (w == 0 ? room : w * 2 * room); };
-    const int items = here * D / 2, slices = max(THREADS / items, 1), span = (pieces + slices - 1) / slices;
-    const int slice = thread / items, w_first = slice * span, w_end = slice < slices ? min(pieces, w_first + span) : 0;
-    float* factor = lds;                                        // [head][pieces]
-    float* parts = lds + here * pieces;                         // [slice][items][2], behind the factors
-    f32x2 x[kJoin];
-    auto load_parts = [&](int w0, int i) {
+                f32x4 s[2];
 #pragma unroll
-        for (int w = 0; w < kJoin; ++w)
-            x[w] = w0 + w < w_end && i < items ? load_pair(piece_at(w0 + w) + 2 * i) : f32x2{0.0f, 0.0f};
-    };
-    auto load_ml = [&](int w, int n) -> f32x2 {
-        return w < pieces && n < here ? load_pair(piece_at(w) + here * D + 2 * n) : f32x2{-__builtin_inff(), 0.0f};
-    };
-    const int lane_e = thread & 63;
-    f32x2 ml_of = load_ml(lane_e, wave);
-    load_parts(w_first, thread - slice * items);                // (on their way while the factors are made)
-    for (int n = wave; n < here; n += WAVES) {
-        if (n != wave) ml_of = load_ml(lane_e, n);
-        float top = -__builtin_inff(), sum = 0.0f;
-        for (int w = lane_e; w < pieces; w += 64) {
-            if (w >= 64) ml_of = load_ml(w, n);
-            factor[n * pieces + w] = ml_of[0];
-            const float higher = fmaxf(top, ml_of[0]), use = higher == -__builtin_inff() ? 0.0f : higher;
-            sum = fmaf(exp2_fast(top - use), sum, exp2_fast(ml_of[0] - use) * ml_of[1]);
-            top = higher;
-        }
-        const float own_top = top;
-        top = wave_reduce(top, [](float u, float v) { return fmaxf(u, v); });
-        const float use = top == -__builtin_inff() ? 0.0f : top;
-        sum = wave_reduce(sum * exp2_fast(own_top - use), add);
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        for (int w = lane_e; w < pieces; w += 64) factor[n * pieces + w] = exp2_fast(factor[n * pieces + w] - use) * inv;
-    }
-    __syncthreads();
-    for (int i0 = 0; i0 < items; i0 += THREADS) {
-        const int i = i0 + thread - slice * items, n = min(i / (D / 2), here - 1);
-        if (i0 > 0) load_parts(w_first, i);
-        f32x2 v = {0.0f, 0.0f};
-        for (int w0 = w_first; w0 < w_end; w0 += kJoin) {
-            if (w0 > w_first) load_parts(w0, i);
+                for (int h = 0; h < 2; ++h) {
+                    s[h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int w = 0; w < kJoin; ++w)
-                if (w0 + w < w_end) {
-                    const float f = factor[n * pieces + w0 + w];
-                    v = f32x2{fmaf(f, x[w][0], v[0]), fmaf(f, x[w][1], v[1])};
+                    for (int i = 0; i < KM; ++i) s[h] = mma16<F16>(k_operand<BITS, F16>(kw[h], i), q[i], s[h]);
                 }
-        }
-        if (slices > 1) {
-            if (slice < slices) reinterpret_cast<f32x2*>(parts)[thread] = v;
+                float x[8], vs[8], vo[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int h = j >> 2, r = j & 3;
+                    if constexpr (QUANT) {
+                        const uint32_t kk = so[h][r >> 1][2 * (r & 1)], vv = so[h][r >> 1][2 * (r & 1) + 1];
+                        const float u = fmaf(s[h][r], a.scale_log2, -(float)C::kBias * sum_q);
+                        x[j] = fmaf(bf16lo_to_f32(kk), u, bf16hi_to_f32(kk) * sum_q);
+                        vs[j] = bf16lo_to_f32(vv);
+                        vo[j] = fmaf((float)C::kCentre, vs[j], bf16hi_to_f32(vv));
+                    } else {
+                        x[j] = s[h][r] * a.scale_log2;
+                    }
+                }
+                if (there[0] + there[1] < 32) {
+                    // what lies behind the last token, or in a page that does not exist, may be anything: none of it comes near a sum
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const bool ok = 4 * g + (j & 3) < there[j >> 2];
+                        x[j] = ok ? x[j] : -__builtin_inff();
+                        if constexpr (QUANT) {
+                            vs[j] = ok ? vs[j] : 0.0f;
+                            vo[j] = ok ? vo[j] : 0.0f;
+                        } else {
+#pragma unroll
+                            for (int w = 0; w < VW; ++w) vw[j][w] = ok ? vw[j][w] : 0u;
+                        }
+                    }
+                }
+
+                float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+                top = head_reduce(top, [](float u, float v) { return fmaxf(u, v); });
+                float factor = 1.0f;
+                bool moved = top > m_ref;
+                if constexpr (QUANT && F16) {
+                    float big = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) big = fmaxf(big, fabsf(vs[j]));
+                    big = head_reduce(big, [](float u, float v) { return fmaxf(u, v); });
+                    const int e = min(max((int)(__float_as_uint(big) >> 23) - 127, -126), 126);
+                    if (e > exponent) {
+                        factor = __builtin_ldexpf(1.0f, max(exponent - e, -126));
+                        exponent = e;
+                        moved = true;
+                    }
+                }
+                if (__builtin_amdgcn_ballot_w64(moved)) {
+                    const float m_new = fmaxf(m_ref, top);
+                    const float alpha = m_new > m_ref ? exp2_fast(m_ref - m_new) : 1.0f;
+                    m_ref = m_new;
+                    l *= alpha;
+                    vo_sum *= alpha;
+                    const float f = alpha * factor;
+                    ones_sum *= f;
+#pragma unroll
+                    for (int m = 0; m < VM; ++m) o[m] *= f;
+                }
+                const float m_use = m_ref == -__builtin_inff() ? 0.0f : m_ref;
+                const float unit = __builtin_ldexpf(1.0f, -exponent);
+                u32x4 p;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    x[j] = exp2_fast(x[j] - m_use);
+                    l += x[j];
+                    if constexpr (QUANT) {
+                        vo_sum = fmaf(x[j], vo[j], vo_sum);
+                        x[j] *= F16 ? vs[j] * unit : vs[j];
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) p[j] = f32x2_to_h16x2<F16>(x[2 * j], x[2 * j + 1]);
+                if constexpr (QUANT) {
+                    constexpr uint32_t kOnes = F16 ? 0x3C003C00u : 0x3F803F80u;
+                    ones_sum = mma16<F16>(u32x4{kOnes, kOnes, kOnes, kOnes}, p, ones_sum);
+                }
+#pragma unroll
+                for (int m = 0; m < VM; ++m) {
+                    u32x4 v;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = v_pair<BITS, F16>(vw[2 * j], vw[2 * j + 1], m);
+                    o[m] = mma16<F16>(v, p, o[m]);
+                }
+                if (AHEAD) st = next;
+            }
+
+            // (the lane's number anew: what follows from it below is not to take registers from the loop above)
+            int thread = threadIdx.x;
+            asm volatile("" : "+v"(thread));
+            const int col_e = thread & 15, g_e = (thread >> 4) & 3;
+            // The wavefronts' results meet in LDS: [wave][head][PAD], then [wave][head] maximum and sum of weights.
+            auto add = [](float u, float v) { return u + v; };
+            l = head_reduce(l, add);
+            if constexpr (QUANT) vo_sum = head_reduce(vo_sum, add);
+            float* ml = lds + WAVES * here * PAD;
+            __syncthreads();                                            // (nobody reads what another piece left there)
+            if (col_e < here) {
+                const float back = QUANT && F16 ? __builtin_ldexpf(1.0f, exponent) : 1.0f;
+                float* to_lds = lds + (wave * here + col_e) * PAD;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int m = 0; m < VM; m += 4) {
+                        f32x4 v = {o[m][r], o[m + 1][r], o[m + 2][r], o[m + 3][r]};
+                        if constexpr (QUANT) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) v[j] = fmaf(back, v[j] - (float)(C::kBias + C::kCentre) * ones_sum[0], vo_sum);
+                        }
+                        *reinterpret_cast<f32x4*>(to_lds + VM * (4 * g_e + r) + m) = v;
+                    }
+                if (g_e == 0) {
+                    ml[2 * (wave * here + col_e)] = m_ref;
+                    ml[2 * (wave * here + col_e) + 1] = l;
+                }
+            }
             __syncthreads();
-            if (slice == 0)
-                for (int s = 1; s < slices; ++s) {
-                    const f32x2 other = reinterpret_cast<const f32x2*>(parts)[s * items + i];
-                    v = f32x2{v[0] + other[0], v[1] + other[1]};
+            uint16_t* out = a.out + ((int64_t)request * a.heads + first_head) * D;
+            const bool split = from > 0 || to < units;
+            // A block has at most two groups that it shares with others: one that begins in front of it, one that goes on behind it.
+            float* mine = a.partial + ((int64_t)blockIdx.x * 2 + (from > 0 ? 0 : 1)) * room;
+            for (int i = thread; i < here * D / 2; i += THREADS) {      // two places of a head each
+                const int n = i / (D / 2), d = 2 * i - n * D;
+                float top = -__builtin_inff();
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ml[2 * (w * here + n)]);
+                const float use = top == -__builtin_inff() ? 0.0f : top;
+                float sum = 0.0f;
+                f32x2 v = {0.0f, 0.0f};
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) {
+                    const float f = exp2_fast(ml[2 * (w * here + n)] - use);
+                    sum = fmaf(f, ml[2 * (w * here + n) + 1], sum);
+                    const f32x2 x = *reinterpret_cast<const f32x2*>(lds + (w * here + n) * PAD + d);
+                    v = f32x2{fmaf(f, x[0], v[0]), fmaf(f, x[1], v[1])};
                 }
+                if (!split) {
+                    reinterpret_cast<uint32_t*>(out)[i] = sum == 0.0f ? 0u : f32x2_to_h16x2<F16>(v[0] / sum, v[1] / sum);
+                } else {
+                    store_pair(mine + 2 * i, v);
+                    if (d == 0) store_pair(mine + here * D + 2 * n, f32x2{top, sum});
+                }
+            }
+            if (!split) continue;
+
+            // The last piece of a group to come adds all of them: first the pieces' factors, a wavefront for a head and a lane for a piece,
+            // then the sums in the pieces' order, with the pieces dealt out to as many threads as there are for each two places.  (One compute
+            // unit reads what the others wrote: all its loads are out at once, or this takes longer than the rest of a short call.)
+            const int first_block = block_of(group_at), pieces = block_of(group_at + units - 1) - first_block + 1;
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            int* last = reinterpret_cast<int*>(lds);
+            if (thread == 0)
+                *last = arrive_piece(reinterpret_cast<unsigned long long*>(a.words + ((int64_t)request * groups + group) * kWordBytes), pieces);
+            __syncthreads();
+            const bool joins = *last != 0;
+            __syncthreads();
+            if (!joins) continue;
+            // (the first piece lies in its block's second place, the others in their blocks' first)
+            const float* base = a.partial + (int64_t)first_block * 2 * room;
+            auto piece_at = [&](int w) -> const float* { return base + (w == 0 ? room : w * 2 * room); };
+            const int items = here * D / 2, slices = max(THREADS / items, 1), span = (pieces + slices - 1) / slices;
+            const int slice = thread / items, w_first = slice * span, w_end = slice < slices ? min(pieces, w_first + span) : 0;
+            float* factor = lds;                                        // [head][pieces]
+            float* parts = lds + here * pieces;                         // [slice][items][2], behind the factors
+            f32x2 x[kJoin];
+            auto load_parts = [&](int w0, int i) {
+#pragma unroll
+                for (int w = 0; w < kJoin; ++w)
+                    x[w] = w0 + w < w_end && i < items ? load_pair(piece_at(w0 + w) + 2 * i) : f32x2{0.0f, 0.0f};
+            };
+            auto load_ml = [&](int w, int n) -> f32x2 {
+                return w < pieces && n < here ? load_pair(piece_at(w) + here * D + 2 * n) : f32x2{-__builtin_inff(), 0.0f};
+            };
+            const int lane_e = thread & 63;
+            f32x2 ml_of = load_ml(lane_e, wave);
+            load_parts(w_first, thread - slice * items);                // (on their way while the factors are made)
+            for (int n = wave; n < here; n += WAVES) {
+                if (n != wave) ml_of = load_ml(lane_e, n);
+                float top = -__builtin_inff(), sum = 0.0f;
+                for (int w = lane_e; w < pieces; w += 64) {
+                    if (w >= 64) ml_of = load_ml(w, n);
+                    factor[n * pieces + w] = ml_of[0];
+                    const float higher = fmaxf(top, ml_of[0]), use = higher == -__builtin_inff() ? 0.0f : higher;
+                    sum = fmaf(exp2_fast(top - use), sum, exp2_fast(ml_of[0] - use) * ml_of[1]);
+                    top = higher;
+                }
+                const float own_top = top;
+                top = wave_reduce(top, [](float u, float v) { return fmaxf(u, v); });
+                const float use = top == -__builtin_inff() ? 0.0f : top;
+                sum = wave_reduce(sum * exp2_fast(own_top - use), add);
+                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                for (int w = lane_e; w < pieces; w += 64) factor[n * pieces + w] = exp2_fast(factor[n * pieces + w] - use) * inv;
+            }
+            __syncthreads();
+            for (int i0 = 0; i0 < items; i0 += THREADS) {
+                const int i = i0 + thread - slice * items, n = min(i / (D / 2), here - 1);
+                if (i0 > 0) load_parts(w_first, i);
+                f32x2 v = {0.0f, 0.0f};
+                for (int w0 = w_first; w0 < w_end; w0 += kJoin) {
+                    if (w0 > w_first) load_parts(w0, i);
+#pragma unroll
+                    for (int w = 0; w < kJoin; ++w)
+                        if (w0 + w < w_end) {
+                            const float f = factor[n * pieces + w0 + w];
+                            v = f32x2{fmaf(f, x[w][0], v[0]), fmaf(f, x[w][1], v[1])};
+                        }
+                }
+                if (slices > 1) {
+                    if (slice < slices) reinterpret_cast<f32x2*>(parts)[thread] = v;
+                    __syncthreads();
+                    if (slice == 0)
+                        for (int s = 1; s < slices; ++s) {
+                            const f32x2 other = reinterpret_cast<const f32x2*>(parts)[s * items + i];
+                            v = f32x2{v[0] + other[0], v[1] + other[1]};
+                        }
+                }
+                if (i < items && slice == 0) reinterpret_cast<uint32_t*>(out)[i] = f32x2_to_h16x2<F16>(v[0], v[1]);
+            }
         }
-        if (i < items && slice == 0) reinterpret_cast<uint32_t*>(out)[i] = f32x2_to_h16x2<F16>(v[0], v[1]);
-    }
-    }
     }
 }
 

@@ -4,6 +4,9 @@
 // The inputs of a block are pieces of 256 bytes a token, its cache side is one contiguous piece where the tokens are
 // neighbours: with 4 bits 1 KB rather than the 64-byte pieces that a block of one token and all heads would write.  Both
 // kernels read every byte once and write every byte once; memory bounds them.
+//
+// Measured, 8 KV heads of 128, us of the kernel: 16384 tokens into 16 bits 30 (134 MB, 4.5 TB/s), 65536 out of it 102 (537 MB, 5.3 TB/s),
+// 32768 out of 4 bits 26 (171 MB, 6.5 TB/s), 2047 into 8 bits 6.6 and out of it 4.0, 16 into 16 bits 2.
 #include "any4_attn.h"
 
 namespace any4 {
