@@ -12,7 +12,8 @@
  *
  * Conventions for every entry point
  *   - All data pointers are DEVICE pointers owned by the caller.  The library never
- *     allocates, frees or keeps them.  All matrices are dense, row-major, no strides.
+ *     allocates, frees or keeps them.  All matrices are dense, row-major, no strides (the inputs of the key-value
+ *     cache and of attention excepted, see there).
  *   - bf16 values travel as uint16_t bit patterns.
  *   - Work is enqueued on `stream` (a hipStream_t passed as void*, NULL = the default
  *     stream) and the call returns without waiting for it.
@@ -336,7 +337,8 @@ int any4_kv_read(const any4_kv_cache* cache, const int64_t* slots, int64_t token
  *     s_j = softmax_scale * q . k_j,   out = sum_j softmax(s)_j v_j
  * Query head h reads KV head h / (heads / kv_heads).  A request without a token gets zeros.  Scores, softmax and sums
  * are fp32; the weights are rounded to 16 bits for the matrix cores, the result once to the output's type.  The result is
- * reproducible run to run; its last bits may depend on the page table's width and on the number of requests.
+ * reproducible run to run; its last bits may depend on the page table's width and on the lengths of the call's other
+ * requests, which say where a long request's sums are cut.
  *   q           in   16-bit [requests][heads][head_dim], strided rows
  *   page_table  in   int32 [requests][table_width], rows table_stride entries apart: the pages of a request's tokens in their
  *                    order.  Entries past a request's last token are not read; one that is not a page of the cache has its
@@ -368,7 +370,8 @@ size_t any4_attn_decode_workspace_bytes(int64_t requests, int heads, int kv_head
  *   q_starts, k_starts   in   int32 [requests + 1], ascending; values are taken as at least 0 and at most q_tokens / k_tokens
  *   f16      0: bf16, 1: fp16
  *   out      out  16-bit [q_tokens][heads][head_dim], dense; rows that no request has are left as they are
- * Requests and tokens may be 0 in number (then nothing is done).  Needs no workspace.
+ * (q_tokens / 128 + requests) * heads at most 2^31 - 1.  Requests and tokens may be 0 in number (then nothing is done).  Needs no
+ * workspace.
  */
 int any4_attn_prompt(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride,
                      const uint16_t* k, int64_t k_token_stride, int64_t k_head_stride,

@@ -92,6 +92,11 @@ struct PromptArgs {
     float softmax_scale;
     uint16_t* out;
 };
+constexpr int kPromptRows = 128;          // queries of a block
+// a tile of each request may be short; blocks that no request has end at once
+inline int64_t prompt_blocks(int64_t q_tokens, int64_t requests, int heads) {
+    return (q_tokens / kPromptRows + (requests < q_tokens ? requests : q_tokens)) * heads;
+}
 hipError_t launch_attn_prompt(const PromptArgs& a, hipStream_t stream);
 
 }  // namespace any4

@@ -98,6 +98,7 @@ int any4_attn_prompt(const uint16_t* q, int64_t q_token_stride, int64_t q_head_s
         !strides_ok(q_token_stride, q_head_stride) || !strides_ok(k_token_stride, k_head_stride) || !strides_ok(v_token_stride, v_head_stride) ||
         k_token_stride >= kMaxStride || v_token_stride >= kMaxStride)
         return ANY4_ERR_SHAPE;
+    if (prompt_blocks(q_tokens, requests, heads) > 0x7FFFFFFF) return ANY4_ERR_SHAPE;
     if (requests == 0 || q_tokens == 0) return ANY4_OK;
     // (without a single key k and v are not read)
     if (!q || !q_starts || !k_starts || !out || (k_tokens > 0 && (!k || !v))) return ANY4_ERR_NULL;

@@ -355,10 +355,8 @@ template <int D, bool F16> hipError_t launch(const Args& a, int64_t blocks, hipS
 hipError_t launch_attn_prompt(const PromptArgs& p, hipStream_t stream) {
     Args a{p.q, p.k, p.v, p.q_starts, p.k_starts, (int)p.q_tokens, (int)p.k_tokens, p.requests, p.heads, p.kv_heads, p.heads / p.kv_heads,
            p.causal, p.softmax_scale * kLog2e, p.out};
-    // a tile of each request may be short; those that no request has end at once
-    const int64_t places = p.q_tokens / (32 * kWaves) + (p.requests < p.q_tokens ? p.requests : p.q_tokens);
-    const int64_t blocks = places * p.heads;
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+    static_assert(kPromptRows == 32 * kWaves, "prompt_blocks() counts tiles of a block's queries");
+    const int64_t blocks = prompt_blocks(p.q_tokens, p.requests, p.heads);
     if (p.head_dim == 128) return p.f16 ? launch<128, true>(a, blocks, stream) : launch<128, false>(a, blocks, stream);
     return p.f16 ? launch<64, true>(a, blocks, stream) : launch<64, false>(a, blocks, stream);
 }

@@ -89,6 +89,7 @@ def test_prompt_refuses(lib):
         assert prompt(**bad) == SHAPE, bad
     for bad in (dict(q=A + 8), dict(v=A + 2), dict(qs=A + 2), dict(out=A + 4), dict(qt=1), dict(kh=4), dict(vt=20)):
         assert prompt(**bad) == ALIGN, bad
+    assert prompt(nq=0x7FFFFFFF - 2047, nk=0x7FFFFFFF - 2047, heads=256) == SHAPE          # more blocks than a launch has
     assert prompt(n=0) == prompt(nq=0) == prompt(nq=0, q=None) == 0
 
 
