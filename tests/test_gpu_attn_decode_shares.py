@@ -33,6 +33,15 @@ def test_full_wavefront_of_requests():
     p.check(p.run())
 
 
+@pytest.mark.parametrize("bits", (16, 4))
+def test_one_request_on_all_blocks(bits):
+    """as many pieces to join as there are blocks: more than a wavefront has lanes"""
+    p = Problem([70001], bits, BF16, 128, 4, 1, 64, seed=33)
+    out = p.run()
+    p.check(out)
+    assert torch.equal(out.view(torch.int16), p.run().view(torch.int16))
+
+
 def test_more_requests_than_a_launch_takes():
     """2500 requests over the pages of one: their own lengths, the same results as in calls of a few"""
     p = Problem([200], 16, BF16, 64, 2, 1, 16, seed=32)
