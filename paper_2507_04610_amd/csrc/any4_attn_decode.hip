@@ -15,8 +15,9 @@
 // bf16 take two bits set in place; c itself for 8 bits in bf16), scale and offset are applied to sums:
 //     q . k_j = ks_j (q . c'_j - kBias sum(q)) + ko_j sum(q)
 //     o = sum_j (p_j vs_j) (c_j - kCentre) + sum_j p_j (vo_j + kCentre vs_j)
-// where the first sum has p_j vs_j rounded to 16 bits and is taken as sum(.. c'_j) - (kBias + kCentre) sum(..) with the same
-// rounded weights, so that their rounding meets values around 0 as it does without codes.
+// where the first sum has p_j vs_j rounded to 16 bits, and every step takes (kBias + kCentre) sum(..) of the same rounded weights off it in
+// front of adding sum(.. c'_j), both on the matrix cores: the rounding of the weights meets values around 0 as it does without codes, and the running sums
+// hold no bias, whose roundings would grow with the tokens (taken off once at the end: 1e-2 of the result at 131072 tokens a block, fp16, 4 bits).
 //
 // Rounding: scores, maxima, sums and accumulators are fp32; p (times vs) is rounded to 16 bits for the matrix cores, once.
 //
@@ -123,6 +124,8 @@ template <int BITS, bool F16> struct Codes {
     static constexpr int kBias = BITS == 16 ? 0 : F16 ? 1024 : BITS == 4 ? 128 : 0;
     static constexpr int kCentre = BITS == 16 ? 0 : 1 << (BITS - 1);
     static constexpr uint32_t kMagic = F16 ? 0x64006400u : 0x43004300u;
+    // -(kBias + kCentre) twice in 16 bits, exact: fp16 -1032 and -1152, bf16 -136 and -128
+    static constexpr uint32_t kOff = F16 ? (BITS == 4 ? 0xE408E408u : 0xE480E480u) : BITS == 4 ? 0xC308C308u : 0xC300C300u;
 };
 
 // A operand of S^T from a token's words: matrix instruction i
@@ -281,7 +284,7 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
             const int t0 = from * UNIT, t1 = min(len, to * UNIT);
 
             float m_ref = -__builtin_inff(), l = 0.0f, vo_sum = 0.0f;
-            f32x4 o[VM], ones_sum = {0.0f, 0.0f, 0.0f, 0.0f};
+            f32x4 o[VM];
 #pragma unroll
             for (int m = 0; m < VM; ++m) o[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             // fp16 weights p * vs: held as p * (vs * 2^-exponent), with the largest vs so far between 1 and 2, or small scales would leave fp16's range
@@ -437,7 +440,6 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
                     l *= alpha;
                     vo_sum *= alpha;
                     const float f = alpha * factor;
-                    ones_sum *= f;
 #pragma unroll
                     for (int m = 0; m < VM; ++m) o[m] *= f;
                 }
@@ -456,8 +458,8 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
 #pragma unroll
                 for (int j = 0; j < 4; ++j) p[j] = f32x2_to_h16x2<F16>(x[2 * j], x[2 * j + 1]);
                 if constexpr (QUANT) {
-                    constexpr uint32_t kOnes = F16 ? 0x3C003C00u : 0x3F803F80u;
-                    ones_sum = mma16<F16>(u32x4{kOnes, kOnes, kOnes, kOnes}, p, ones_sum);
+#pragma unroll
+                    for (int m = 0; m < VM; ++m) o[m] = mma16<F16>(u32x4{C::kOff, C::kOff, C::kOff, C::kOff}, p, o[m]);
                 }
 #pragma unroll
                 for (int m = 0; m < VM; ++m) {
@@ -489,7 +491,7 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
                         f32x4 v = {o[m][r], o[m + 1][r], o[m + 2][r], o[m + 3][r]};
                         if constexpr (QUANT) {
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) v[j] = fmaf(back, v[j] - (float)(C::kBias + C::kCentre) * ones_sum[0], vo_sum);
+                            for (int j = 0; j < 4; ++j) v[j] = fmaf(back, v[j], vo_sum);
                         }
                         *reinterpret_cast<f32x4*>(to_lds + VM * (4 * g_e + r) + m) = v;
                     }

@@ -1,5 +1,5 @@
 """any4_attn_decode against 64 bits under the narrow bound of attention_close.py (which a missing piece or even weights exceed, see
-test_attention_close.py)."""
+test_attention_close.py), and with more tokens in one block's sums than a bias on the codes would survive."""
 import pytest
 import torch
 
@@ -40,6 +40,22 @@ def test_close_to_64_bits(name):
     p = close.Requests(*args)
     out = any4.any4_attn_decode(p.q.cuda(), *cache_of(p, page), bits=p.bits)
     check(p, out)
+
+
+@pytest.mark.parametrize("bits,dtype", [(4, close.F16), (8, close.F16), (4, close.BF16), (8, close.BF16), (16, close.F16)])
+@pytest.mark.parametrize("dim", (128, 64))
+def test_long_requests_that_are_not_cut(bits, dtype, dim):
+    """1024 requests of 131072 tokens each (the same ones): more requests than blocks, each block adds up whole requests"""
+    n, requests, page = 131072, 1024, 128
+    p = close.Requests([n], bits, dtype, dim, 4, 1, seed=8)
+    ck, cv, table, length, scales = cache_of(p, page)
+    p.q = torch.randn(requests, 4, dim, generator=torch.Generator().manual_seed(9)).to(dtype)
+    out = any4.any4_attn_decode(p.q.cuda(), ck, cv, table.expand(requests, -1).contiguous(), length.expand(requests).contiguous(), scales, bits=bits)
+    out = out.double().cpu().numpy()
+    held = close.Held(p.k[0][:, 0], p.v[0][:, 0], bits, dtype)
+    for i in (0, 1, 500, 1023):
+        worst, mean = close.fits(out[i], p.q[i].double().numpy(), held, p.scale)
+        assert worst <= 1 and mean <= 1, (i, worst, mean)
 
 
 def test_requests_of_the_second_launch():
