@@ -21,9 +21,11 @@
  *     device-independent refusal happens before the first launch: on any error other than
  *     ANY4_ERR_HIP nothing was launched and no output byte was written.  ANY4_ERR_HIP means the
  *     HIP runtime refused a launch; calls that are served by several launches (any4_gemm with
- *     16 < M <= 128 or with groups of 64 and 8 < M <= 16, and the matrix-core path, whose
- *     group-sum pre-pass precedes the GEMM kernel) may then have written part of y or of the
- *     workspace: their contents are unspecified.  No exception or abort crosses the ABI.
+ *     16 < M <= 128 or with groups of 64 and 8 < M <= 16, the matrix-core path, whose
+ *     group-sum pre-pass precedes the GEMM kernel, any4_attn_decode with more than 2048 requests (fewer where
+ *     requests * table_width * page_size / 128 units of its KV heads pass 2^31), any4_attn_prompt with
+ *     (q_tokens / 128 + requests) * heads of 2^24 and more, any4_kv_write and any4_kv_read with 2^28 tokens and more) may then
+ *     have written part of their outputs or of the workspace: their contents are unspecified.  No exception or abort crosses the ABI.
  *   - K must be a positive multiple of 128 (the group size); M, N >= 1; bits is 4, 3
  *     or 2.  Every pointer must be 16-byte aligned.
  *   - The library keeps no state between calls that affects results: the only process-wide data

@@ -30,6 +30,7 @@
 // Rounding: scores, maxima, sums and accumulators are fp32; the weights are rounded to 16 bits for the matrix cores, once.
 #include "any4_attn.h"
 #include "any4_internal.h"
+#include "any4_launches.h"
 #include "any4_lds_copy.h"
 
 namespace any4 {
@@ -50,6 +51,7 @@ struct Args {
     const int32_t* q_starts;
     const int32_t* k_starts;
     int q_tokens, k_tokens, requests, heads, kv_heads, shared, causal;
+    unsigned first_block;              // of this launch
     float scale_log2;
     uint16_t* out;
 };
@@ -75,7 +77,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_prompt_kernel(Args a) {
     const int n = lane & 31, g = lane >> 5;
 
     // KV heads fastest: blocks that read the same keys tend to share an XCD and its L2
-    const unsigned rest = blockIdx.x / (unsigned)a.kv_heads, kv_head = blockIdx.x - rest * (unsigned)a.kv_heads;
+    const unsigned block = a.first_block + blockIdx.x, rest = block / (unsigned)a.kv_heads, kv_head = block - rest * (unsigned)a.kv_heads;
     const unsigned place = rest / (unsigned)a.shared;
     const int head = (int)(kv_head * (unsigned)a.shared + (rest - place * (unsigned)a.shared));
 
@@ -342,19 +344,22 @@ __global__ __launch_bounds__(kThreads, 2) void attn_prompt_kernel(Args a) {
     }
 }
 
-template <int D, bool F16> hipError_t launch(const Args& a, int64_t blocks, hipStream_t stream) {
+template <int D, bool F16> hipError_t launch(Args a, int64_t blocks, hipStream_t stream) {
     constexpr auto kernel = attn_prompt_kernel<D, F16>;
     constexpr int bytes = 4 * Tile<D>::kBytes;
     if (hipError_t e = ensure_lds<kernel>(bytes); e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), bytes, stream, a);
-    return hipGetLastError();
+    return launch_blocks(blocks, kThreads, hipSuccess, [&](int64_t first, int64_t count) {
+        a.first_block = (unsigned)first;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(kThreads), bytes, stream, a);
+        return hipGetLastError();
+    });
 }
 
 }  // namespace
 
 hipError_t launch_attn_prompt(const PromptArgs& p, hipStream_t stream) {
     Args a{p.q, p.k, p.v, p.q_starts, p.k_starts, (int)p.q_tokens, (int)p.k_tokens, p.requests, p.heads, p.kv_heads, p.heads / p.kv_heads,
-           p.causal, p.softmax_scale * kLog2e, p.out};
+           p.causal, 0u, p.softmax_scale * kLog2e, p.out};
     static_assert(kPromptRows == 32 * kWaves, "prompt_blocks() counts tiles of a block's queries");
     const int64_t blocks = prompt_blocks(p.q_tokens, p.requests, p.heads);
     if (p.head_dim == 128) return p.f16 ? launch<128, true>(a, blocks, stream) : launch<128, false>(a, blocks, stream);

@@ -8,6 +8,7 @@
 // Measured, 8 KV heads of 128, us of the kernel: 16384 tokens into 16 bits 30 (134 MB, 4.5 TB/s), 65536 out of it 102 (537 MB, 5.3 TB/s),
 // 32768 out of 4 bits 26 (171 MB, 6.5 TB/s), 2047 into 8 bits 6.6 and out of it 4.0, 16 into 16 bits 2.
 #include "any4_attn.h"
+#include "any4_launches.h"
 
 namespace any4 {
 
@@ -153,27 +154,36 @@ template <class F> void with_variant(const any4_kv_cache& c, F f) {
     else types(std::integral_constant<int, 4>{});
 }
 
-dim3 grid_of(const any4_kv_cache& c, int64_t tokens) {
+// launch(first token, tokens, grid) until one is refused: one launch below 2^28 tokens (heads of 64: 2^29)
+template <class F> hipError_t launch_tokens(const any4_kv_cache& c, int64_t tokens, F launch) {
     const int per_block = kThreads / (c.head_dim / 8);
-    return dim3((unsigned)((tokens + per_block - 1) / per_block), (unsigned)c.kv_heads);
+    return launch_blocks((tokens + per_block - 1) / per_block, kThreads, hipSuccess, [&](int64_t first, int64_t count) {
+        const int64_t at = first * per_block, left = tokens - at;
+        launch(at, left < count * per_block ? left : count * per_block, dim3((unsigned)count, (unsigned)c.kv_heads));
+        return hipGetLastError();
+    });
 }
 
 }  // namespace
 
 hipError_t launch_kv_write(const Rows& k, const Rows& v, int64_t tokens, const int64_t* slots, const any4_kv_cache& c, hipStream_t stream) {
-    with_variant(c, [&](auto bits, auto dim, auto f16) {
-        hipLaunchKernelGGL((kv_write_kernel<decltype(bits)::value, decltype(dim)::value, decltype(f16)::value>), grid_of(c, tokens), dim3(kThreads), 0,
-                           stream, k, v, tokens, slots, kv_pages(c));
+    return launch_tokens(c, tokens, [&](int64_t at, int64_t n, dim3 grid) {
+        const Rows kr{k.p + at * k.token, k.token, k.head}, vr{v.p + at * v.token, v.token, v.head};
+        with_variant(c, [&](auto bits, auto dim, auto f16) {
+            hipLaunchKernelGGL((kv_write_kernel<decltype(bits)::value, decltype(dim)::value, decltype(f16)::value>), grid, dim3(kThreads), 0,
+                               stream, kr, vr, n, slots + at, kv_pages(c));
+        });
     });
-    return hipGetLastError();
 }
 
 hipError_t launch_kv_read(const any4_kv_cache& c, const int64_t* slots, int64_t tokens, uint16_t* k, uint16_t* v, hipStream_t stream) {
-    with_variant(c, [&](auto bits, auto dim, auto f16) {
-        hipLaunchKernelGGL((kv_read_kernel<decltype(bits)::value, decltype(dim)::value, decltype(f16)::value>), grid_of(c, tokens), dim3(kThreads), 0,
-                           stream, kv_pages(c), slots, tokens, k, v);
+    return launch_tokens(c, tokens, [&](int64_t at, int64_t n, dim3 grid) {
+        const int64_t to = at * c.kv_heads * c.head_dim;
+        with_variant(c, [&](auto bits, auto dim, auto f16) {
+            hipLaunchKernelGGL((kv_read_kernel<decltype(bits)::value, decltype(dim)::value, decltype(f16)::value>), grid, dim3(kThreads), 0,
+                               stream, kv_pages(c), slots + at, n, k + to, v + to);
+        });
     });
-    return hipGetLastError();
 }
 
 }  // namespace any4
