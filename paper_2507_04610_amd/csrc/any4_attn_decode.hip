@@ -49,6 +49,9 @@ constexpr int kMaxRequests = 2048;                              // of a launch: 
 constexpr int kWholeUnits = 4;                                  // with fewer units a group (on average) no group is cut for the sake of more blocks
 constexpr int kJoin = 16;                                       // pieces whose loads are out at a time
 
+// where the join's parts begin in LDS, behind a factor for each head and piece: they are pairs of floats
+__host__ __device__ constexpr int parts_at(int heads, int pieces) { return (heads * pieces + 1) & ~1; }
+
 struct DecodeArgs {
     Rows q;
     KvPages c;
@@ -203,7 +206,7 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
     constexpr int VB = VM * BITS / 8, VW = VB < 4 ? 1 : VB / 4; // bytes and words of a lane: v of one token
     constexpr bool QUANT = BITS != 16;
     constexpr int PAD = D + 4;                                  // a head's sums in LDS: 16 heads' pieces in different banks
-    extern __shared__ float lds[];
+    extern __shared__ __attribute__((aligned(16))) float lds[];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
@@ -213,7 +216,7 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
     // Where the requests' units begin: with up to 64 requests in the lanes, with more in LDS behind the wavefronts' sums or the
     // pieces' factors and parts.
     const bool many = a.requests > 64;
-    int* begins = reinterpret_cast<int*>(lds + max(WAVES * most * (PAD + 2), most * (int)gridDim.x + 2 * THREADS));
+    int* begins = reinterpret_cast<int*>(lds + max(WAVES * most * (PAD + 2), parts_at(most, (int)gridDim.x) + 2 * THREADS));
     int lane_begin, lane_end, units_of_all;
     if (!many) {
         const int r = min(lane, a.requests - 1);
@@ -548,7 +551,7 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
             const int items = here * D / 2, slices = max(THREADS / items, 1), span = (pieces + slices - 1) / slices;
             const int slice = thread / items, w_first = slice * span, w_end = slice < slices ? min(pieces, w_first + span) : 0;
             float* factor = lds;                                        // [head][pieces]
-            float* parts = lds + here * pieces;                         // [slice][items][2], behind the factors
+            float* parts = lds + parts_at(here, pieces);                // [slice][items][2], behind the factors
             f32x2 x[kJoin];
             auto load_parts = [&](int w0, int i) {
 #pragma unroll
@@ -610,7 +613,7 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
 template <int BITS, int D, bool F16, int WAVES> hipError_t launch(const DecodeArgs& a, const DecodePlan& pl, hipStream_t stream) {
     constexpr auto kernel = attn_decode_kernel<BITS, D, F16, WAVES, BITS == 16 || WAVES == 8>;
     auto bytes = [](int heads, int requests, int blocks) {
-        const int own = WAVES * heads * (D + 6), join = heads * blocks + 128 * WAVES;
+        const int own = WAVES * heads * (D + 6), join = parts_at(heads, blocks) + 128 * WAVES;
         return (int)sizeof(float) * ((own > join ? own : join) + requests + 1 + WAVES);
     };
     if (hipError_t e = ensure_lds<kernel>(bytes(16, kMaxRequests, 1024)); e != hipSuccess) return e;

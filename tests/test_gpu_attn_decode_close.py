@@ -71,3 +71,12 @@ def test_requests_of_the_second_launch():
         held = close.Held(p.k[0][:m, 0], p.v[0][:m, 0], 16, close.BF16)
         worst, mean = close.fits(out[i], q[i].double().numpy(), held, p.scale)
         assert worst <= 1 and mean <= 1, (i, m, worst, mean)
+
+
+@pytest.mark.parametrize("bits", (16, 8, 4))
+@pytest.mark.parametrize("heads", (1, 3, 5))
+@pytest.mark.parametrize("lengths", [[700], [1300], [2900, 1000], [260, 9000]])
+def test_odd_numbers_of_heads_and_pieces(bits, heads, lengths):
+    """the join's sums lie behind as many factors as there are heads and pieces"""
+    p = close.Requests(lengths, bits, close.BF16, 128, heads, 1, seed=12)
+    check(p, any4.any4_attn_decode(p.q.cuda(), *cache_of(p, 64), bits=bits))
