@@ -39,6 +39,7 @@ namespace {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kKeys = 64;
 constexpr float kSlack = 8.0f;
+constexpr float kFar = 1048576.0f;        // 2^20: up to there a maximum's rounding moves the exponents by 2^-4 at most, for all keys of a query alike
 
 #pragma clang diagnostic ignored "-Wint-to-pointer-cast"          // LDS offsets as pointers
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -193,23 +194,42 @@ __global__ __launch_bounds__(kThreads, 2) void attn_prompt_kernel(Args a) {
         const u32x2 both = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false));
         return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * a.scale_log2;
     };
-    auto raise = [&](float top) {
-        if (__builtin_amdgcn_ballot_w64(top > m_ref + kSlack || (m_ref == -__builtin_inff() && top > m_ref))) {
+    // The maximum in use follows the scores x, whose weights' exponents are then scale x - m_sub: a product that is not rounded, less a maximum that
+    // is.  Beyond 2^31 that rounding alone would leave the exponents' range: where some query's maximum lies beyond kFar, the scores are
+    // replaced by their distance from it, both rounded alike.
+    float m_sub = 0.0f;
+    unsigned long long far = 0ull;                              // queries whose maximum lies beyond kFar
+    auto raise = [&](f32x16 (&x)[2]) {
+        const float top = highest(x);
+        if ((__builtin_amdgcn_ballot_w64(top > m_ref + kSlack) | far) != 0ull) {
             const float m_new = fmaxf(m_ref, top);
             const float alpha = m_new > m_ref ? exp2_fast(m_ref - m_new) : 1.0f;
             m_ref = m_new;
+            m_sub = m_ref == -__builtin_inff() ? 0.0f : m_ref;
             l *= alpha;
 #pragma unroll
             for (int m = 0; m < OM; ++m) o[m] *= alpha;
+            far = __builtin_amdgcn_ballot_w64(fabsf(m_sub) > kFar);
+            if (far) {
+                const float back = 1.0f / a.scale_log2;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+#pragma clang fp contract(off)
+                        const float scaled = x[u][r] * a.scale_log2;
+                        x[u][r] = (scaled - m_sub) * back;
+                    }
+                m_sub = 0.0f;
+            }
         }
     };
     auto weigh = [&](const f32x16 (&x)[2], u32x4 (&p)[4]) {
-        const float m_use = m_ref == -__builtin_inff() ? 0.0f : m_ref;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int r = 0; r < 16; r += 2) {
-                const float e = exp2_fast(fmaf(x[u][r], a.scale_log2, -m_use)), f = exp2_fast(fmaf(x[u][r + 1], a.scale_log2, -m_use));
+                const float e = exp2_fast(fmaf(x[u][r], a.scale_log2, -m_sub)), f = exp2_fast(fmaf(x[u][r + 1], a.scale_log2, -m_sub));
                 l += e + f;
                 p[2 * u + (r >> 3)][(r >> 1) & 3] = f32x2_to_h16x2<F16>(e, f);
             }
@@ -237,7 +257,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_prompt_kernel(Args a) {
             for (int m = 0; m < OM; ++m) o[m] = mma32<F16>(v_operand(even * T::kBytes, c, m), p[c], o[m]);
         s[0] = next[0];
         s[1] = next[1];
-        raise(highest(s));
+        raise(s);
     };
     // The same where some query may not see some key of t or t + 1, or t is the last.
     auto last_step = [&](int t, uint32_t even) {
@@ -308,7 +328,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_prompt_kernel(Args a) {
             if (t + 1 < tiles) {
                 scores((even ^ 1u) * T::kBytes, s);
                 mask(t + 1, s);
-                raise(highest(s));
+                raise(s);
             }
         }
     };
@@ -321,7 +341,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_prompt_kernel(Args a) {
         lds_barrier();
         scores(0, s);
         if (whole == 0) mask(0, s);
-        raise(highest(s));
+        raise(s);
     }
     int t = 0;
     for (; t + 2 < whole; t += 2) {
