@@ -2,8 +2,8 @@
 
 Argument marshalling only: every function takes torch tensors that already live in device
 memory, checks dtype / shape / contiguity (every array the kernels index is compared with the
-shape (N, K, bits, group) implies), and passes raw pointers plus the current HIP stream
-to the library.  No arithmetic of the method happens here, and there is no fallback: if the
+shape (N, K, bits, group) implies), and passes raw pointers plus the current HIP stream of
+the tensors' device to the library.  No arithmetic of the method happens here, and there is no fallback: if the
 shared library is missing or a call is made with host tensors, this module raises.
 """
 from __future__ import annotations
@@ -180,8 +180,23 @@ def _scratch(t, device) -> tuple[int, int]:
     return t.data_ptr(), t.numel() * t.element_size()
 
 
-def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+def _launch(entry: str, device, *args) -> None:
+    """the entry point on the tensors' device, on torch's current stream of it"""
+    stream = torch.cuda.current_stream()
+    if stream.device_index != device.index:
+        with torch.cuda.device(device):
+            return _launch(entry, device, *args)
+    rc = getattr(load_library(), entry)(*args, stream.cuda_stream)
+    if rc != 0:
+        _check(rc, entry)
+
+
+def _bytes_on(device, entry: str, *args) -> int:
+    """a workspace's size, which depends on the device"""
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _bytes_on(device, entry, *args)
+    return int(getattr(load_library(), entry)(*args))
 
 
 def row_words(K: int, bits: int) -> int:
@@ -203,14 +218,13 @@ def any4_gemm_workspace_bytes(M: int, N: int, K: int, bits: int = 4) -> int:
 def any4_pack(codes_u8: torch.Tensor, bits: int = 4, out: torch.Tensor | None = None) -> torch.Tensor:
     """uint8 [N,K] codes (one per byte) -> packed words, int32 tensor [N, K*bits/32]
     (torch has no usable uint32; the bit patterns are what matters)."""
-    lib = load_library()
     N, K = codes_u8.shape
     src = _dev(codes_u8, torch.uint8, "codes_u8")
     if out is None:
         out = torch.empty((N, max(K * bits // 32, 0)), dtype=torch.int32, device=codes_u8.device)
     _shape(out, (N, max(K * bits // 32, 0)), "out")
     dst = _dev(out, torch.int32, "out")
-    _check(lib.any4_pack(src, N, K, bits, dst, _stream()), "any4_pack")
+    _launch("any4_pack", codes_u8.device, src, N, K, bits, dst)
     return out
 
 
@@ -220,7 +234,6 @@ def any4_dequant(codes: torch.Tensor, lut: torch.Tensor | None, scale: torch.Ten
     shape [1, 2^bits]: one table for the whole matrix);
     scale / offset are [N, K / group] (any4_dequant_grouped when group is not 128).
     lut / scale / offset are bf16, or all fp16 (any4_dequant_f16: groups of 128, a table)."""
-    lib = load_library()
     N = codes.shape[0]
     pc = _dev(codes, torch.int32, "codes")
     dt = scale.dtype if isinstance(scale, torch.Tensor) and scale.dtype == torch.float16 else torch.bfloat16
@@ -236,21 +249,20 @@ def any4_dequant(codes: torch.Tensor, lut: torch.Tensor | None, scale: torch.Ten
     if single:
         if dt == torch.float16 or group != GROUP:
             raise Any4Error("one table for the whole matrix comes with bf16 and groups of 128")
-        _check(lib.any4_dequant_single_table(pc, pl, ps, po, N, K, bits, pw, _stream()), "any4_dequant_single_table")
+        _launch("any4_dequant_single_table", codes.device, pc, pl, ps, po, N, K, bits, pw)
     elif dt == torch.float16:
         if group != GROUP:
             raise Any4Error("fp16 inputs come with groups of 128")
-        _check(lib.any4_dequant_f16(pc, pl, ps, po, N, K, bits, pw, _stream()), "any4_dequant_f16")
+        _launch("any4_dequant_f16", codes.device, pc, pl, ps, po, N, K, bits, pw)
     elif group == GROUP:
-        _check(lib.any4_dequant(pc, pl, ps, po, N, K, bits, pw, _stream()), "any4_dequant")
+        _launch("any4_dequant", codes.device, pc, pl, ps, po, N, K, bits, pw)
     else:
-        _check(lib.any4_dequant_grouped(pc, pl, ps, po, N, K, bits, group, pw, _stream()), "any4_dequant_grouped")
+        _launch("any4_dequant_grouped", codes.device, pc, pl, ps, po, N, K, bits, group, pw)
     return out
 
 
 def _gemm(entry: str, x, codes, N, lut, scale, offset, bits, out, workspace, group=None):
     """the checked call, one argument after the other: what the native call below says no to comes here to be named"""
-    lib = load_library()
     M, K = x.shape
     dt = x.dtype if isinstance(x, torch.Tensor) and x.dtype == torch.float16 else torch.bfloat16
     if dt == torch.float16:
@@ -274,14 +286,14 @@ def _gemm(entry: str, x, codes, N, lut, scale, offset, bits, out, workspace, gro
         out = torch.empty((M, N), dtype=dt, device=x.device)
     _shape(out, (M, N), "out")
     py = _dev(out, dt, "out")
-    need = int(lib.any4_gemm_workspace_bytes(M, N, K, bits))
+    need = _bytes_on(x.device, "any4_gemm_workspace_bytes", M, N, K, bits)
     if workspace is None and need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
     pw, wbytes = _scratch(workspace, x.device) if workspace is not None else (None, 0)
     if group is None:
-        _check(getattr(lib, entry)(px, pc, pl, ps, po, M, N, K, bits, py, pw, wbytes, _stream()), entry)
+        _launch(entry, x.device, px, pc, pl, ps, po, M, N, K, bits, py, pw, wbytes)
     else:
-        _check(getattr(lib, entry)(px, pc, pl, ps, po, M, N, K, bits, group, py, pw, wbytes, _stream()), entry)
+        _launch(entry, x.device, px, pc, pl, ps, po, M, N, K, bits, group, py, pw, wbytes)
     return out
 
 
@@ -318,7 +330,6 @@ def any4_gemm_noalloc(x: torch.Tensor, codes: torch.Tensor, lut: torch.Tensor | 
                       offset: torch.Tensor, bits: int = 4, out: torch.Tensor | None = None) -> torch.Tensor:
     """any4_gemm without a workspace: the library's own fixed scratch array serves (see include/any4.h;
     calls on one GPU must not overlap in time).  `out` should be passed by callers that must not allocate."""
-    lib = load_library()
     M, K = x.shape
     N = codes.shape[0]
     px = _dev(x, torch.bfloat16, "x")
@@ -331,7 +342,7 @@ def any4_gemm_noalloc(x: torch.Tensor, codes: torch.Tensor, lut: torch.Tensor | 
         out = torch.empty((M, N), dtype=torch.bfloat16, device=x.device)
     _shape(out, (M, N), "out")
     py = _dev(out, torch.bfloat16, "out")
-    _check(lib.any4_gemm_noalloc(px, pc, pl, ps, po, M, N, K, bits, py, _stream()), "any4_gemm_noalloc")
+    _launch("any4_gemm_noalloc", x.device, px, pc, pl, ps, po, M, N, K, bits, py)
     return out
 
 
@@ -350,7 +361,7 @@ def any4_repack(codes: torch.Tensor, bits: int = 4) -> torch.Tensor:
     if nbytes == 0:
         raise Any4Error("any4_repack: bad shape or bits")
     out = torch.empty(nbytes // 4, dtype=torch.int32, device=codes.device)
-    _check(lib.any4_repack(pc, N, K, bits, out.data_ptr(), _stream()), "any4_repack")
+    _launch("any4_repack", codes.device, pc, N, K, bits, out.data_ptr())
     return out
 
 
@@ -374,7 +385,6 @@ def any4_quantize(w: torch.Tensor, act: torch.Tensor | None, u: torch.Tensor, bi
     uniform draws -> dict with codes_u8 uint8 [N,K], lut bf16 [N,2^bits], scale / offset bf16
     [N,K/128] and msteps int32 [N].  Everything stays in device memory.  centre_gap: None calls
     any4_quantize, a number calls any4_quantize_with_gap."""
-    lib = load_library()
     N, K = w.shape
     L = 1 << bits
     pw = _dev(w, torch.float32, "w")
@@ -389,12 +399,11 @@ def any4_quantize(w: torch.Tensor, act: torch.Tensor | None, u: torch.Tensor, bi
     offset = torch.empty((N, max(K // GROUP, 0)), dtype=torch.bfloat16, device=dev)
     msteps = torch.empty((N,), dtype=torch.int32, device=dev)
     if centre_gap is None:
-        _check(lib.any4_quantize(pw, pa, pu, N, K, bits, int(symmetric), iters, codes.data_ptr(), lut.data_ptr(),
-                                 scale.data_ptr(), offset.data_ptr(), msteps.data_ptr(), _stream()), "any4_quantize")
+        _launch("any4_quantize", dev, pw, pa, pu, N, K, bits, int(symmetric), iters, codes.data_ptr(), lut.data_ptr(),
+                scale.data_ptr(), offset.data_ptr(), msteps.data_ptr())
     else:
-        _check(lib.any4_quantize_with_gap(pw, pa, pu, N, K, bits, int(symmetric), iters, float(centre_gap),
-                                          codes.data_ptr(), lut.data_ptr(), scale.data_ptr(), offset.data_ptr(),
-                                          msteps.data_ptr(), _stream()), "any4_quantize_with_gap")
+        _launch("any4_quantize_with_gap", dev, pw, pa, pu, N, K, bits, int(symmetric), iters, float(centre_gap),
+                codes.data_ptr(), lut.data_ptr(), scale.data_ptr(), offset.data_ptr(), msteps.data_ptr())
     return {"codes_u8": codes, "lut": lut, "scale": scale, "offset": offset, "msteps": msteps}
 
 
@@ -459,7 +468,6 @@ def any4_kv_write(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache_k
         if r.__class__ is int:
             _check(r, "any4_kv_write")
         return
-    lib = load_library()
     if not isinstance(k, torch.Tensor):
         raise Any4Error("k must be a tensor in device memory")
     cache, heads, dim = _cache(cache_k, cache_v, scales, bits, k.dtype)
@@ -469,7 +477,7 @@ def any4_kv_write(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache_k
         raise Any4Error("slots must have one dimension")
     pk, pv = _rows(k, k.dtype, "k", shape), _rows(v, k.dtype, "v", shape)
     _same_device(k, v, slots, cache_k)
-    _check(lib.any4_kv_write(*pk, *pv, shape[0], ptr, ctypes.byref(cache), _stream()), "any4_kv_write")
+    _launch("any4_kv_write", cache_k.device, *pk, *pv, shape[0], ptr, ctypes.byref(cache))
 
 
 def any4_kv_read(cache_k: torch.Tensor, cache_v: torch.Tensor, slots: torch.Tensor, scales: torch.Tensor | None = None, bits: int = 16,
@@ -482,7 +490,6 @@ def any4_kv_read(cache_k: torch.Tensor, cache_v: torch.Tensor, slots: torch.Tens
             if r.__class__ is int:
                 _check(r, "any4_kv_read")
             return r
-    lib = load_library()
     cache, heads, dim = _cache(cache_k, cache_v, scales, bits, dtype)
     ptr = _dev(slots, torch.int64, "slots")
     if slots.dim() != 1:
@@ -493,7 +500,7 @@ def any4_kv_read(cache_k: torch.Tensor, cache_v: torch.Tensor, slots: torch.Tens
     _shape(k, (n, heads, dim), "out[0]")
     _shape(v, (n, heads, dim), "out[1]")
     _same_device(cache_k, slots, k, v)
-    _check(lib.any4_kv_read(ctypes.byref(cache), ptr, n, pk, pv, _stream()), "any4_kv_read")
+    _launch("any4_kv_read", cache_k.device, ctypes.byref(cache), ptr, n, pk, pv)
     return k, v
 
 
@@ -512,7 +519,6 @@ def any4_attn_decode(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tens
         if r.__class__ is int:
             _check(r, "any4_attn_decode")
         return r
-    lib = load_library()
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise Any4Error("q must be a tensor of 3 dimensions: requests, heads, head_dim")
     n, heads = q.shape[:2]
@@ -532,12 +538,12 @@ def any4_attn_decode(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tens
     po = _dev(out, q.dtype, "out")
     _same_device(q, cache_k, page_table, lengths, out)
     width = page_table.shape[1]
-    need = int(lib.any4_attn_decode_workspace_bytes(n, heads, kv_heads, dim, width * cache.page_size))
+    need = _bytes_on(q.device, "any4_attn_decode_workspace_bytes", n, heads, kv_heads, dim, width * cache.page_size)
     if workspace is None and need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     pw, wbytes = _scratch(workspace, q.device) if workspace is not None else (None, 0)
-    _check(lib.any4_attn_decode(*pq, ctypes.byref(cache), page_table.data_ptr(), page_table.stride(0), width, pl, n, heads,
-                                dim ** -0.5 if softmax_scale is None else softmax_scale, po, pw, wbytes, _stream()), "any4_attn_decode")
+    _launch("any4_attn_decode", q.device, *pq, ctypes.byref(cache), page_table.data_ptr(), page_table.stride(0), width, pl, n, heads,
+            dim ** -0.5 if softmax_scale is None else softmax_scale, po, pw, wbytes)
     return out
 
 
@@ -551,7 +557,6 @@ def any4_attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts
         if r.__class__ is int:
             _check(r, "any4_attn_prompt")
         return r
-    lib = load_library()
     for t, name in ((q, "q"), (k, "k"), (v, "v")):
         if not isinstance(t, torch.Tensor) or t.dim() != 3:
             raise Any4Error(f"{name} must be a tensor of 3 dimensions: tokens, heads, head_dim")
@@ -576,7 +581,6 @@ def any4_attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts
     _shape(out, (n, heads, dim), "out")
     po = _dev(out, q.dtype, "out")
     _same_device(q, k, v, q_starts, k_starts, out)
-    _check(lib.any4_attn_prompt(*pq, *pk, *pv, n, k.shape[0], ps, pt, q_starts.shape[0] - 1, heads, kv_heads, dim,
-                                int(q.dtype == torch.float16), int(causal), dim ** -0.5 if softmax_scale is None else softmax_scale, po, _stream()),
-           "any4_attn_prompt")
+    _launch("any4_attn_prompt", q.device, *pq, *pk, *pv, n, k.shape[0], ps, pt, q_starts.shape[0] - 1, heads, kv_heads, dim,
+            int(q.dtype == torch.float16), int(causal), dim ** -0.5 if softmax_scale is None else softmax_scale, po)
     return out

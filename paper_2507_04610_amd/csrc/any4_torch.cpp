@@ -6,10 +6,12 @@
 // the same checks on the tensors themselves and calls the C ABI.  It only ever says yes: whatever is not a
 // plain valid call (a wrong type, shape, device, layout, a combination that does not exist) returns None
 // with nothing done, and binding.py goes through its own checks, which name the mistake.  The functions for the cache and for
-// attention are the same for calls whose kernels take 3 - 5 us.
+// attention are the same for calls whose kernels take 3 - 5 us.  All of them run on the tensors' device, on torch's current stream of
+// it, and without the interpreter's lock while they launch (a full queue makes a launch wait).
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <cmath>
 #include "any4.h"
@@ -23,6 +25,17 @@ bool plain(const at::Tensor& t, at::ScalarType ty) {
     return t.is_cuda() && t.scalar_type() == ty && t.is_contiguous() && t.layout() == at::kStrided;
 }
 bool shaped(const at::Tensor& t, int64_t a, int64_t b) { return t.dim() == 2 && t.size(0) == a && t.size(1) == b; }
+
+// torch's current stream of the tensors' device, which is the current one for as long as the guard lives.  (The stream says which device is
+// current: a guard that is not needed took 0.25 us of a call of 5.)
+void* stream_on(const c10::Device& device, c10::OptionalDeviceGuard& guard) {
+    c10::hip::HIPStream s = c10::hip::getCurrentHIPStream();
+    if (s.device_index() != device.index()) {
+        guard.reset_device(device);
+        s = c10::hip::getCurrentHIPStream();
+    }
+    return s.stream();
+}
 
 const uint16_t* u16(const at::Tensor& t) { return static_cast<const uint16_t*>(t.data_ptr()); }
 
@@ -62,6 +75,8 @@ PyObject* gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     // (of any type, but as much memory as it has elements, and on the device)
     if (ws && !(ws->layout() == at::kStrided && ws->device() == x->device() && ws->is_non_overlapping_and_dense())) Py_RETURN_NONE;
 
+    c10::OptionalDeviceGuard guard;
+    void* const stream = stream_on(x->device(), guard);
     at::Tensor y = out ? *out : at::empty({M, N}, x->options().requires_grad(false));
     at::Tensor scratch;
     void* wp = nullptr;
@@ -74,7 +89,6 @@ PyObject* gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
         wp = scratch.data_ptr();
         wbytes = need;
     }
-    void* stream = c10::hip::getCurrentHIPStream().stream();
     const uint16_t *px = u16(*x), *pl = lut ? u16(*lut) : nullptr, *ps = u16(*scale), *po = u16(*offset);
     const uint32_t* pc = static_cast<const uint32_t*>(codes->data_ptr());
     uint16_t* py = static_cast<uint16_t*>(y.data_ptr());
@@ -109,6 +123,12 @@ bool kv_cache(const at::Tensor& k, const at::Tensor& v, const at::Tensor* scales
     c.scales = static_cast<uint16_t*>(scales->data_ptr());
     return true;
 }
+// address and strides of rows [tokens, heads, head_dim]
+struct Rows {
+    const uint16_t* p;
+    int64_t token, head;
+    explicit Rows(const at::Tensor& t) : p(u16(t)), token(t.stride(0)), head(t.stride(1)) {}
+};
 // rows [tokens, heads, head_dim] whose heads' values lie side by side
 bool rows(const at::Tensor& t, at::ScalarType ty, int64_t tokens, int64_t heads, int64_t dim, const at::Tensor& on) {
     return t.is_cuda() && t.scalar_type() == ty && t.layout() == at::kStrided && t.dim() == 3 && t.size(0) == tokens && t.size(1) == heads &&
@@ -152,8 +172,14 @@ PyObject* kv_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!kv_cache(*ck, *cv, scales, bits, k->scalar_type(), c) || !list(*slots, at::kLong, *ck)) Py_RETURN_NONE;
     const int64_t tokens = slots->size(0);
     if (!rows(*k, k->scalar_type(), tokens, c.kv_heads, c.head_dim, *ck) || !rows(*v, k->scalar_type(), tokens, c.kv_heads, c.head_dim, *ck)) Py_RETURN_NONE;
-    const int rc = any4_kv_write(u16(*k), k->stride(0), k->stride(1), u16(*v), v->stride(0), v->stride(1), tokens,
-                                 static_cast<const int64_t*>(slots->data_ptr()), &c, c10::hip::getCurrentHIPStream().stream());
+    c10::OptionalDeviceGuard guard;
+    void* const stream = stream_on(ck->device(), guard);
+    const Rows kr(*k), vr(*v);
+    const int64_t* ps = static_cast<const int64_t*>(slots->data_ptr());
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = any4_kv_write(kr.p, kr.token, kr.head, vr.p, vr.token, vr.head, tokens, ps, &c, stream);
+    Py_END_ALLOW_THREADS
     if (rc == ANY4_OK) Py_RETURN_TRUE;
     if (rc == ANY4_ERR_HIP) return PyLong_FromLong(rc);
     Py_RETURN_NONE;
@@ -173,10 +199,16 @@ PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t tokens = slots->size(0);
     for (const at::Tensor* o : {ok, ov})
         if (o && !(plain(*o, ty) && o->dim() == 3 && o->size(0) == tokens && o->size(1) == c.kv_heads && o->size(2) == c.head_dim && o->device() == ck->device())) Py_RETURN_NONE;
+    c10::OptionalDeviceGuard guard;
+    void* const stream = stream_on(ck->device(), guard);
     at::Tensor k = ok ? *ok : at::empty({tokens, c.kv_heads, c.head_dim}, ck->options().dtype(ty).requires_grad(false));
     at::Tensor v = ov ? *ov : at::empty({tokens, c.kv_heads, c.head_dim}, ck->options().dtype(ty).requires_grad(false));
-    const int rc = any4_kv_read(&c, static_cast<const int64_t*>(slots->data_ptr()), tokens, static_cast<uint16_t*>(k.data_ptr()),
-                                static_cast<uint16_t*>(v.data_ptr()), c10::hip::getCurrentHIPStream().stream());
+    const int64_t* ps = static_cast<const int64_t*>(slots->data_ptr());
+    uint16_t *pk = static_cast<uint16_t*>(k.data_ptr()), *pv = static_cast<uint16_t*>(v.data_ptr());
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = any4_kv_read(&c, ps, tokens, pk, pv, stream);
+    Py_END_ALLOW_THREADS
     if (rc == ANY4_ERR_HIP) return PyLong_FromLong(rc);
     if (rc != ANY4_OK) Py_RETURN_NONE;
     PyObject* both = PyTuple_New(2);
@@ -208,7 +240,9 @@ PyObject* attn_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
         Py_RETURN_NONE;
     if (out && !(plain(*out, ty) && rows(*out, ty, requests, heads, c.head_dim, *ck))) Py_RETURN_NONE;
     if (ws && !(ws->layout() == at::kStrided && ws->device() == ck->device() && ws->is_non_overlapping_and_dense())) Py_RETURN_NONE;
-    const int64_t width = table->size(1);
+    const int64_t width = table->size(1), table_stride = table->stride(0);
+    c10::OptionalDeviceGuard guard;
+    void* const stream = stream_on(ck->device(), guard);
     at::Tensor o = out ? *out : at::empty({requests, heads, c.head_dim}, q->options().requires_grad(false));
     at::Tensor scratch;
     void* wp = nullptr;
@@ -221,9 +255,13 @@ PyObject* attn_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
         wp = scratch.data_ptr();
         wbytes = need;
     }
-    const int rc = any4_attn_decode(u16(*q), q->stride(0), q->stride(1), &c, static_cast<const int32_t*>(table->data_ptr()), table->stride(0), width,
-                                    static_cast<const int32_t*>(lengths->data_ptr()), requests, (int)heads, scale, static_cast<uint16_t*>(o.data_ptr()), wp,
-                                    wbytes, c10::hip::getCurrentHIPStream().stream());
+    const Rows qr(*q);
+    const int32_t *pt = static_cast<const int32_t*>(table->data_ptr()), *pl = static_cast<const int32_t*>(lengths->data_ptr());
+    uint16_t* po = static_cast<uint16_t*>(o.data_ptr());
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = any4_attn_decode(qr.p, qr.token, qr.head, &c, pt, table_stride, width, pl, requests, (int)heads, scale, po, wp, wbytes, stream);
+    Py_END_ALLOW_THREADS
     return answer(rc, a[8], std::move(o));
     END_HANDLE_TH_ERRORS
 }
@@ -244,11 +282,19 @@ PyObject* attn_prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!list(*qs, at::kInt, *q) || qs->size(0) < 1 || (ks && (!list(*ks, at::kInt, *q) || ks->size(0) != qs->size(0)))) Py_RETURN_NONE;
     if ((!ks && nk != nq) || !scale_of(a[6], dim, scale)) Py_RETURN_NONE;
     if (out && !(plain(*out, ty) && rows(*out, ty, nq, heads, dim, *q))) Py_RETURN_NONE;
+    c10::OptionalDeviceGuard guard;
+    void* const stream = stream_on(q->device(), guard);
     at::Tensor o = out ? *out : at::empty({nq, heads, dim}, q->options().requires_grad(false));
-    const int rc = any4_attn_prompt(u16(*q), q->stride(0), q->stride(1), u16(*k), k->stride(0), k->stride(1), u16(*v), v->stride(0), v->stride(1), nq, nk,
-                                    static_cast<const int32_t*>(qs->data_ptr()), static_cast<const int32_t*>((ks ? ks : qs)->data_ptr()), qs->size(0) - 1,
-                                    (int)heads, (int)kv_heads, (int)dim, ty == at::kHalf, a[5] == Py_True, scale, static_cast<uint16_t*>(o.data_ptr()),
-                                    c10::hip::getCurrentHIPStream().stream());
+    const Rows qr(*q), kr(*k), vr(*v);
+    const int32_t *pqs = static_cast<const int32_t*>(qs->data_ptr()), *pks = static_cast<const int32_t*>((ks ? ks : qs)->data_ptr());
+    const int64_t requests = qs->size(0) - 1;
+    const bool causal = a[5] == Py_True;
+    uint16_t* po = static_cast<uint16_t*>(o.data_ptr());
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = any4_attn_prompt(qr.p, qr.token, qr.head, kr.p, kr.token, kr.head, vr.p, vr.token, vr.head, nq, nk, pqs, pks, requests, (int)heads, (int)kv_heads,
+                          (int)dim, ty == at::kHalf, causal, scale, po, stream);
+    Py_END_ALLOW_THREADS
     return answer(rc, a[7], std::move(o));
     END_HANDLE_TH_ERRORS
 }
