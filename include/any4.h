@@ -343,8 +343,9 @@ int any4_kv_read(const any4_kv_cache* cache, const int64_t* slots, int64_t token
  * requests, which say where a long request's sums are cut.
  *   q           in   16-bit [requests][heads][head_dim], strided rows
  *   page_table  in   int32 [requests][table_width], rows table_stride entries apart: the pages of a request's tokens in their
- *                    order.  Entries past a request's last token are not read; one that is not a page of the cache has its
- *                    tokens left out as if masked (a request without any other gets NaN)
+ *                    order.  Entries past a request's last token are not used (nor read, but for the first one of a request
+ *                    without a token); one that is not a page of the cache has its tokens left out as if masked (a request
+ *                    without any other gets zeros)
  *   lengths     in   int32 [requests]; taken as at least 0 and at most table_width * page_size
  *   out         out  16-bit [requests][heads][head_dim], dense
  *   workspace   at least any4_attn_decode_workspace_bytes() bytes; may be NULL when that is 0.  What is said of any4_gemm's
