@@ -484,8 +484,12 @@ def any4_kv_read(cache_k: torch.Tensor, cache_v: torch.Tensor, slots: torch.Tens
                  dtype: torch.dtype = torch.bfloat16, out: tuple[torch.Tensor, torch.Tensor] | None = None):
     """(k, v) [tokens, kv_heads, head_dim] of slots (int64 [tokens]) of the cache, in dtype (the cache's own with 16 bits); zeros
     for a slot outside the cache."""
+    try:
+        out_k, out_v = (None, None) if out is None else out
+    except (TypeError, ValueError):
+        raise Any4Error("out must be a pair of tensors, k and v") from None
     if dtype is torch.bfloat16 or dtype is torch.float16:
-        r = _calls().kv_read(cache_k, cache_v, slots, scales, bits, dtype is torch.float16, *(out if out is not None else (None, None)))
+        r = _calls().kv_read(cache_k, cache_v, slots, scales, bits, dtype is torch.float16, out_k, out_v)
         if r is not None:
             if r.__class__ is int:
                 _check(r, "any4_kv_read")
@@ -495,7 +499,7 @@ def any4_kv_read(cache_k: torch.Tensor, cache_v: torch.Tensor, slots: torch.Tens
     if slots.dim() != 1:
         raise Any4Error("slots must have one dimension")
     n = slots.shape[0]
-    k, v = out if out is not None else (torch.empty((n, heads, dim), dtype=dtype, device=cache_k.device) for _ in range(2))
+    k, v = (out_k, out_v) if out is not None else (torch.empty((n, heads, dim), dtype=dtype, device=cache_k.device) for _ in range(2))
     pk, pv = _dev(k, dtype, "out[0]"), _dev(v, dtype, "out[1]")
     _shape(k, (n, heads, dim), "out[0]")
     _shape(v, (n, heads, dim), "out[1]")
