@@ -2,8 +2,9 @@
 //
 // For a KV head and the up to 16 query heads that share it, tokens j:
 //     s_j = scale q . k_j,   o = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),   m = max_j s_j
-// in one pass over the cache with a running maximum.  The cache is read once, and that bounds the operator: a few
-// floating-point operations for each byte at up to 16 heads.  Everything else is arranged so that no byte takes a detour.
+// in one pass over the cache with a running maximum.  The cache is read once (with more than 16 query heads on a KV head once for every 16
+// of them), and that bounds the operator: a few floating-point operations for each byte at up to 16 heads.  Everything else is arranged so
+// that no byte takes a detour.
 //
 // A wavefront takes 32 tokens a step, for all heads of the KV head.  S^T = K Q^T with v_mfma_f32_16x16x32, k's rows as the A
 // operand straight from memory (lane: token l % 16, 8 values along the head); the scores of a head then lie in the 4 lanes l % 16 =
@@ -30,10 +31,10 @@
 // the join costs as much as four steps.
 //
 // Measured, 8 KV heads of 128, us (bytes of the cache / time):
-//     16 bits, 64 requests of 2048 .. 8192 tokens, 32 query heads          208   (6.5 TB/s; a copy reaches 4.9 read and written)
-//     8 bits, 32 requests of 1 .. 4096 tokens, 32 query heads               33   (4.2 TB/s)
-//     4 bits, one request of 131071 tokens, 64 query heads                  37   (3.8 TB/s: 24 us of streaming at 6 TB/s, 3 until the first
-//                                                                                bytes are asked for, 6 for the join of 32 pieces)
+//     16 bits, 64 requests of 2048 .. 8192 tokens, 32 query heads          208   (6.5 TB/s; the fastest read-only stream measured here reaches 6.8)
+//     8 bits, 32 requests of 1 .. 4096 tokens, 32 query heads               34   (4.1 TB/s)
+//     4 bits, one request of 131071 tokens, 64 query heads                  39   (3.7 TB/s; 3 us until the first bytes are asked for, 6 for the
+//                                                                                join of 32 pieces; vector units busy half of the time)
 //     16 bits, one request of 333 tokens, 32 query heads                     8.3 (loads that wait for each other: length, page, k and v)
 #include "any4_attn.h"
 #include "any4_internal.h"
@@ -192,10 +193,11 @@ template <class F> __device__ __forceinline__ float head_reduce(float v, F f) {
 // over all lanes of a wavefront
 template <class F> __device__ __forceinline__ float wave_reduce(float v, F f) { return head_reduce(lanes_reduce<16>(v, f), f); }
 
-// WAVES 8: one block for a compute unit, for few groups, whose pieces are then few to join (131071 tokens, 8 groups: 37 us, with 4 wavefronts
-// 45); WAVES 4: two or three, whose beginnings and ends overlap (32 requests, 256 groups: 33 us against 42).  AHEAD: a step's loads are out
-// before the step in front of it is worked on; otherwise the other wavefronts of the SIMD cover for it (8 bits and 4 wavefronts: 33.8 us against
-// 35.3 with, as more blocks fit).
+// WAVES 8: one block for a compute unit, for few groups, whose pieces are then few to join (one request of 32768 tokens, 8 groups, 16 / 8 / 4 bits:
+// 28 / 22 / 17 us, with 4 wavefronts 34 / 25 / 29); WAVES 4: two or three, whose beginnings and ends overlap (32 requests of 1 .. 4096, 256
+// groups: 52 / 33 / 27 against 52 / 41 / 35).  AHEAD: a step's loads are out before the step in front of it is worked on, which takes a
+// second step's registers; otherwise the other wavefronts of the SIMD cover for it (4 wavefronts, 32 and 16 requests of 1 .. 4096: 8 bits 33.4
+// and 21.3 us, with it 35.2 and 23.8; 4 bits 27.5 and 19.5, with it 35.5 and 24.8).
 template <int BITS, int D, bool F16, int WAVES, bool AHEAD>
 __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(DecodeArgs a) {
     using C = Codes<BITS, F16>;
@@ -618,8 +620,11 @@ template <int BITS, int D, bool F16, int WAVES> hipError_t launch(const DecodeAr
     };
     if (hipError_t e = ensure_lds<kernel>(bytes(16, kMaxRequests, 1024)); e != hipSuccess) return e;
     const int most = pl.shared < 16 ? pl.shared : 16;
-    // blocks of 4 wavefronts: two for a compute unit, with 4 bits three (64 requests of up to 2048 tokens: 33 -> 27 us; 8 bits and 32 of up to
-    // 4096: 34 -> 36)
+    // Blocks of 4 wavefronts: two for a compute unit, with 4 bits three.  What decides is how many units a block gets beside its beginning and
+    // end; by bits, us with two / three blocks for 16 requests of 1 .. 4096 tokens, 32 of them, 64 of 100 .. 2048, 64 of 2048 .. 8192:
+    //     16 bits 30.7 / 35.5   52.2 / 61.9   57.2 / 66.9   208 / 210
+    //      8      21.3 / 22.6   33.4 / 35.7   39.7 / 37.6   121 / 125
+    //      4      18.8 / 19.5   29.4 / 27.3   33.5 / 27.6    87 /  81
     const int fill = pl.cus * (WAVES == 8 ? 1 : BITS == 4 ? 3 : 2), blocks = pl.blocks < fill ? pl.blocks : fill;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * WAVES), bytes(most, a.requests, blocks), stream, a);
     return hipGetLastError();

@@ -12,15 +12,17 @@
 // neighbouring rows' pieces lie in different banks.
 //
 // The matrix cores make a tile's scores while the vector units turn the ones of the tile in front of it into weights: one after the other
-// 2 x 8192 causal tokens took 1140 us, like this 1055.  So k is copied two tiles ahead, v one.
+// 2 x 8192 causal tokens took 1140 us, like this 1050.  So k is copied two tiles ahead, v one.
 //
 // Measured, 32 query heads on 8 KV heads of 128, bf16, causal:
-//     2 prompts of 8192 tokens            1055 us, 1.04 PFLOP/s (a product of 8192^3 in the library: 1.28)
-//     12 of 65 .. 2048 behind contexts of up to 1024    371 us, 0.81 PFLOP/s
-//     one of 77                            9 us (starts, q, k and v wait for each other; 32 blocks)
-// The matrix cores were busy half of the time at 1.9 GHz (counters of the version without that, 1.13 ms).  For each score of a lane they take 32
-// cycles, the exponential 9 and its scaling, maximum, sum and rounding about 14 on the vector units; the rest is waiting for LDS and for the
-// block's other wavefronts.
+//     2 prompts of 8192 tokens            1050 us, 1.05 PFLOP/s (a product of 8192^3 in the library: 1.28 .. 1.36)
+//         in fp16                         1150 us (two conversions and a pack for each pair of weights, one instruction in bf16)
+//         heads of 64                      630 us (half the matrix work, as many exponentials)
+//     12 of 65 .. 2048 behind contexts of up to 1024    370 us, 0.81 PFLOP/s
+//     one of 77                            9.3 us (starts, q, k and v wait for each other; 32 blocks)
+// Of the long ones' time the matrix cores are busy 54 %, the vector units 53 % (packed: 41 and 49), beside each other, at 1.8 .. 1.9 GHz; a wavefront
+// waits 30 % of its time.  For each score of a lane the matrix cores take 32 cycles, the exponential 9 and its scaling, maximum, sum and rounding
+// about 14 on the vector units; the rest is waiting for LDS and for the block's other wavefronts.
 // Prescribing the order of LDS reads, matrix and vector instructions changed nothing (1046 .. 1061 us), 64 queries a wavefront do not fit
 // the registers (85 spilled, 1600 us).
 //

@@ -3,10 +3,12 @@
 // A block does 16 tokens (32 with heads of 64) of one KV head: a head's vector is 8 values each for 16 (8) lanes, 16 bytes a load.
 // The inputs of a block are pieces of 256 bytes a token, its cache side is one contiguous piece where the tokens are
 // neighbours: with 4 bits 1 KB rather than the 64-byte pieces that a block of one token and all heads would write.  Both
-// kernels read every byte once and write every byte once; memory bounds them.
+// kernels read every byte once and write every byte once; memory bounds all but the writes of codes.
 //
 // Measured, 8 KV heads of 128, us of the kernel: 16384 tokens into 16 bits 30 (134 MB, 4.5 TB/s), 65536 out of it 102 (537 MB, 5.3 TB/s),
-// 32768 out of 4 bits 26 (171 MB, 6.5 TB/s), 2047 into 8 bits 6.6 and out of it 4.0, 16 into 16 bits 2.
+// 16384 into 8 bits 29 (102 MB, 3.5 TB/s) and out of it 16 (6.2), into 4 bits 28 (85 MB, 3.1 TB/s) and out of it 14 (6.0), 2047 into 8 bits 6.7 and
+// out of it 4.0, 16 into 16 bits 2.  Writes of codes are bound by their arithmetic rather than by memory: the vector units are busy 72 % of the time
+// (16384 tokens, 8 bits; 480 instructions a wavefront, about 170 of them for the 16 quotients of a lane).
 #include "any4_attn.h"
 #include "any4_launches.h"
 
