@@ -24,7 +24,8 @@
  *     16 < M <= 128 or with groups of 64 and 8 < M <= 16, the matrix-core path, whose
  *     group-sum pre-pass precedes the GEMM kernel, any4_attn_decode with more than 2048 requests (fewer where
  *     requests * table_width * page_size / 128 units of its KV heads pass 2^31), any4_attn_prompt with
- *     (q_tokens / 128 + requests) * heads of 2^24 and more, any4_kv_write and any4_kv_read with 2^28 tokens and more) may then
+ *     (q_tokens / 128 + requests) * heads of 2^24 and more, any4_kv_write and any4_kv_read with 2^28 tokens and more,
+ *     any4_rope and any4_rope_kv_write with 2^26 tokens and more) may then
  *     have written part of their outputs or of the workspace: their contents are unspecified.  No exception or abort crosses the ABI.
  *   - K must be a positive multiple of 128 (the group size); M, N >= 1; bits is 4, 3
  *     or 2.  Every pointer must be 16-byte aligned.
@@ -335,6 +336,58 @@ int any4_kv_read(const any4_kv_cache* cache, const int64_t* slots, int64_t token
                  void* stream);
 
 /*
+ * What a token's heads go through between the fused QKV projection and the cache: a norm of each head (optional) and the rotation by
+ * the token's position(s).
+ *     y = x / sqrt(mean(x^2) + eps) * w             over the head_dim values of a head; without w: y = x
+ *     (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t),    t = position[axis_of[i]] * freqs[i],    pair i of rotary_dim / 2
+ * Pair i is (i, i + rotary_dim / 2), or with interleaved = 1 (2 i, 2 i + 1); values from rotary_dim on are not turned.  Angles are fp64,
+ * the rest is fp32, and the result is rounded once, to the type of the rows.  What is frequency scaling (longer contexts) is the caller's, in freqs.
+ *   positions   in   int64 [axes][tokens], axis_stride entries from an axis to the next; any value
+ *   freqs       in   double [rotary_dim / 2]: the angle of position 1, in radians
+ *   axis_of     in   uint8 [rotary_dim / 2]: which of a token's positions turns pair i (images and video: time, height, width); values from axes on
+ *                    are taken as axes - 1.  NULL: the first for all
+ *   q_norm, k_norm   in   16-bit [head_dim] (the rows' type), shared by the heads; NULL: no norm
+ *   axes        1 .. 4
+ *   rotary_dim  a multiple of 8, 8 .. head_dim
+ *   eps         >= 0, finite
+ */
+typedef struct any4_rotation {
+    const int64_t* positions;
+    int64_t axis_stride;
+    const double* freqs;
+    const uint8_t* axis_of;
+    const uint16_t* q_norm;
+    const uint16_t* k_norm;
+    int axes, rotary_dim, interleaved;
+    float eps;
+} any4_rotation;
+
+/*
+ * any4_rope - norms and rotation of q and k of `tokens` tokens.
+ *   q, k          in   16-bit [tokens][heads][head_dim] and [tokens][kv_heads][head_dim], strided rows
+ *   q_out, k_out  out  the same, strided rows; may be q and k themselves (with their strides), must not overlap them otherwise
+ *   heads       1 .. 65535 (no multiple of kv_heads is asked for here), kv_heads 1 .. 4095, head_dim 64 or 128
+ *   f16         0: bf16, 1: fp16
+ * tokens = 0 is a call that does nothing.
+ */
+int any4_rope(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const uint16_t* k, int64_t k_token_stride, int64_t k_head_stride,
+              int64_t tokens, int heads, int kv_heads, int head_dim, int f16, const any4_rotation* turn,
+              uint16_t* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+              uint16_t* k_out, int64_t k_out_token_stride, int64_t k_out_head_stride, void* stream);
+
+/*
+ * any4_rope_kv_write - any4_rope, with k and v written into their slots of the cache: the same cache and q_out, bit for bit, as any4_rope followed by
+ * any4_kv_write of its k (keys are rounded to 16 bits before they become codes), in one pass.
+ *   slots       in   as for any4_kv_write; q (and k_out) of a token that is left out are turned all the same
+ *   k_out            NULL: the keys go into the cache alone
+ * KV heads, head_dim and type are the cache's.
+ */
+int any4_rope_kv_write(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const uint16_t* k, int64_t k_token_stride, int64_t k_head_stride,
+                       const uint16_t* v, int64_t v_token_stride, int64_t v_head_stride, int64_t tokens, int heads, const any4_rotation* turn,
+                       const int64_t* slots, const any4_kv_cache* cache, uint16_t* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+                       uint16_t* k_out, int64_t k_out_token_stride, int64_t k_out_head_stride, void* stream);
+
+/*
  * any4_attn_decode - one new token of each request attends to the first lengths[r] tokens of its pages:
  *     s_j = softmax_scale * q . k_j,   out = sum_j softmax(s)_j v_j
  * Query head h reads KV head h / (heads / kv_heads).  A request without a token gets zeros.  Scores, softmax and sums
@@ -358,6 +411,18 @@ int any4_attn_decode(const uint16_t* q, int64_t q_request_stride, int64_t q_head
                      const int32_t* page_table, int64_t table_stride, int64_t table_width, const int32_t* lengths,
                      int64_t requests, int heads, float softmax_scale, uint16_t* out,
                      void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * any4_attn_decode_window - any4_attn_decode where the new token of a request of n tokens sees its last `window` tokens (itself among them) and its first
+ * `sinks` only.  The others, and their entries of the page table, may be anything (a page that a request needs no more can go to another).
+ *   window      1 and more; from n on the result is any4_attn_decode's
+ *   sinks       0 and more
+ * Everything else as there, the workspace's size too.
+ */
+int any4_attn_decode_window(const uint16_t* q, int64_t q_request_stride, int64_t q_head_stride, const any4_kv_cache* cache,
+                            const int32_t* page_table, int64_t table_stride, int64_t table_width, const int32_t* lengths,
+                            int64_t requests, int heads, int64_t window, int64_t sinks, float softmax_scale, uint16_t* out,
+                            void* workspace, size_t workspace_bytes, void* stream);
 
 /* Bytes of workspace any4_attn_decode needs (0 for invalid arguments); max_tokens = table_width * page_size. */
 size_t any4_attn_decode_workspace_bytes(int64_t requests, int heads, int kv_heads, int head_dim, int64_t max_tokens);

@@ -20,7 +20,7 @@ GROUP = 128
 
 EXPORTS = ("any4_pack", "any4_dequant", "any4_gemm", "any4_gemm_workspace_bytes", "any4_repack", "any4_repack_bytes", "any4_gemm_repacked", "any4_dequant_grouped", "any4_gemm_grouped", "any4_dequant_f16", "any4_gemm_f16",
            "any4_quantize", "any4_quantize_with_gap", "any4_quantize_max_k", "any4_gemm_noalloc", "any4_dequant_single_table", "any4_gemm_single_table",
-           "any4_kv_write", "any4_kv_read", "any4_attn_decode", "any4_attn_decode_workspace_bytes", "any4_attn_prompt", "any4_strerror", "any4_version")
+           "any4_kv_write", "any4_kv_read", "any4_rope", "any4_rope_kv_write", "any4_attn_decode", "any4_attn_decode_window", "any4_attn_decode_workspace_bytes", "any4_attn_prompt", "any4_strerror", "any4_version")
 
 
 class Any4Error(RuntimeError):
@@ -32,6 +32,13 @@ class _KvCache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("pages", ctypes.c_int64),
                 ("page_size", ctypes.c_int), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("bits", ctypes.c_int),
                 ("f16", ctypes.c_int)]
+
+
+class _Rotation(ctypes.Structure):
+    """any4_rotation of include/any4.h"""
+    _fields_ = [("positions", ctypes.c_void_p), ("axis_stride", ctypes.c_int64), ("freqs", ctypes.c_void_p), ("axis_of", ctypes.c_void_p),
+                ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p), ("axes", ctypes.c_int), ("rotary_dim", ctypes.c_int),
+                ("interleaved", ctypes.c_int), ("eps", ctypes.c_float)]
 
 
 _lib = None
@@ -90,6 +97,13 @@ def load_library() -> ctypes.CDLL:
     lib.any4_kv_read.argtypes = [cache, vp, i64, vp, vp, vp]
     lib.any4_attn_decode.restype = ci
     lib.any4_attn_decode.argtypes = [vp, i64, i64, cache, vp, i64, i64, vp, i64, ci, f32, vp, vp, ctypes.c_size_t, vp]
+    lib.any4_attn_decode_window.restype = ci
+    lib.any4_attn_decode_window.argtypes = [vp, i64, i64, cache, vp, i64, i64, vp, i64, ci, i64, i64, f32, vp, vp, ctypes.c_size_t, vp]
+    turn = ctypes.POINTER(_Rotation)
+    lib.any4_rope.restype = ci
+    lib.any4_rope.argtypes = [vp, i64, i64, vp, i64, i64, i64, ci, ci, ci, ci, turn, vp, i64, i64, vp, i64, i64, vp]
+    lib.any4_rope_kv_write.restype = ci
+    lib.any4_rope_kv_write.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, i64, ci, turn, vp, cache, vp, i64, i64, vp, i64, i64, vp]
     lib.any4_attn_decode_workspace_bytes.restype = ctypes.c_size_t
     lib.any4_attn_decode_workspace_bytes.argtypes = [i64, ci, ci, ci, i64]
     lib.any4_attn_prompt.restype = ci
@@ -120,7 +134,7 @@ def _no_native_gemm(*args):
 
 class _NoNativeCalls:
     """the same for the cache and attention"""
-    kv_write = kv_read = attn_decode = attn_prompt = staticmethod(_no_native_gemm)
+    kv_write = kv_read = rope = rope_kv_write = attn_decode = attn_decode_window = attn_prompt = staticmethod(_no_native_gemm)
 
 
 def _calls():
@@ -508,17 +522,131 @@ def any4_kv_read(cache_k: torch.Tensor, cache_v: torch.Tensor, slots: torch.Tens
     return k, v
 
 
+def _rows_out(t, dtype, name: str, shape) -> tuple[int, int, int]:
+    """the same of rows that are written to: no value may lie where another does"""
+    r = _rows(t, dtype, name, shape)
+    (s1, n1), (s2, n2) = sorted(((r[1], shape[0]), (r[2], shape[1])), key=lambda x: -x[0])
+    if (n2 > 1 and s2 < shape[2]) or (n1 > 1 and s1 < ((n2 - 1) * s2 if n2 > 1 else 0) + shape[2]):
+        raise Any4Error(f"{name}: rows to be written must not overlap")
+    return r
+
+
+def _rotation(positions, freqs, q_norm, k_norm, eps, interleaved, axis_of, tokens: int, dim: int, dtype, like) -> _Rotation:
+    if not isinstance(positions, torch.Tensor) or not positions.is_cuda or positions.dtype != torch.int64:
+        raise Any4Error("positions must be an int64 tensor in device memory")
+    if positions.dim() not in (1, 2) or positions.shape[-1] != tokens or (tokens > 1 and positions.stride(-1) != 1):
+        raise Any4Error(f"positions must have shape ({tokens},) or (axes, {tokens}) with an axis's entries side by side, got {tuple(positions.shape)}")
+    axes = positions.shape[0] if positions.dim() == 2 else 1
+    if not 1 <= axes <= 4:
+        raise Any4Error(f"a token has 1 to 4 positions, got {axes}")
+    pf = _dev(freqs, torch.float64, "freqs")
+    if freqs.dim() != 1 or freqs.shape[0] < 4 or freqs.shape[0] % 4 or freqs.shape[0] > dim // 2:
+        raise Any4Error(f"freqs must have a multiple of 4 entries, up to {dim // 2}, got shape {tuple(freqs.shape)}")
+    given = {}
+    for t, name, ty, shape in ((q_norm, "q_norm", dtype, (dim,)), (k_norm, "k_norm", dtype, (dim,)), (axis_of, "axis_of", torch.uint8, freqs.shape)):
+        given[name] = None
+        if t is not None:
+            given[name] = _dev(t, ty, name)
+            _shape(t, shape, name)
+    _same_device(like, positions, freqs, q_norm, k_norm, axis_of)
+    return _Rotation(positions.data_ptr(), positions.stride(0) if positions.dim() == 2 else 0, pf, given["axis_of"], given["q_norm"], given["k_norm"],
+                     axes, 2 * freqs.shape[0], int(interleaved), eps)
+
+
+def any4_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, q_norm: torch.Tensor | None = None,
+              k_norm: torch.Tensor | None = None, eps: float = 1e-6, interleaved: bool = False, axis_of: torch.Tensor | None = None,
+              out: tuple[torch.Tensor, torch.Tensor] | None = None):
+    """(q, k), each head normalised (q_norm, k_norm: [head_dim] of their type; None: not) and turned by its token's position.  q [tokens, heads,
+    head_dim], k [tokens, kv_heads, head_dim] (slices of a fused projection's rows serve as they are); positions int64 [tokens] or, with
+    several axes, [axes, tokens]; freqs float64 [rotary_dim / 2], radians a position; axis_of uint8 [rotary_dim / 2]: the axis that turns a pair (None:
+    the first).  Pairs are (i, i + rotary_dim / 2), interleaved (2 i, 2 i + 1); values from rotary_dim on are not turned.  out: a pair of such rows,
+    which may be q and k themselves."""
+    try:
+        out_q, out_k = (None, None) if out is None else out
+    except (TypeError, ValueError):
+        raise Any4Error("out must be a pair of tensors, q and k") from None
+    r = _calls().rope(q, k, positions, freqs, q_norm, k_norm, eps, interleaved, axis_of, out_q, out_k)
+    if r is not None:
+        if r.__class__ is int:
+            _check(r, "any4_rope")
+        return r
+    for t, name in ((q, "q"), (k, "k")):
+        if not isinstance(t, torch.Tensor) or t.dim() != 3:
+            raise Any4Error(f"{name} must be a tensor of 3 dimensions: tokens, heads, head_dim")
+    if q.dtype not in (torch.bfloat16, torch.float16):
+        raise Any4Error(f"q must be bf16 or fp16, got {q.dtype}")
+    n, heads, dim = q.shape
+    kv_heads = k.shape[1]
+    pq, pk = _rows(q, q.dtype, "q", q.shape), _rows(k, q.dtype, "k", (n, kv_heads, dim))
+    turn = _rotation(positions, freqs, q_norm, k_norm, eps, interleaved, axis_of, n, dim, q.dtype, q)
+    yq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out_q is None else out_q
+    yk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if out_k is None else out_k
+    po, pp = _rows_out(yq, q.dtype, "out[0]", q.shape), _rows_out(yk, q.dtype, "out[1]", k.shape)
+    _same_device(q, k, yq, yk)
+    _launch("any4_rope", q.device, *pq, *pk, n, heads, kv_heads, dim, int(q.dtype == torch.float16), ctypes.byref(turn), *po, *pp)
+    return yq, yk
+
+
+def any4_rope_kv_write(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, slots: torch.Tensor,
+                       cache_k: torch.Tensor, cache_v: torch.Tensor, scales: torch.Tensor | None = None, bits: int = 16,
+                       q_norm: torch.Tensor | None = None, k_norm: torch.Tensor | None = None, eps: float = 1e-6, interleaved: bool = False,
+                       axis_of: torch.Tensor | None = None, out: torch.Tensor | None = None, k_out: torch.Tensor | None = None) -> torch.Tensor:
+    """q as any4_rope turns it; k, turned likewise, and v go into slots of the cache as any4_kv_write puts them there, in the same pass.  k_out: rows for
+    the turned keys as well (a prompt's own attention takes them).  out and k_out may be q and k themselves."""
+    r = _calls().rope_kv_write(q, k, v, positions, freqs, slots, cache_k, cache_v, scales, bits, q_norm, k_norm, eps, interleaved, axis_of, out, k_out)
+    if r is not None:
+        if r.__class__ is int:
+            _check(r, "any4_rope_kv_write")
+        return r
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise Any4Error("q must be a tensor of 3 dimensions: tokens, heads, head_dim")
+    n, heads = q.shape[:2]
+    cache, kv_heads, dim = _cache(cache_k, cache_v, scales, bits, q.dtype)
+    pq = _rows(q, q.dtype, "q", (n, heads, dim))
+    pk, pv = _rows(k, q.dtype, "k", (n, kv_heads, dim)), _rows(v, q.dtype, "v", (n, kv_heads, dim))
+    ps = _dev(slots, torch.int64, "slots")
+    _shape(slots, (n,), "slots")
+    turn = _rotation(positions, freqs, q_norm, k_norm, eps, interleaved, axis_of, n, dim, q.dtype, q)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    po = _rows_out(out, q.dtype, "out", q.shape)
+    pp = (None, 0, 0) if k_out is None else _rows_out(k_out, q.dtype, "k_out", k.shape)
+    _same_device(q, k, v, slots, cache_k, out, k_out)
+    _launch("any4_rope_kv_write", q.device, *pq, *pk, *pv, n, heads, ctypes.byref(turn), ps, ctypes.byref(cache), *po, *pp)
+    return out
+
+
+def _part(window, sinks) -> tuple[int, int]:
+    """window and sinks of a call with a window"""
+    for x, name, least in ((window, "window", 1), (sinks, "sinks", 0)):
+        if not isinstance(x, int) or isinstance(x, bool) or not least <= x < 1 << 63:
+            raise Any4Error(f"{name} must be a whole number from {least} on, got {x!r}")
+    return window, sinks
+
+
+def _no_sinks(sinks) -> None:
+    if sinks != 0:
+        raise Any4Error("sinks are the first tokens beside a window; without one all tokens are seen")
+
+
 def any4_attn_decode_workspace_bytes(requests: int, heads: int, kv_heads: int, head_dim: int, max_tokens: int) -> int:
     return int(load_library().any4_attn_decode_workspace_bytes(requests, heads, kv_heads, head_dim, max_tokens))
 
 
 def any4_attn_decode(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
                      scales: torch.Tensor | None = None, bits: int = 16, softmax_scale: float | None = None,
-                     out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+                     out: torch.Tensor | None = None, workspace: torch.Tensor | None = None, window: int | None = None,
+                     sinks: int = 0) -> torch.Tensor:
     """[requests, heads, head_dim]: the newest token of each request (q, of that shape; slices of a fused projection's rows serve as
     they are) attends to the first lengths[r] (int32 [requests]) tokens of its pages (page_table, int32 [requests, table_width]) in
-    the cache.  Query head h reads KV head h // (heads // kv_heads); softmax_scale is head_dim ** -0.5 unless given."""
-    r = _calls().attn_decode(q, cache_k, cache_v, page_table, lengths, scales, bits, softmax_scale, out, workspace)
+    the cache.  Query head h reads KV head h // (heads // kv_heads); softmax_scale is head_dim ** -0.5 unless given.
+    window: only the last `window` tokens of a request are seen, its newest among them, and the first `sinks`."""
+    if window is None:
+        _no_sinks(sinks)
+        r = _calls().attn_decode(q, cache_k, cache_v, page_table, lengths, scales, bits, softmax_scale, out, workspace)
+    else:
+        window, sinks = _part(window, sinks)
+        r = _calls().attn_decode_window(q, cache_k, cache_v, page_table, lengths, scales, bits, softmax_scale, out, workspace, window, sinks)
     if r is not None:
         if r.__class__ is int:
             _check(r, "any4_attn_decode")
@@ -546,7 +674,8 @@ def any4_attn_decode(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tens
     if workspace is None and need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     pw, wbytes = _scratch(workspace, q.device) if workspace is not None else (None, 0)
-    _launch("any4_attn_decode", q.device, *pq, ctypes.byref(cache), page_table.data_ptr(), page_table.stride(0), width, pl, n, heads,
+    name, part = ("any4_attn_decode", ()) if window is None else ("any4_attn_decode_window", (window, sinks))
+    _launch(name, q.device, *pq, ctypes.byref(cache), page_table.data_ptr(), page_table.stride(0), width, pl, n, heads, *part,
             dim ** -0.5 if softmax_scale is None else softmax_scale, po, pw, wbytes)
     return out
 

@@ -11,6 +11,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libany4.so")
 TORCH_SRC = os.path.join(CSRC, "any4_torch.cpp")
+TORCH_ROWS_SRC = os.path.join(CSRC, "any4_torch_rows.cpp")
 TORCH_EXT = os.path.join(PKG, "_any4_torch.so")
 BENCH_SRC = os.path.join(PKG, "bench_support", "stream_read.hip")
 BENCH_LIB = os.path.join(PKG, "bench_support", "libany4_bench.so")
@@ -32,7 +33,7 @@ def torch_extension_command():
     includes = [os.path.join(ROOT, "include"), *cpp_extension.include_paths(), os.path.join(rocm, "include"),
                 sysconfig.get_paths()["include"]]
     return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", "-w",
-            *[f"-I{d}" for d in includes], TORCH_SRC, "-o", TORCH_EXT,
+            *[f"-I{d}" for d in includes], TORCH_SRC, TORCH_ROWS_SRC, "-o", TORCH_EXT,
             *[f"-L{d}" for d in cpp_extension.library_paths()], "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10",
             "-lc10_hip", f"-L{PKG}", "-lany4", "-Wl,-rpath,$ORIGIN"]
 

@@ -69,6 +69,18 @@ constexpr float kLog2e = 1.44269504088896340736f;
 hipError_t launch_kv_write(const Rows& k, const Rows& v, int64_t tokens, const int64_t* slots, const any4_kv_cache& c, hipStream_t stream);
 hipError_t launch_kv_read(const any4_kv_cache& c, const int64_t* slots, int64_t tokens, uint16_t* k, uint16_t* v, hipStream_t stream);
 
+// Rows of q, k and v (without a cache no v) and where the turned ones go.
+struct RopeArgs {
+    Rows q, k, v;
+    uint16_t *q_out, *k_out;
+    int64_t qo_token, qo_head, ko_token, ko_head;
+    int64_t tokens;
+    const int64_t* slots;
+    int heads, kv_heads, head_dim;
+    bool f16;
+};
+hipError_t launch_rope(const RopeArgs& r, const any4_rotation& turn, const any4_kv_cache* c, int cus, hipStream_t stream);
+
 // How a decode call is shared out.
 struct DecodePlan {
     int shared, head_tiles;   // query heads of a KV head, and in how many parts of at most 16
@@ -78,8 +90,8 @@ struct DecodePlan {
 };
 DecodePlan plan_attn_decode(int64_t requests, int heads, int kv_heads, int head_dim, int64_t max_tokens, int cus);
 hipError_t launch_attn_decode(const Rows& q, const any4_kv_cache& c, const int32_t* table, int64_t table_stride, int64_t table_width,
-                              const int32_t* lengths, int64_t requests, int heads, float softmax_scale, uint16_t* out, const DecodePlan& pl,
-                              void* workspace, hipStream_t stream);
+                              const int32_t* lengths, int64_t requests, int heads, int window, int sinks, float softmax_scale, uint16_t* out,
+                              const DecodePlan& pl, void* workspace, hipStream_t stream);          // window 0: all tokens are seen
 
 // Packed prompts: rows of q, k and v, where each request's rows start.
 struct PromptArgs {

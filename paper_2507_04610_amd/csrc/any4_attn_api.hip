@@ -34,7 +34,38 @@ int cache_check(const any4_kv_cache* c) {
     return ANY4_OK;
 }
 
+int rotation_check(const any4_rotation* r, int head_dim) {
+    if (!r || !r->positions || !r->freqs) return ANY4_ERR_NULL;
+    if (r->axes < 1 || r->axes > 4 || r->axis_stride < 0 || r->rotary_dim < 8 || r->rotary_dim % 8 || r->rotary_dim > head_dim || !(r->eps >= 0.0f) ||
+        !(r->eps < __builtin_inff()))
+        return ANY4_ERR_SHAPE;
+    if (!aligned(r->positions, 8) || !aligned(r->freqs, 8) || !aligned16(r->q_norm) || !aligned16(r->k_norm)) return ANY4_ERR_ALIGN;
+    return ANY4_OK;
+}
+
 int launched(hipError_t e) { return e == hipSuccess ? ANY4_OK : ANY4_ERR_HIP; }
+
+// more tokens than a request may have are as good as all
+int at_most(int64_t tokens) { return (int)(tokens < kMaxTokens ? tokens : kMaxTokens); }
+
+int decode(const uint16_t* q, int64_t q_request_stride, int64_t q_head_stride, const any4_kv_cache* cache, const int32_t* page_table,
+           int64_t table_stride, int64_t table_width, const int32_t* lengths, int64_t requests, int heads, int window, int sinks, float softmax_scale,
+           uint16_t* out, void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = cache_check(cache)) return rc;
+    if (requests < 0 || requests > kMaxRequests || !heads_ok(heads, cache->kv_heads) || !scale_ok(softmax_scale) ||
+        !strides_ok(q_request_stride, q_head_stride) || table_width < 1 || table_width > kMaxTokens / cache->page_size || table_stride < 0 ||
+        !tokens_ok(table_width * cache->page_size, heads, cache->kv_heads))
+        return ANY4_ERR_SHAPE;
+    if (requests == 0) return ANY4_OK;
+    if (!q || !page_table || !lengths || !out) return ANY4_ERR_NULL;
+    if (!aligned16(q) || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned16(out) || !aligned16(workspace) ||
+        !strides_aligned(q_request_stride, q_head_stride))
+        return ANY4_ERR_ALIGN;
+    const DecodePlan pl = plan_attn_decode(requests, heads, cache->kv_heads, cache->head_dim, table_width * cache->page_size, device_compute_units());
+    if (pl.workspace > 0 && (!workspace || workspace_bytes < pl.workspace)) return ANY4_ERR_WORKSPACE;
+    return launched(launch_attn_decode({q, q_request_stride, q_head_stride}, *cache, page_table, table_stride, table_width, lengths, requests, heads,
+                                       window, sinks, softmax_scale, out, pl, workspace, static_cast<hipStream_t>(stream)));
+}
 
 }  // namespace
 
@@ -63,6 +94,47 @@ int any4_kv_read(const any4_kv_cache* cache, const int64_t* slots, int64_t token
     return launched(launch_kv_read(*cache, slots, tokens, k, v, static_cast<hipStream_t>(stream)));
 }
 
+int any4_rope(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const uint16_t* k, int64_t k_token_stride, int64_t k_head_stride,
+              int64_t tokens, int heads, int kv_heads, int head_dim, int f16, const any4_rotation* turn, uint16_t* q_out, int64_t q_out_token_stride,
+              int64_t q_out_head_stride, uint16_t* k_out, int64_t k_out_token_stride, int64_t k_out_head_stride, void* stream) {
+    if (tokens < 0 || tokens > kMaxTokens || heads < 1 || heads > kMaxHeads || kv_heads < 1 || kv_heads > kMaxKvHeads || (head_dim != 64 && head_dim != 128) ||
+        !strides_ok(q_token_stride, q_head_stride) || !strides_ok(k_token_stride, k_head_stride) || !strides_ok(q_out_token_stride, q_out_head_stride) ||
+        !strides_ok(k_out_token_stride, k_out_head_stride))
+        return ANY4_ERR_SHAPE;
+    if (tokens == 0) return ANY4_OK;
+    if (int rc = rotation_check(turn, head_dim)) return rc;
+    if (!q || !k || !q_out || !k_out) return ANY4_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !strides_aligned(q_token_stride, q_head_stride) ||
+        !strides_aligned(k_token_stride, k_head_stride) || !strides_aligned(q_out_token_stride, q_out_head_stride) ||
+        !strides_aligned(k_out_token_stride, k_out_head_stride))
+        return ANY4_ERR_ALIGN;
+    const RopeArgs r{{q, q_token_stride, q_head_stride}, {k, k_token_stride, k_head_stride}, {nullptr, 0, 0}, q_out, k_out, q_out_token_stride, q_out_head_stride,
+                     k_out_token_stride, k_out_head_stride, tokens, nullptr, heads, kv_heads, head_dim, f16 != 0};
+    return launched(launch_rope(r, *turn, nullptr, device_compute_units(), static_cast<hipStream_t>(stream)));
+}
+
+int any4_rope_kv_write(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const uint16_t* k, int64_t k_token_stride, int64_t k_head_stride,
+                       const uint16_t* v, int64_t v_token_stride, int64_t v_head_stride, int64_t tokens, int heads, const any4_rotation* turn,
+                       const int64_t* slots, const any4_kv_cache* cache, uint16_t* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+                       uint16_t* k_out, int64_t k_out_token_stride, int64_t k_out_head_stride, void* stream) {
+    if (int rc = cache_check(cache)) return rc;
+    if (tokens < 0 || tokens > kMaxTokens || heads < 1 || heads > kMaxHeads || !strides_ok(q_token_stride, q_head_stride) ||
+        !strides_ok(k_token_stride, k_head_stride) || !strides_ok(v_token_stride, v_head_stride) || !strides_ok(q_out_token_stride, q_out_head_stride) ||
+        (k_out && !strides_ok(k_out_token_stride, k_out_head_stride)))
+        return ANY4_ERR_SHAPE;
+    if (tokens == 0) return ANY4_OK;
+    if (int rc = rotation_check(turn, cache->head_dim)) return rc;
+    if (!q || !k || !v || !slots || !q_out) return ANY4_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(k_out) || !aligned(slots, 8) ||
+        !strides_aligned(q_token_stride, q_head_stride) || !strides_aligned(k_token_stride, k_head_stride) || !strides_aligned(v_token_stride, v_head_stride) ||
+        !strides_aligned(q_out_token_stride, q_out_head_stride) || (k_out && !strides_aligned(k_out_token_stride, k_out_head_stride)))
+        return ANY4_ERR_ALIGN;
+    const RopeArgs r{{q, q_token_stride, q_head_stride}, {k, k_token_stride, k_head_stride}, {v, v_token_stride, v_head_stride}, q_out, k_out,
+                     q_out_token_stride, q_out_head_stride, k_out_token_stride, k_out_head_stride, tokens, slots, heads, cache->kv_heads, cache->head_dim,
+                     cache->f16 != 0};
+    return launched(launch_rope(r, *turn, cache, device_compute_units(), static_cast<hipStream_t>(stream)));
+}
+
 size_t any4_attn_decode_workspace_bytes(int64_t requests, int heads, int kv_heads, int head_dim, int64_t max_tokens) {
     if (requests < 1 || requests > kMaxRequests || !heads_ok(heads, kv_heads) || (head_dim != 64 && head_dim != 128) ||
         !tokens_ok(max_tokens, heads, kv_heads))
@@ -73,20 +145,17 @@ size_t any4_attn_decode_workspace_bytes(int64_t requests, int heads, int kv_head
 int any4_attn_decode(const uint16_t* q, int64_t q_request_stride, int64_t q_head_stride, const any4_kv_cache* cache,
                      const int32_t* page_table, int64_t table_stride, int64_t table_width, const int32_t* lengths, int64_t requests,
                      int heads, float softmax_scale, uint16_t* out, void* workspace, size_t workspace_bytes, void* stream) {
-    if (int rc = cache_check(cache)) return rc;
-    if (requests < 0 || requests > kMaxRequests || !heads_ok(heads, cache->kv_heads) || !scale_ok(softmax_scale) ||
-        !strides_ok(q_request_stride, q_head_stride) || table_width < 1 || table_width > kMaxTokens / cache->page_size || table_stride < 0 ||
-        !tokens_ok(table_width * cache->page_size, heads, cache->kv_heads))
-        return ANY4_ERR_SHAPE;
-    if (requests == 0) return ANY4_OK;
-    if (!q || !page_table || !lengths || !out) return ANY4_ERR_NULL;
-    if (!aligned16(q) || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned16(out) || !aligned16(workspace) ||
-        !strides_aligned(q_request_stride, q_head_stride))
-        return ANY4_ERR_ALIGN;
-    const DecodePlan pl = plan_attn_decode(requests, heads, cache->kv_heads, cache->head_dim, table_width * cache->page_size, device_compute_units());
-    if (pl.workspace > 0 && (!workspace || workspace_bytes < pl.workspace)) return ANY4_ERR_WORKSPACE;
-    return launched(launch_attn_decode({q, q_request_stride, q_head_stride}, *cache, page_table, table_stride, table_width, lengths, requests, heads,
-                                       softmax_scale, out, pl, workspace, static_cast<hipStream_t>(stream)));
+    return decode(q, q_request_stride, q_head_stride, cache, page_table, table_stride, table_width, lengths, requests, heads, 0, 0, softmax_scale, out,
+                  workspace, workspace_bytes, stream);
+}
+
+int any4_attn_decode_window(const uint16_t* q, int64_t q_request_stride, int64_t q_head_stride, const any4_kv_cache* cache,
+                            const int32_t* page_table, int64_t table_stride, int64_t table_width, const int32_t* lengths, int64_t requests,
+                            int heads, int64_t window, int64_t sinks, float softmax_scale, uint16_t* out, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+    if (window < 1 || sinks < 0) return cache_check(cache) ? cache_check(cache) : ANY4_ERR_SHAPE;
+    return decode(q, q_request_stride, q_head_stride, cache, page_table, table_stride, table_width, lengths, requests, heads, at_most(window),
+                  at_most(sinks), softmax_scale, out, workspace, workspace_bytes, stream);
 }
 
 int any4_attn_prompt(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const uint16_t* k, int64_t k_token_stride,

@@ -61,6 +61,7 @@ struct DecodeArgs {
     int table_width;
     const int32_t* lengths;
     int requests, heads, shared, head_tiles;
+    int window, sinks;                 // tokens seen at the end and at the beginning (WINDOW variants)
     float scale_log2;                  // softmax scale * log2(e)
     uint16_t* out;
     float* partial;                    // [block][2][query head][D + 2]: sums, then maximum and sum of weights of every head
@@ -172,6 +173,18 @@ template <int UNIT> __device__ __forceinline__ int units_of(int length, int64_t 
     return (int)max((min((int64_t)length, capacity) + UNIT - 1) / UNIT, (int64_t)1);
 }
 
+// With a window a request's work is the steps that hold a token it sees: those of the first tokens (`sinks`), then from the step in which
+// the window begins.  Tokens are counted without the whole steps in between, `hidden` of them behind the first `front`.
+struct Seen {
+    int start, front, hidden;
+    __device__ __forceinline__ Seen(int len, int window, int sinks) {
+        start = max(len - window, 0);
+        const int base = start & ~(kStep - 1);
+        front = min((sinks + kStep - 1) & ~(kStep - 1), base);
+        hidden = base - front;
+    }
+};
+
 // each lane gets the sum of the lanes up to its own
 __device__ __forceinline__ int lanes_scan(int v) {
     v += __builtin_amdgcn_update_dpp(0, v, 0x111 /*row_shr:1*/, 0xF, 0xF, true);
@@ -198,7 +211,7 @@ template <class F> __device__ __forceinline__ float wave_reduce(float v, F f) { 
 // groups: 52 / 33 / 27 against 52 / 41 / 35).  AHEAD: a step's loads are out before the step in front of it is worked on, which takes a
 // second step's registers; otherwise the other wavefronts of the SIMD cover for it (4 wavefronts, 32 and 16 requests of 1 .. 4096: 8 bits 33.4
 // and 21.3 us, with it 35.2 and 23.8; 4 bits 27.5 and 19.5, with it 35.5 and 24.8).
-template <int BITS, int D, bool F16, int WAVES, bool AHEAD>
+template <int BITS, int D, bool F16, int WAVES, bool AHEAD, bool WINDOW>
 __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(DecodeArgs a) {
     using C = Codes<BITS, F16>;
     constexpr int THREADS = 64 * WAVES, UNIT = kStep * WAVES;
@@ -215,6 +228,15 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
     const int most = min(16, a.shared), room = most * (D + 2);  // query heads of a full head tile; floats of a piece's result
     const int64_t capacity = (int64_t)a.table_width << a.c.page_shift;
 
+    auto request_units = [&](int length) -> int {
+        if constexpr (WINDOW) {
+            const int len = (int)min((int64_t)max(length, 0), capacity);
+            return units_of<UNIT>(len - Seen(len, a.window, a.sinks).hidden, capacity);
+        } else {
+            return units_of<UNIT>(length, capacity);
+        }
+    };
+
     // Where the requests' units begin: with up to 64 requests in the lanes, with more in LDS behind the wavefronts' sums or the
     // pieces' factors and parts.
     const bool many = a.requests > 64;
@@ -222,7 +244,7 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
     int lane_begin, lane_end, units_of_all;
     if (!many) {
         const int r = min(lane, a.requests - 1);
-        const int units = lane < a.requests ? units_of<UNIT>(a.lengths[r], capacity) : 0;
+        const int units = lane < a.requests ? request_units(a.lengths[r]) : 0;
         lane_end = lanes_scan(units);
         lane_begin = lane_end - units;
         units_of_all = __builtin_amdgcn_readlane(lane_end, 63);
@@ -231,7 +253,7 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
         int before = 0;
         for (int r0 = 0; r0 < a.requests; r0 += THREADS) {
             const int r = r0 + (int)threadIdx.x;
-            const int sum = lanes_scan(r < a.requests ? units_of<UNIT>(a.lengths[r], capacity) : 0);
+            const int sum = lanes_scan(r < a.requests ? request_units(a.lengths[r]) : 0);
             if (lane == 63) sums[wave] = sum;
             __syncthreads();
             int here = before;
@@ -275,6 +297,9 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
     }
     for (; at < end; ++request) {
         const int len = (int)min((int64_t)max(scalar(a.lengths)[request], 0), capacity);
+        const Seen seen(len, WINDOW ? a.window : len, WINDOW ? a.sinks : 0);
+        // a counted token's place in the request
+        auto real = [&](int t) -> int { return !WINDOW || t < seen.front ? t : t + seen.hidden; };
         const scalar_i32 table = scalar(a.table + (int64_t)request * a.table_stride);
         const unsigned begin = many ? __builtin_amdgcn_readfirstlane(begins[request]) : __builtin_amdgcn_readlane(lane_begin, request & 63);
         const unsigned units = (many ? __builtin_amdgcn_readfirstlane(begins[request + 1]) : __builtin_amdgcn_readlane(lane_end, request & 63)) - begin;
@@ -286,7 +311,7 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
             const int kv_head = a.head_tiles == 1 ? group : group / a.head_tiles;
             const int head_tile = group - kv_head * a.head_tiles;
             const int first_head = kv_head * a.shared + head_tile * 16, here = min(16, a.shared - head_tile * 16);
-            const int t0 = from * UNIT, t1 = min(len, to * UNIT);
+            const int t0 = from * UNIT, t1 = min(WINDOW ? len - seen.hidden : len, to * UNIT);
 
             float m_ref = -__builtin_inff(), l = 0.0f, vo_sum = 0.0f;
             f32x4 o[VM];
@@ -307,16 +332,16 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int th = t + 16 * h < t1 ? t + 16 * h : t < t1 ? t : t0;
-                    page[h] = table[th >> a.c.page_shift];
+                    page[h] = table[real(th) >> a.c.page_shift];
                 }
             };
             auto load = [&](int t, const int (&page)[2], Step& st) {
                 int64_t tok[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int th = t + 16 * h < t1 ? t + 16 * h : t;
+                    const int th = real(t + 16 * h < t1 ? t + 16 * h : t);
                     const bool ok = page[h] >= 0 && page[h] < a.c.pages;           // a page that does not exist has no tokens
-                    st.there[h] = ok ? min(max(len - (t + 16 * h), 0), 16) : 0;
+                    st.there[h] = ok ? min(max(len - (WINDOW ? real(t) + 16 * h : t + 16 * h), 0), 16) : 0;
                     tok[h] = a.c.first_token(ok ? page[h] : 0, kv_head) + (th & page_mask);
                     const uint8_t* kp = a.c.k + tok[h] * ROW;
                     if constexpr (BITS == 16) {
@@ -406,11 +431,14 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
                         x[j] = s[h][r] * a.scale_log2;
                     }
                 }
-                if (there[0] + there[1] < 32) {
-                    // what lies behind the last token, or in a page that does not exist, may be anything: none of it comes near a sum
+                const int at = real(t);
+                if (there[0] + there[1] < 32 || (WINDOW && at < seen.start && at + kStep > a.sinks)) {
+                    // what lies behind the last token, outside of the window or in a page that does not exist may be anything: none of it
+                    // comes near a sum
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const bool ok = 4 * g + (j & 3) < there[j >> 2];
+                        const int in_half = 4 * g + (j & 3), place = at + 16 * (j >> 2) + in_half;
+                        const bool ok = in_half < there[j >> 2] && (!WINDOW || place >= seen.start || place < a.sinks);
                         x[j] = ok ? x[j] : -__builtin_inff();
                         if constexpr (QUANT) {
                             vs[j] = ok ? vs[j] : 0.0f;
@@ -612,8 +640,8 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
     }
 }
 
-template <int BITS, int D, bool F16, int WAVES> hipError_t launch(const DecodeArgs& a, const DecodePlan& pl, hipStream_t stream) {
-    constexpr auto kernel = attn_decode_kernel<BITS, D, F16, WAVES, BITS == 16 || WAVES == 8>;
+template <int BITS, int D, bool F16, int WAVES, bool WINDOW> hipError_t launch(const DecodeArgs& a, const DecodePlan& pl, hipStream_t stream) {
+    constexpr auto kernel = attn_decode_kernel<BITS, D, F16, WAVES, BITS == 16 || WAVES == 8, WINDOW>;
     auto bytes = [](int heads, int requests, int blocks) {
         const int own = WAVES * heads * (D + 6), join = parts_at(heads, blocks) + 128 * WAVES;
         return (int)sizeof(float) * ((own > join ? own : join) + requests + 1 + WAVES);
@@ -656,14 +684,17 @@ DecodePlan plan_attn_decode(int64_t requests, int heads, int kv_heads, int head_
 }
 
 hipError_t launch_attn_decode(const Rows& q, const any4_kv_cache& c, const int32_t* table, int64_t table_stride, int64_t table_width,
-                              const int32_t* lengths, int64_t requests, int heads, float softmax_scale, uint16_t* out, const DecodePlan& pl,
-                              void* workspace, hipStream_t stream) {
-    DecodeArgs a{q, kv_pages(c), table, table_stride, (int)table_width, lengths, 0, heads, pl.shared, pl.head_tiles, softmax_scale * kLog2e, out,
+                              const int32_t* lengths, int64_t requests, int heads, int window, int sinks, float softmax_scale, uint16_t* out,
+                              const DecodePlan& pl, void* workspace, hipStream_t stream) {
+    DecodeArgs a{q, kv_pages(c), table, table_stride, (int)table_width, lengths, 0, heads, pl.shared, pl.head_tiles, window, sinks, softmax_scale * kLog2e, out,
                  nullptr, static_cast<uint8_t*>(workspace)};
     a.partial = reinterpret_cast<float*>(a.words + pl.words_bytes);
+    auto windows = [&](auto bits, auto f16, auto dim, auto waves) {
+        constexpr int BITS = decltype(bits)::value, D = decltype(dim)::value, WAVES = decltype(waves)::value;
+        return window > 0 ? launch<BITS, D, decltype(f16)::value, WAVES, true>(a, pl, stream) : launch<BITS, D, decltype(f16)::value, WAVES, false>(a, pl, stream);
+    };
     auto waves = [&](auto bits, auto f16, auto dim) {
-        return pl.waves == 8 ? launch<decltype(bits)::value, decltype(dim)::value, decltype(f16)::value, 8>(a, pl, stream)
-                             : launch<decltype(bits)::value, decltype(dim)::value, decltype(f16)::value, 4>(a, pl, stream);
+        return pl.waves == 8 ? windows(bits, f16, dim, std::integral_constant<int, 8>{}) : windows(bits, f16, dim, std::integral_constant<int, 4>{});
     };
     auto dims = [&](auto bits, auto f16) {
         return c.head_dim == 128 ? waves(bits, f16, std::integral_constant<int, 128>{}) : waves(bits, f16, std::integral_constant<int, 64>{});

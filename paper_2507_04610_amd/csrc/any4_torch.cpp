@@ -8,23 +8,11 @@
 // with nothing done, and binding.py goes through its own checks, which name the mistake.  The functions for the cache and for
 // attention are the same for calls whose kernels take 3 - 5 us.  All of them run on the tensors' device, on torch's current stream of
 // it, and without the interpreter's lock while they launch (a full queue makes a launch wait).
-#include <torch/csrc/Exceptions.h>
-#include <torch/csrc/autograd/python_variable.h>
-#include <ATen/ATen.h>
-#include <c10/core/DeviceGuard.h>
-#include <c10/hip/HIPStream.h>
-#include <cmath>
-#include "any4.h"
+#include "any4_torch.h"
 
-namespace {
+using namespace any4_torch;
 
-const at::Tensor* tensor(PyObject* o) {
-    return THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr;
-}
-bool plain(const at::Tensor& t, at::ScalarType ty) {
-    return t.is_cuda() && t.scalar_type() == ty && t.is_contiguous() && t.layout() == at::kStrided;
-}
-bool shaped(const at::Tensor& t, int64_t a, int64_t b) { return t.dim() == 2 && t.size(0) == a && t.size(1) == b; }
+namespace any4_torch {
 
 // torch's current stream of the tensors' device, which is the current one for as long as the guard lives.  (The stream says which device is
 // current: a guard that is not needed took 0.25 us of a call of 5.)
@@ -37,7 +25,9 @@ void* stream_on(const c10::Device& device, c10::OptionalDeviceGuard& guard) {
     return s.stream();
 }
 
-const uint16_t* u16(const at::Tensor& t) { return static_cast<const uint16_t*>(t.data_ptr()); }
+}  // namespace any4_torch
+
+namespace {
 
 // gemm(x, codes, lut, scale, offset, bits, out, workspace, group, repacked)
 //   -> the output tensor; None: not a plain valid call, nothing was done; an int: the runtime refused a launch
@@ -106,59 +96,6 @@ PyObject* gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (out) { Py_INCREF(a[6]); return a[6]; }
     return THPVariable_Wrap(std::move(y));
     END_HANDLE_TH_ERRORS
-}
-
-// The cache as the C ABI takes it, from tensors [pages, kv_heads, page_size, head_dim (bytes of codes)]; false: not a valid one
-bool kv_cache(const at::Tensor& k, const at::Tensor& v, const at::Tensor* scales, long bits, at::ScalarType ty, any4_kv_cache& c) {
-    const at::ScalarType held = bits == 16 ? ty : at::kByte;
-    if ((bits != 16 && bits != 8 && bits != 4) || (ty != at::kBFloat16 && ty != at::kHalf) || k.dim() != 4) return false;
-    if (!plain(k, held) || !plain(v, held) || v.sizes() != k.sizes() || v.device() != k.device()) return false;
-    const int64_t pages = k.size(0), heads = k.size(1), page = k.size(2), width = k.size(3);
-    if (heads > 0xFFFF || page > 0xFFFF || width > 0xFFFF) return false;
-    c = any4_kv_cache{k.data_ptr(), v.data_ptr(), nullptr, pages, (int)page, (int)heads, (int)(bits == 16 ? width : width * 8 / bits), (int)bits, ty == at::kHalf};
-    if (bits == 16) return true;
-    if (!scales || !plain(*scales, at::kBFloat16) || scales->dim() != 4 || scales->size(0) != pages || scales->size(1) != heads ||
-        scales->size(2) != page || scales->size(3) != 4 || scales->device() != k.device())
-        return false;
-    c.scales = static_cast<uint16_t*>(scales->data_ptr());
-    return true;
-}
-// address and strides of rows [tokens, heads, head_dim]
-struct Rows {
-    const uint16_t* p;
-    int64_t token, head;
-    explicit Rows(const at::Tensor& t) : p(u16(t)), token(t.stride(0)), head(t.stride(1)) {}
-};
-// rows [tokens, heads, head_dim] whose heads' values lie side by side
-bool rows(const at::Tensor& t, at::ScalarType ty, int64_t tokens, int64_t heads, int64_t dim, const at::Tensor& on) {
-    return t.is_cuda() && t.scalar_type() == ty && t.layout() == at::kStrided && t.dim() == 3 && t.size(0) == tokens && t.size(1) == heads &&
-           t.size(2) == dim && t.stride(2) == 1 && t.device() == on.device();
-}
-bool list(const at::Tensor& t, at::ScalarType ty, const at::Tensor& on) { return plain(t, ty) && t.dim() == 1 && t.device() == on.device(); }
-// a tensor, or None; false: something else
-bool optional_tensor(PyObject* o, const at::Tensor*& t) {
-    t = o == Py_None ? nullptr : tensor(o);
-    return o == Py_None || t;
-}
-bool whole(PyObject* o, long& v) {
-    if (!PyLong_CheckExact(o)) return false;
-    v = PyLong_AsLong(o);
-    if (!PyErr_Occurred()) return true;
-    PyErr_Clear();
-    return false;
-}
-// softmax_scale, or None: head_dim ** -0.5
-bool scale_of(PyObject* o, int64_t dim, float& s) {
-    if (o == Py_None) { s = (float)std::pow((double)dim, -0.5); return true; }
-    if (!PyFloat_CheckExact(o)) return false;
-    s = (float)PyFloat_AS_DOUBLE(o);
-    return true;
-}
-PyObject* answer(int rc, PyObject* given, at::Tensor&& made) {
-    if (rc == ANY4_ERR_HIP) return PyLong_FromLong(rc);
-    if (rc != ANY4_OK) Py_RETURN_NONE;
-    if (given != Py_None) { Py_INCREF(given); return given; }
-    return THPVariable_Wrap(std::move(made));
 }
 
 // kv_write(k, v, slots, cache_k, cache_v, scales, bits) -> True; None and an int as gemm's
@@ -305,6 +242,12 @@ PyMethodDef methods[] = {
      "kv_read(cache_k, cache_v, slots, scales, bits, f16, out_k, out_v)"},
     {"attn_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attn_decode)), METH_FASTCALL,
      "attn_decode(q, cache_k, cache_v, page_table, lengths, scales, bits, softmax_scale, out, workspace)"},
+    {"attn_decode_window", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attn_decode_window)), METH_FASTCALL,
+     "attn_decode_window(q, cache_k, cache_v, page_table, lengths, scales, bits, softmax_scale, out, workspace, window, sinks)"},
+    {"rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(rope)), METH_FASTCALL,
+     "rope(q, k, positions, freqs, q_norm, k_norm, eps, interleaved, axis_of, out_q, out_k)"},
+    {"rope_kv_write", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(rope_kv_write)), METH_FASTCALL,
+     "rope_kv_write(q, k, v, positions, freqs, slots, cache_k, cache_v, scales, bits, q_norm, k_norm, eps, interleaved, axis_of, out, k_out)"},
     {"attn_prompt", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attn_prompt)), METH_FASTCALL,
      "attn_prompt(q, k, v, q_starts, k_starts, causal, softmax_scale, out)"},
     {"gemm", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(gemm)), METH_FASTCALL,
