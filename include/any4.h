@@ -25,7 +25,7 @@
  *     group-sum pre-pass precedes the GEMM kernel, any4_attn_decode with more than 2048 requests (fewer where
  *     requests * table_width * page_size / 128 units of its KV heads pass 2^31), any4_attn_prompt with
  *     (q_tokens / 128 + requests) * heads of 2^24 and more, any4_kv_write and any4_kv_read with 2^28 tokens and more,
- *     any4_rope and any4_rope_kv_write with 2^26 tokens and more) may then
+ *     any4_rope and any4_rope_kv_write with 2^26 tokens and more, any4_attn_chunk, any4_attn_prompt_window with 2^24 blocks of 128 rows and more) may then
  *     have written part of their outputs or of the workspace: their contents are unspecified.  No exception or abort crosses the ABI.
  *   - K must be a positive multiple of 128 (the group size); M, N >= 1; bits is 4, 3
  *     or 2.  Every pointer must be 16-byte aligned.
@@ -447,6 +447,47 @@ int any4_attn_prompt(const uint16_t* q, int64_t q_token_stride, int64_t q_head_s
                      int64_t q_tokens, int64_t k_tokens, const int32_t* q_starts, const int32_t* k_starts,
                      int64_t requests, int heads, int kv_heads, int head_dim, int f16, int causal,
                      float softmax_scale, uint16_t* out, void* stream);
+
+/*
+ * any4_attn_prompt_window - any4_attn_prompt, causal, where a query sees its last `window` keys (the one at its own place, i + nk - nq, among them) and its
+ * request's first `sinks` only.
+ *   window      1 and more
+ *   sinks       0 and more
+ * q_tokens * (heads / kv_heads) at most 2^31 - 2048, (that / 128 + requests) * kv_heads at most 2^31 - 1.  Everything else as there.
+ */
+int any4_attn_prompt_window(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride,
+                            const uint16_t* k, int64_t k_token_stride, int64_t k_head_stride,
+                            const uint16_t* v, int64_t v_token_stride, int64_t v_head_stride,
+                            int64_t q_tokens, int64_t k_tokens, const int32_t* q_starts, const int32_t* k_starts,
+                            int64_t requests, int heads, int kv_heads, int head_dim, int f16, int64_t window, int64_t sinks,
+                            float softmax_scale, uint16_t* out, void* stream);
+
+/*
+ * any4_attn_chunk - several new tokens of each request (one and more; the next part of a prompt, drafted tokens that are checked, requests of both kinds and
+ * such with a single token in one call) attend to their request's tokens in the cache, where they themselves are the last: request r has the rows
+ * q_starts[r] .. q_starts[r + 1] - 1 of q, nq of them, and its query i sees tokens 0 .. i + lengths[r] - nq, with a window the last `window` of those and
+ * the first `sinks` tokens.  A query that sees no token (nq > lengths[r]) gets zeros.  A token that a query does not see has no influence on it,
+ * whatever the cache holds there, and entries of the page table all of whose tokens no query sees may be anything.
+ * Arithmetic as in any4_attn_decode, with codes p_j times v's scale is what is rounded to 16 bits.  The result is reproducible run to run; its last bits may
+ * depend on the call's other requests and on the page table's width, which say where long sums are cut.
+ *   q           in   16-bit [q_tokens][heads][head_dim], strided rows
+ *   q_starts    in   int32 [requests + 1], ascending; values are taken as at least 0 and at most q_tokens
+ *   lengths     in   int32 [requests], tokens in the cache, the new ones among them; taken as at least 0 and at most table_width * page_size
+ *   page_table  in   as for any4_attn_decode
+ *   window      0: all tokens are seen;  sinks  0 and more (of no effect without a window)
+ *   out         out  16-bit [q_tokens][heads][head_dim], dense; rows that no request has are left as they are
+ *   workspace   at least any4_attn_chunk_workspace_bytes() bytes; may be NULL when that is 0.  Contents on entry and on exit mean nothing; it must not
+ *               serve two calls that overlap in time
+ * q_tokens * (heads / kv_heads) at most 2^31 - 2048, (that / 128 + requests) * kv_heads below 2^31 - 4096, table_width * page_size at most 2^31 - 2048.
+ * requests = 0 and q_tokens = 0 do nothing.
+ */
+int any4_attn_chunk(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const any4_kv_cache* cache,
+                    const int32_t* page_table, int64_t table_stride, int64_t table_width, const int32_t* q_starts, const int32_t* lengths,
+                    int64_t q_tokens, int64_t requests, int heads, int64_t window, int64_t sinks, float softmax_scale, uint16_t* out,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace any4_attn_chunk needs (0 for invalid arguments); max_tokens = table_width * page_size. */
+size_t any4_attn_chunk_workspace_bytes(int64_t requests, int64_t q_tokens, int heads, int kv_heads, int head_dim, int64_t max_tokens);
 
 /* Static, human-readable text for a return code. */
 const char* any4_strerror(int code);

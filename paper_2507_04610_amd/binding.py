@@ -20,7 +20,7 @@ GROUP = 128
 
 EXPORTS = ("any4_pack", "any4_dequant", "any4_gemm", "any4_gemm_workspace_bytes", "any4_repack", "any4_repack_bytes", "any4_gemm_repacked", "any4_dequant_grouped", "any4_gemm_grouped", "any4_dequant_f16", "any4_gemm_f16",
            "any4_quantize", "any4_quantize_with_gap", "any4_quantize_max_k", "any4_gemm_noalloc", "any4_dequant_single_table", "any4_gemm_single_table",
-           "any4_kv_write", "any4_kv_read", "any4_rope", "any4_rope_kv_write", "any4_attn_decode", "any4_attn_decode_window", "any4_attn_decode_workspace_bytes", "any4_attn_prompt", "any4_strerror", "any4_version")
+           "any4_kv_write", "any4_kv_read", "any4_rope", "any4_rope_kv_write", "any4_attn_decode", "any4_attn_decode_window", "any4_attn_decode_workspace_bytes", "any4_attn_chunk", "any4_attn_chunk_workspace_bytes", "any4_attn_prompt", "any4_attn_prompt_window", "any4_strerror", "any4_version")
 
 
 class Any4Error(RuntimeError):
@@ -108,6 +108,12 @@ def load_library() -> ctypes.CDLL:
     lib.any4_attn_decode_workspace_bytes.argtypes = [i64, ci, ci, ci, i64]
     lib.any4_attn_prompt.restype = ci
     lib.any4_attn_prompt.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, i64, i64, vp, vp, i64, ci, ci, ci, ci, ci, f32, vp, vp]
+    lib.any4_attn_prompt_window.restype = ci
+    lib.any4_attn_prompt_window.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, i64, i64, vp, vp, i64, ci, ci, ci, ci, i64, i64, f32, vp, vp]
+    lib.any4_attn_chunk.restype = ci
+    lib.any4_attn_chunk.argtypes = [vp, i64, i64, cache, vp, i64, i64, vp, vp, i64, i64, ci, i64, i64, f32, vp, vp, ctypes.c_size_t, vp]
+    lib.any4_attn_chunk_workspace_bytes.restype = ctypes.c_size_t
+    lib.any4_attn_chunk_workspace_bytes.argtypes = [i64, i64, ci, ci, ci, i64]
     lib.any4_strerror.restype = ctypes.c_char_p
     lib.any4_strerror.argtypes = [ci]
     lib.any4_version.restype = ci
@@ -134,7 +140,7 @@ def _no_native_gemm(*args):
 
 class _NoNativeCalls:
     """the same for the cache and attention"""
-    kv_write = kv_read = rope = rope_kv_write = attn_decode = attn_decode_window = attn_prompt = staticmethod(_no_native_gemm)
+    kv_write = kv_read = rope = rope_kv_write = attn_decode = attn_decode_window = attn_chunk = attn_prompt = attn_prompt_window = staticmethod(_no_native_gemm)
 
 
 def _calls():
@@ -680,12 +686,73 @@ def any4_attn_decode(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tens
     return out
 
 
+def any4_attn_chunk_workspace_bytes(requests: int, q_tokens: int, heads: int, kv_heads: int, head_dim: int, max_tokens: int) -> int:
+    return int(load_library().any4_attn_chunk_workspace_bytes(requests, q_tokens, heads, kv_heads, head_dim, max_tokens))
+
+
+def any4_attn_chunk(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tensor, page_table: torch.Tensor, q_starts: torch.Tensor,
+                    lengths: torch.Tensor, scales: torch.Tensor | None = None, bits: int = 16, window: int | None = None, sinks: int = 0,
+                    softmax_scale: float | None = None, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """[q_tokens, heads, head_dim]: several new tokens of each request (q, packed: request r in rows q_starts[r] .. q_starts[r + 1] - 1, int32
+    [requests + 1]) attend to the tokens of its pages (page_table, int32 [requests, table_width]) in the cache, where they are the last of
+    lengths[r] (int32 [requests]): query i of nq sees tokens 0 .. i + lengths[r] - nq, with a window the last `window` of those and the first `sinks`."""
+    if window is None:
+        _no_sinks(sinks)
+        some = 0, 0
+    else:
+        some = _part(window, sinks)
+    r = _calls().attn_chunk(q, cache_k, cache_v, page_table, q_starts, lengths, scales, bits, *some, softmax_scale, out, workspace)
+    if r is not None:
+        if r.__class__ is int:
+            _check(r, "any4_attn_chunk")
+        return r
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise Any4Error("q must be a tensor of 3 dimensions: tokens, heads, head_dim")
+    n, heads = q.shape[:2]
+    cache, kv_heads, dim = _cache(cache_k, cache_v, scales, bits, q.dtype)
+    pq = _rows(q, q.dtype, "q", (n, heads, dim))
+    if heads < 1 or kv_heads < 1 or heads % kv_heads:
+        raise Any4Error(f"{heads} query heads are no multiple of {kv_heads} KV heads")
+    pl = _dev(lengths, torch.int32, "lengths")
+    if lengths.dim() != 1:
+        raise Any4Error("lengths must have one dimension")
+    requests = lengths.shape[0]
+    ps = _dev(q_starts, torch.int32, "q_starts")
+    _shape(q_starts, (requests + 1,), "q_starts")
+    if not isinstance(page_table, torch.Tensor) or not page_table.is_cuda or page_table.dtype != torch.int32:
+        raise Any4Error("page_table must be an int32 tensor in device memory")
+    if page_table.dim() != 2 or page_table.shape[0] != requests or page_table.stride(1) != 1:
+        raise Any4Error(f"page_table must have {requests} rows of page numbers that lie side by side, got shape {tuple(page_table.shape)}")
+    if out is None:
+        out = torch.empty((n, heads, dim), dtype=q.dtype, device=q.device)
+    _shape(out, (n, heads, dim), "out")
+    po = _dev(out, q.dtype, "out")
+    _same_device(q, cache_k, page_table, q_starts, lengths, out)
+    width = page_table.shape[1]
+    need = _bytes_on(q.device, "any4_attn_chunk_workspace_bytes", requests, n, heads, kv_heads, dim, width * cache.page_size)
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    pw, wbytes = _scratch(workspace, q.device) if workspace is not None else (None, 0)
+    _launch("any4_attn_chunk", q.device, *pq, ctypes.byref(cache), page_table.data_ptr(), page_table.stride(0), width, ps, pl, n, requests, heads, *some,
+            dim ** -0.5 if softmax_scale is None else softmax_scale, po, pw, wbytes)
+    return out
+
+
 def any4_attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts: torch.Tensor, k_starts: torch.Tensor | None = None,
-                     causal: bool = True, softmax_scale: float | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+                     causal: bool = True, softmax_scale: float | None = None, out: torch.Tensor | None = None, window: int | None = None,
+                     sinks: int = 0) -> torch.Tensor:
     """[q_tokens, heads, head_dim]: packed prompts, request r in rows q_starts[r] .. q_starts[r + 1] - 1 of q and k_starts[r] .. of k and v
     [k_tokens, kv_heads, head_dim] (int32 [requests + 1]; k_starts None: q_starts).  Where a request has more rows in k, the first
-    of them are the context in front of its queries: causal, query i of nq sees keys 0 .. i + nk - nq."""
-    r = _calls().attn_prompt(q, k, v, q_starts, k_starts, causal, softmax_scale, out)
+    of them are the context in front of its queries: causal, query i of nq sees keys 0 .. i + nk - nq.
+    window (causal only): of those the last `window` and the request's first `sinks`."""
+    if window is None:
+        _no_sinks(sinks)
+        r = _calls().attn_prompt(q, k, v, q_starts, k_starts, causal, softmax_scale, out)
+    else:
+        window, sinks = _part(window, sinks)
+        if not causal:
+            raise Any4Error("a window is of causal attention")
+        r = _calls().attn_prompt_window(q, k, v, q_starts, k_starts, window, sinks, softmax_scale, out)
     if r is not None:
         if r.__class__ is int:
             _check(r, "any4_attn_prompt")
@@ -714,6 +781,7 @@ def any4_attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts
     _shape(out, (n, heads, dim), "out")
     po = _dev(out, q.dtype, "out")
     _same_device(q, k, v, q_starts, k_starts, out)
-    _launch("any4_attn_prompt", q.device, *pq, *pk, *pv, n, k.shape[0], ps, pt, q_starts.shape[0] - 1, heads, kv_heads, dim,
-            int(q.dtype == torch.float16), int(causal), dim ** -0.5 if softmax_scale is None else softmax_scale, po)
+    name, part = ("any4_attn_prompt", (int(causal),)) if window is None else ("any4_attn_prompt_window", (window, sinks))
+    _launch(name, q.device, *pq, *pk, *pv, n, k.shape[0], ps, pt, q_starts.shape[0] - 1, heads, kv_heads, dim,
+            int(q.dtype == torch.float16), *part, dim ** -0.5 if softmax_scale is None else softmax_scale, po)
     return out

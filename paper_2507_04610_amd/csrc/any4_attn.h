@@ -45,6 +45,17 @@ template <int LANES, class F> __device__ __forceinline__ float lanes_reduce(floa
     return v;
 }
 
+// each lane gets the sum of the lanes up to its own
+__device__ __forceinline__ int lanes_scan(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111 /*row_shr:1*/, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112 /*row_shr:2*/, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114 /*row_shr:4*/, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118 /*row_shr:8*/, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142 /*row_bcast:15*/, 0xA, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143 /*row_bcast:31*/, 0xC, 0xF, false);
+    return v;
+}
+
 // Strides in values: from a token (or request) to the next, from a head to the next.  A head's values lie side by side.
 struct Rows {
     const uint16_t* p;
@@ -110,5 +121,29 @@ inline int64_t prompt_blocks(int64_t q_tokens, int64_t requests, int heads) {
     return (q_tokens / kPromptRows + (requests < q_tokens ? requests : q_tokens)) * heads;
 }
 hipError_t launch_attn_prompt(const PromptArgs& a, hipStream_t stream);
+
+// The newest tokens of requests over the cache, or packed prompts over packed keys (k, v, k_starts; no cache), with or without a window.
+struct ChunkArgs {
+    Rows q, k, v;
+    int64_t q_tokens, k_tokens;
+    const int32_t* q_starts;
+    const int32_t* k_starts;
+    const int32_t* table;
+    int64_t table_stride, table_width;
+    const int32_t* lengths;
+    int requests, heads, kv_heads, head_dim, window, sinks;      // window 0: all tokens are seen
+    bool f16;
+    float softmax_scale;
+    uint16_t* out;
+};
+// How a call is shared out: blocks (some have nothing to do), how many of them would fill the chip (0: no keys are cut into pieces), pieces that
+// the workspace has room for, tiles of rows that may be cut.
+struct ChunkPlan {
+    int64_t blocks;
+    int target, slots, cut_tiles;
+    size_t workspace;
+};
+ChunkPlan plan_attn_chunk(int64_t requests, int64_t q_tokens, int heads, int kv_heads, int head_dim, int64_t max_tokens, int cus);
+hipError_t launch_attn_chunk(const ChunkArgs& a, const any4_kv_cache* cache, const ChunkPlan& pl, void* workspace, hipStream_t stream);
 
 }  // namespace any4

@@ -23,6 +23,9 @@ bool heads_ok(int heads, int kv_heads) {
     return kv_heads >= 1 && kv_heads <= kMaxKvHeads && heads >= 1 && heads <= kMaxHeads && heads % kv_heads == 0;
 }
 
+// the rows of a call (queries of the heads that share a KV head) are counted in 32 bits
+bool rows_ok(int64_t q_tokens, int heads, int kv_heads) { return q_tokens * (heads / kv_heads) <= kMaxTokens; }
+
 int cache_check(const any4_kv_cache* c) {
     if (!c || !c->k || !c->v) return ANY4_ERR_NULL;
     if (c->bits != 16 && c->bits != 8 && c->bits != 4) return ANY4_ERR_BITS;
@@ -178,6 +181,57 @@ int any4_attn_prompt(const uint16_t* q, int64_t q_token_stride, int64_t q_head_s
     const PromptArgs a{{q, q_token_stride, q_head_stride}, {k, k_token_stride, k_head_stride}, {v, v_token_stride, v_head_stride},
                        q_tokens, k_tokens, q_starts, k_starts, (int)requests, heads, kv_heads, head_dim, f16 != 0, causal != 0, softmax_scale, out};
     return launched(launch_attn_prompt(a, static_cast<hipStream_t>(stream)));
+}
+
+int any4_attn_prompt_window(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const uint16_t* k, int64_t k_token_stride,
+                            int64_t k_head_stride, const uint16_t* v, int64_t v_token_stride, int64_t v_head_stride, int64_t q_tokens,
+                            int64_t k_tokens, const int32_t* q_starts, const int32_t* k_starts, int64_t requests, int heads, int kv_heads,
+                            int head_dim, int f16, int64_t window, int64_t sinks, float softmax_scale, uint16_t* out, void* stream) {
+    if (requests < 0 || requests > kMaxTokens || q_tokens < 0 || q_tokens > kMaxTokens || k_tokens < 0 || k_tokens > kMaxTokens ||
+        !heads_ok(heads, kv_heads) || (head_dim != 64 && head_dim != 128) || !scale_ok(softmax_scale) || window < 1 || sinks < 0 ||
+        !strides_ok(q_token_stride, q_head_stride) || !strides_ok(k_token_stride, k_head_stride) || !strides_ok(v_token_stride, v_head_stride) ||
+        k_token_stride >= kMaxStride || v_token_stride >= kMaxStride || !rows_ok(q_tokens, heads, kv_heads))
+        return ANY4_ERR_SHAPE;
+    const ChunkPlan pl = plan_attn_chunk(requests, q_tokens, heads, kv_heads, head_dim, 0, device_compute_units());
+    if (pl.blocks > 0x7FFFFFFF) return ANY4_ERR_SHAPE;
+    if (requests == 0 || q_tokens == 0) return ANY4_OK;
+    // (without a single key k and v are not read)
+    if (!q || !q_starts || !k_starts || !out || (k_tokens > 0 && (!k || !v))) return ANY4_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned(q_starts, 4) || !aligned(k_starts, 4) || !aligned16(out) ||
+        !strides_aligned(q_token_stride, q_head_stride) || !strides_aligned(k_token_stride, k_head_stride) ||
+        !strides_aligned(v_token_stride, v_head_stride))
+        return ANY4_ERR_ALIGN;
+    const ChunkArgs a{{q, q_token_stride, q_head_stride}, {k, k_token_stride, k_head_stride}, {v, v_token_stride, v_head_stride}, q_tokens, k_tokens, q_starts,
+                      k_starts, nullptr, 0, 0, nullptr, (int)requests, heads, kv_heads, head_dim, at_most(window), at_most(sinks), f16 != 0, softmax_scale, out};
+    return launched(launch_attn_chunk(a, nullptr, pl, nullptr, static_cast<hipStream_t>(stream)));
+}
+
+size_t any4_attn_chunk_workspace_bytes(int64_t requests, int64_t q_tokens, int heads, int kv_heads, int head_dim, int64_t max_tokens) {
+    if (requests < 1 || requests > kMaxTokens || q_tokens < 1 || q_tokens > kMaxTokens || !heads_ok(heads, kv_heads) || (head_dim != 64 && head_dim != 128) ||
+        max_tokens < 1 || max_tokens > kMaxTokens || !rows_ok(q_tokens, heads, kv_heads))
+        return 0;
+    return plan_attn_chunk(requests, q_tokens, heads, kv_heads, head_dim, max_tokens, device_compute_units()).workspace;
+}
+
+int any4_attn_chunk(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const any4_kv_cache* cache, const int32_t* page_table,
+                    int64_t table_stride, int64_t table_width, const int32_t* q_starts, const int32_t* lengths, int64_t q_tokens, int64_t requests,
+                    int heads, int64_t window, int64_t sinks, float softmax_scale, uint16_t* out, void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = cache_check(cache)) return rc;
+    if (requests < 0 || requests > kMaxTokens || q_tokens < 0 || q_tokens > kMaxTokens || !heads_ok(heads, cache->kv_heads) || !scale_ok(softmax_scale) ||
+        !strides_ok(q_token_stride, q_head_stride) || table_width < 1 || table_width > kMaxTokens / cache->page_size || table_stride < 0 || window < 0 ||
+        sinks < 0 || !rows_ok(q_tokens, heads, cache->kv_heads))
+        return ANY4_ERR_SHAPE;
+    const ChunkPlan pl = plan_attn_chunk(requests, q_tokens, heads, cache->kv_heads, cache->head_dim, table_width * cache->page_size, device_compute_units());
+    if (pl.blocks > 0x7FFFFFFF) return ANY4_ERR_SHAPE;
+    if (requests == 0 || q_tokens == 0) return ANY4_OK;
+    if (!q || !page_table || !q_starts || !lengths || !out) return ANY4_ERR_NULL;
+    if (!aligned16(q) || !aligned(page_table, 4) || !aligned(q_starts, 4) || !aligned(lengths, 4) || !aligned16(out) || !aligned16(workspace) ||
+        !strides_aligned(q_token_stride, q_head_stride))
+        return ANY4_ERR_ALIGN;
+    if (pl.workspace > 0 && (!workspace || workspace_bytes < pl.workspace)) return ANY4_ERR_WORKSPACE;
+    const ChunkArgs a{{q, q_token_stride, q_head_stride}, {nullptr, 0, 0}, {nullptr, 0, 0}, q_tokens, 0, q_starts, nullptr, page_table, table_stride, table_width,
+                      lengths, (int)requests, heads, cache->kv_heads, cache->head_dim, at_most(window), at_most(sinks), cache->f16 != 0, softmax_scale, out};
+    return launched(launch_attn_chunk(a, cache, pl, workspace, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -1,0 +1,833 @@
+// any4_attn_chunk / any4_attn_prompt_window: the newest tokens of each request attend, causally, to its tokens in the paged cache (16 bits, or codes
+// of 8 or 4), or packed prompts to packed keys; with a window each query sees the last keys up to its own and the first of the request.
+//
+//     s_ij = scale q_i . k_j,   o_i = sum_j exp(s_ij - m_i) v_j / sum_j exp(s_ij - m_i)     over j <= p_i, j > p_i - window or j < sinks
+// in one pass over the keys with a running maximum, as any4_attn_prompt does it.
+//
+// A block takes 128 rows of one KV head: a row is a query of one of the heads that share it, a query's heads side by side, so that a few new
+// tokens fill a block with their heads and read k and v once.  A wavefront takes 32 rows and walks over the keys 64 at a time: S^T = K Q^T with
+// v_mfma_f32_32x32x16, the scores of a row in two lanes, the weights at once the B operand of O^T = V^T P^T.  Tiles outside of what the block's rows see (behind
+// the last query, between the first tokens and the window) are left out.
+//
+// 16 bits: k and v are copied to LDS without passing registers, the next 64 keys while these are worked on.  Codes c become fp16 on their way
+// to LDS, exactly (k: c + kBias, v: c - kCentre), and scales and offsets are applied to sums, so that codes cost no rounding of their own:
+//     q . k_j = ks_j (q . c'_j) + (ko_j - kBias ks_j) sum(q)
+//     o = sum_j (p_j vs_j) (c_j - kCentre) + sum_j p_j (vo_j + kCentre vs_j)
+// bf16 queries become fp16 for that, exactly too: a row is scaled by a power of two.  The product p_j vs_j is rounded to fp16; the exponent of the
+// largest vs_j that a row has seen is taken off it together with the running maximum.
+//
+// Who does what.  Lengths are the device's, so each block finds its rows itself.  Where whole tiles of rows do not fill the chip, their keys are cut
+// into pieces, no more than it takes; pieces leave sums, maximum and sum of weights in the workspace, and a second launch joins them.
+//
+// Rounding: scores, maxima, sums and accumulators are fp32; the weights (times vs_j) are rounded to 16 bits for the matrix cores, once.
+#include "any4_attn.h"
+#include "any4_attn_tile.h"
+#include "any4_internal.h"
+#include "any4_launches.h"
+#include "any4_lds_copy.h"
+
+namespace any4 {
+
+namespace {
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves, kRowTile = 32 * kWaves;
+constexpr int kLeastPiece = 4;                                  // key tiles of a piece: a join costs as much as a few of them
+constexpr int kNoWindow = 0x7FFFF800;                           // more than any request's tokens
+constexpr int kFold = 60;                                       // exponents of vs_j beyond this one are taken off p_j vs_j apart from the maximum
+typedef __attribute__((address_space(3))) float* lds_f;
+typedef __attribute__((address_space(3))) f32x4* lds_f4;
+typedef __attribute__((address_space(3))) uint32_t* lds_u1;
+constexpr int kRows = 0;                                        // SOURCE: packed rows; otherwise the cache's bits
+
+struct Args {
+    Rows q, k, v;                      // k, v: packed keys
+    KvPages c;
+    const int32_t* table;
+    int64_t table_stride;
+    int table_width;
+    const int32_t* q_starts;
+    const int32_t* k_starts;           // packed keys
+    const int32_t* lengths;            // cache
+    int q_tokens, k_tokens, requests, heads, kv_heads, shared, window, sinks;
+    int target, slots;                 // blocks that fill the chip (0: nothing is cut); pieces that the workspace has room for
+    unsigned first_block;              // of this launch
+    float scale_log2;
+    uint16_t* out;
+    float* partial;
+};
+
+// A request's rows and keys.
+struct Request {
+    int q_at, lq, k_at, lk;
+};
+template <int SOURCE> __device__ __forceinline__ Request request_of(const Args& a, int r) {
+    Request q;
+    q.q_at = min(max(a.q_starts[r], 0), a.q_tokens);
+    q.lq = max(min(max(a.q_starts[r + 1], 0), a.q_tokens) - q.q_at, 0);
+    if constexpr (SOURCE == kRows) {
+        q.k_at = min(max(a.k_starts[r], 0), a.k_tokens);
+        q.lk = max(min(max(a.k_starts[r + 1], 0), a.k_tokens) - q.k_at, 0);
+    } else {
+        q.k_at = 0;
+        q.lk = (int)min((int64_t)max(a.lengths[r], 0), (int64_t)a.table_width << a.c.page_shift);
+    }
+    return q;
+}
+
+// The tiles of keys that a tile of rows sees: the first `front`, then from the one in which the window begins, `gap` tiles further on.
+struct Span {
+    int first, last;                   // first and last query
+    int front, gap, tiles;
+    __device__ __forceinline__ int real(int t) const { return t < front ? t : t + gap; }
+};
+__device__ __forceinline__ Span span_of(const Args& a, const Request& r, int tile) {
+    Span s;
+    const int rows = r.lq * a.shared, ahead = r.lk - r.lq;
+    s.first = (int)((unsigned)(tile * kRowTile) / (unsigned)a.shared);
+    s.last = (int)((unsigned)(min(tile * kRowTile + kRowTile, rows) - 1) / (unsigned)a.shared);
+    const int end = max(ahead + s.last + 1, 0), start = max(max(ahead + s.first, 0) + 1 - a.window, 0);
+    const int begin = start / kKeys;
+    s.front = min((int)(((unsigned)min(a.sinks, end) + kKeys - 1) / kKeys), begin);
+    s.gap = begin - s.front;
+    s.tiles = (int)(((unsigned)end + kKeys - 1) / kKeys) - s.gap;
+    return s;
+}
+
+// Which rows and keys a block has.  Blocks of a request: tile of rows by tile of rows, each tile's pieces side by side.
+struct Work {
+    int request, tile, piece, pieces, slot;
+    Request r;
+};
+struct Shares {                        // of 64 requests, a lane each
+    Request r;
+    int tiles, pieces;
+};
+template <int SOURCE> __device__ __forceinline__ Shares shares_of(const Args& a, int r0, int least, int lane) {
+    Shares s{};
+    s.pieces = 1;
+    if (r0 + lane < a.requests) {
+        s.r = request_of<SOURCE>(a, r0 + lane);
+        s.tiles = (int)(((unsigned)(s.r.lq * a.shared) + kRowTile - 1) / kRowTile);
+        if (s.tiles > 0 && least > 0) s.pieces = max((span_of(a, s.r, s.tiles - 1).tiles + least - 1) / least, 1);
+    }
+    return s;
+}
+// key tiles of a piece where all requests' fill the chip: sums of tiles in fp32, in one order everywhere
+template <int SOURCE> __device__ __forceinline__ int piece_tiles(const Args& a, int lane) {
+    if (a.target == 0) return 0;
+    float all = 0.0f;
+    for (int r0 = 0; r0 < a.requests; r0 += 64) {
+        const Shares s = shares_of<SOURCE>(a, r0, 0, lane);
+        float mine = 0.0f;
+        if (s.tiles > 0) mine = (float)s.tiles * (float)span_of(a, s.r, s.tiles - 1).tiles;
+        all += wave_sum(mine);
+    }
+    return __builtin_amdgcn_readfirstlane(max((int)fminf(ceilf(all * (float)a.kv_heads / (float)a.target), 1073741824.0f), kLeastPiece));
+}
+// JOIN: place counts the tiles of rows that are cut, otherwise blocks; both without KV heads
+template <int SOURCE, bool JOIN> __device__ __forceinline__ Work work_of(const Args& a, unsigned place, unsigned kv_head, int lane) {
+    const int least = piece_tiles<SOURCE>(a, lane);
+    Work w{-1, 0, 0, 1, 0, {}};
+    for (int r0 = 0, before = 0, cut_before = 0; r0 < a.requests && w.request < 0; r0 += 64) {
+        Shares s = shares_of<SOURCE>(a, r0, least, lane);
+        int cut = s.pieces > 1 ? s.tiles * s.pieces : 0;
+        const int cut_sum = lanes_scan(cut);
+        // (as many as were planned for; were there more, they would be left whole)
+        if (cut > 0 && (int64_t)(cut_before + cut_sum) * a.kv_heads > a.slots) {
+            s.pieces = 1;
+            cut = 0;
+        }
+        const int own = JOIN ? (s.pieces > 1 ? s.tiles : 0) : s.tiles * s.pieces, sum = lanes_scan(own);
+        const unsigned long long past = __builtin_amdgcn_ballot_w64((unsigned)(before + sum) > place);
+        if (past) {
+            const int f = __builtin_ctzll(past);
+            w.request = r0 + f;
+            w.r.q_at = __builtin_amdgcn_readlane(s.r.q_at, f);
+            w.r.lq = __builtin_amdgcn_readlane(s.r.lq, f);
+            w.r.k_at = __builtin_amdgcn_readlane(s.r.k_at, f);
+            w.r.lk = __builtin_amdgcn_readlane(s.r.lk, f);
+            w.pieces = __builtin_amdgcn_readlane(s.pieces, f);
+            const int tiles = __builtin_amdgcn_readlane(s.tiles, f);
+            const int at = (int)place - (before + __builtin_amdgcn_readlane(sum, f) - __builtin_amdgcn_readlane(own, f));
+            const int tile = JOIN ? at : at / w.pieces;
+            w.piece = JOIN ? 0 : at - tile * w.pieces;
+            w.tile = tiles - 1 - tile;                          // the most keys first
+            w.slot = (cut_before + __builtin_amdgcn_readlane(cut_sum, f) - tiles * w.pieces + tile * w.pieces + w.piece) * a.kv_heads + (int)kv_head;
+        }
+        before += __builtin_amdgcn_readlane(sum, 63);
+        cut_before += __builtin_amdgcn_readlane(cut_sum, 63);
+    }
+    return w;
+}
+
+// floats of a piece: sums [wavefront][4 values of a row][lane][4], then [row] maximum and sum of weights
+template <int D> constexpr int kPieceFloats = kRowTile * (D + 2);
+
+template <int BITS> struct Codes {
+    static constexpr float kBias = BITS == 8 ? 1024.0f : 64.0f, kCentre = (float)(1 << (BITS - 1));
+};
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t add_f16(uint32_t x, float y) {
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, x) + f16x2{(_Float16)y, (_Float16)y});
+}
+// codes of a word as fp16, k: c + kBias, with 4 bits in the order 0 4 1 5 2 6 3 7; v: c - kCentre
+template <int BITS, bool V> __device__ __forceinline__ void widen(uint32_t w, uint32_t* to) {
+    if constexpr (BITS == 8) {
+        to[0] = __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u);
+        to[1] = __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u);
+        if constexpr (V) {
+            to[0] = add_f16(to[0], -1152.0f);
+            to[1] = add_f16(to[1], -1152.0f);
+        }
+    } else {
+        // 1024 + c where a code lies in the last bits of a half, 64 + c four bits further up
+        const uint32_t u = w >> 8;
+        uint32_t x[4] = {(w & 0x000F000Fu) | 0x64006400u, (w & 0x00F000F0u) | 0x54005400u, (u & 0x000F000Fu) | 0x64006400u, (u & 0x00F000F0u) | 0x54005400u};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (V) x[i] = add_f16(x[i], i & 1 ? -72.0f : -1032.0f);
+            else if (!(i & 1)) x[i] = add_f16(x[i], -960.0f);
+        }
+        if constexpr (V) {
+            to[0] = __builtin_amdgcn_perm(x[1], x[0], 0x05040100u);
+            to[1] = __builtin_amdgcn_perm(x[3], x[2], 0x05040100u);
+            to[2] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302u);
+            to[3] = __builtin_amdgcn_perm(x[3], x[2], 0x07060302u);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) to[i] = x[i];
+        }
+    }
+}
+
+// bytes that a thread loads at a time, as words
+template <int N> __device__ __forceinline__ void load_bytes(const uint8_t* p, uint32_t (&w)[N]) {
+    if constexpr (N == 4) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = x[i];
+    } else {
+        static_assert(N == 2, "a thread's part of a tile");
+        const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+        w[0] = x[0];
+        w[1] = x[1];
+    }
+}
+
+// two weights for the matrix cores, the first in the low half
+template <bool F16> __device__ __forceinline__ uint32_t pack(float a, float b) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    if constexpr (F16) return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{a, b}), f16x2));
+    else return f32x2_to_h16x2<false>(a, b);
+}
+
+// the other half of the wavefront's
+__device__ __forceinline__ float other_half(float v) {
+    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+    return __uint_as_float((threadIdx.x & 32) ? x[0] : x[1]);
+}
+
+template <int SOURCE, int D, bool F16>
+__global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
+    using T = Tile<D, kWaves>;
+    constexpr bool CODES = SOURCE == 8 || SOURCE == 4, PAGED = SOURCE != kRows, MMA16 = F16 || CODES;
+    constexpr int QM = D / 16, OM = D / 32;
+    // LDS: two tiles of k, two of v; per tile either rows of v that are not finite (16 bits a wavefront), or the tokens' scales, the largest, and whose are not finite
+    constexpr uint32_t kAside = 4 * T::kBytes, kAsideBytes = CODES ? 4 * 256 + 16 : 16;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 31, g = lane >> 5;
+
+    // KV heads fastest: blocks that read the same keys tend to share an XCD and its L2
+    const unsigned block = a.first_block + blockIdx.x, place = block / (unsigned)a.kv_heads, kv_head = block - place * (unsigned)a.kv_heads;
+    const Work w = work_of<SOURCE, false>(a, place, kv_head, lane);
+    if (w.request < 0) return;
+    const int lq = w.r.lq, lk = w.r.lk, rows = lq * a.shared, ahead = lk - lq;
+    const Span span = span_of(a, w.r, w.tile);
+    const int each = (span.tiles + w.pieces - 1) / w.pieces;
+    const int t_first = w.piece * each, t_end = min(span.tiles, t_first + each);
+    if (w.pieces > 1 && t_first >= t_end) return;               // (the join knows)
+
+    const int row0 = w.tile * kRowTile + 32 * wave, row = min(row0 + n, rows - 1);
+    const bool active = row0 < rows;
+    const int query = (int)((unsigned)row / (unsigned)a.shared);
+    // this row sees keys up to `lim` that lie in its window or are among the first `sinks`
+    const int lim = ahead + query;
+    // all rows see keys up to `all_lim` that lie at `all_lo` or behind it or are among the first
+    const int all_lim = ahead + span.first, all_lo = max(ahead + span.last, 0) + 1 - a.window;
+
+    // Q^T, fp16 for codes: a row of bf16 is scaled by a power of two into the upper part of fp16's range
+    u32x4 q[QM];
+    float scale = a.scale_log2, sum_q = 0.0f;
+    {
+        const int head = (int)kv_head * a.shared + (row - query * a.shared);
+        const uint16_t* qp = a.q.p + (int64_t)(w.r.q_at + query) * a.q.token + (int64_t)head * a.q.head + 8 * g;
+#pragma unroll
+        for (int i = 0; i < QM; ++i) q[i] = *reinterpret_cast<const u32x4*>(qp + 16 * i);
+        if constexpr (CODES) {
+            if constexpr (!F16) {
+                float top = 0.0f;
+#pragma unroll
+                for (int i = 0; i < QM; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(bf16lo_to_f32(q[i][j])), fabsf(bf16hi_to_f32(q[i][j]))));
+                top = fmaxf(top, other_half(top));
+                const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 127);
+                const float by = __builtin_ldexpf(1.0f, 14 - e);
+                scale *= __builtin_ldexpf(1.0f, e - 14);
+#pragma unroll
+                for (int i = 0; i < QM; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) q[i][j] = pack<true>(bf16lo_to_f32(q[i][j]) * by, bf16hi_to_f32(q[i][j]) * by);
+            }
+#pragma unroll
+            for (int i = 0; i < QM; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum_q += h16lo_to_f32<true>(q[i][j]) + h16hi_to_f32<true>(q[i][j]);
+            sum_q += other_half(sum_q);
+            if constexpr (SOURCE == 4) {
+#pragma unroll
+                for (int i = 0; i < QM; ++i) {
+                    const u32x4 r = q[i];
+                    q[i] = u32x4{__builtin_amdgcn_perm(r[2], r[0], 0x05040100u), __builtin_amdgcn_perm(r[2], r[0], 0x07060302u),
+                                 __builtin_amdgcn_perm(r[3], r[1], 0x05040100u), __builtin_amdgcn_perm(r[3], r[1], 0x07060302u)};
+                }
+            }
+        }
+    }
+
+    // Pages of a tile: lane 0 .. 3's of 16 tokens each (the last token's again behind it).
+    const int page_mask = PAGED ? (1 << a.c.page_shift) - 1 : 0;
+    const int32_t* table = PAGED ? a.table + (int64_t)w.request * a.table_stride : nullptr;
+    auto pages_of = [&](int t) -> int {
+        if constexpr (PAGED) return table[min(span.real(t) * kKeys + 16 * (lane & 3), lk - 1) >> a.c.page_shift];
+        else return 0;
+    };
+    // a page that does not exist has no tokens: the first one is read in its place and masked
+    auto there = [&](int page) -> bool { return !PAGED || (page >= 0 && page < a.c.pages); };
+    auto valid_of = [&](int page) -> unsigned { return (unsigned)__builtin_amdgcn_ballot_w64(there(page)) & 15u; };
+
+    // 16 bits.  Copies: lane -> row and piece of each instruction; LDS has piece c of row r at c ^ swizzle(r).
+    const int copy_row = T::kCopies * T::kRows * wave + lane / T::kPieces, copy_piece = lane % T::kPieces;
+    const uint32_t k_step = SOURCE == kRows ? (uint32_t)a.k.token * 2u : (uint32_t)T::kRow, v_step = SOURCE == kRows ? (uint32_t)a.v.token * 2u : (uint32_t)T::kRow;
+    auto copy_tile = [&](int t, int page, uint32_t parity) {
+        const int k0 = span.real(t) * kKeys;
+        const char *kb, *vb;
+        int first;                                              // the token that row 0's address would be of
+        if constexpr (SOURCE == kRows) {
+            first = k0;
+            kb = reinterpret_cast<const char*>(a.k.p + (int64_t)w.r.k_at * a.k.token + (int64_t)kv_head * a.k.head) + (int64_t)k0 * k_step;
+            vb = reinterpret_cast<const char*>(a.v.p + (int64_t)w.r.k_at * a.v.token + (int64_t)kv_head * a.v.head) + (int64_t)k0 * v_step;
+        } else {
+            // (a wavefront's 16 rows are one page's)
+            static_assert(T::kCopies * T::kRows == 16, "a wavefront copies 16 rows");
+            const int p = __builtin_amdgcn_readlane(there(page) ? page : 0, wave);
+            const int tok = min(k0 + 16 * wave, lk - 1);
+            const int64_t at = (a.c.first_token(p, (int)kv_head) + (tok & page_mask)) * T::kRow;
+            kb = reinterpret_cast<const char*>(a.c.k) + at;
+            vb = reinterpret_cast<const char*>(a.c.v) + at;
+            first = tok;
+        }
+#pragma unroll
+        for (int j = 0; j < T::kCopies; ++j) {
+            const int r = copy_row + j * T::kRows, base = SOURCE == kRows ? 0 : 16 * wave;
+            // (rows past the last are copies of it; they are masked)
+            const uint32_t from = (uint32_t)min(r - base, lk - 1 - first);
+            const uint32_t to = parity * T::kBytes + (uint32_t)(T::kCopies * wave + j) * 1024u;
+            copy_to_lds(to, kb, from * k_step + 16u * (uint32_t)(copy_piece ^ T::swizzle_k(r)));
+            copy_to_lds(to + 2 * T::kBytes, vb, from * v_step + 16u * (uint32_t)(copy_piece ^ T::swizzle_v(r)));
+        }
+    };
+    // which of this wavefront's 16 rows of a tile of v are not finite
+    auto look_at_v = [&](uint32_t parity) {
+        constexpr uint32_t kExp = F16 ? 0x7C007C00u : 0x7F807F80u, kOne = F16 ? 0x04000400u : 0x00800080u;
+        uint32_t bad = 0u;
+#pragma unroll
+        for (int j = 0; j < T::kCopies; ++j) {
+            const u32x4 v = *(lds_u4)((2 + parity) * T::kBytes + (uint32_t)(T::kCopies * wave + j) * 1024u + 16u * (uint32_t)lane);
+            uint32_t bits = 0u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bits |= (v[i] & kExp) + kOne;               // (an exponent of all ones carries into the half's top bit)
+            const unsigned long long lanes = __builtin_amdgcn_ballot_w64((bits & 0x80008000u) != 0u);
+            if (lanes) {
+#pragma unroll
+                for (int r = 0; r < T::kRows; ++r)
+                    bad |= ((lanes >> (r * T::kPieces)) & ((1ull << T::kPieces) - 1) ? 1u : 0u) << (j * T::kRows + r);
+            }
+        }
+        if (lane == 0) *(lds_u1)(kAside + parity * kAsideBytes + 4u * (uint32_t)wave) = bad;
+    };
+    // Such rows are taken out of the tile, when all wavefronts have had what they need of them.
+    auto take_out = [&](uint32_t parity, unsigned long long bad) {
+        lds_barrier();
+#pragma unroll
+        for (int j = 0; j < T::kCopies; ++j)
+            if ((bad >> (copy_row + j * T::kRows)) & 1ull)
+                *(lds_u4)((2 + parity) * T::kBytes + (uint32_t)(T::kCopies * wave + j) * 1024u + 16u * (uint32_t)lane) = u32x4{0u, 0u, 0u, 0u};
+        lds_barrier();
+    };
+    // tokens of a tile whose v is not finite (codes: whose scale or offset is not), where the tile was looked at
+    auto bad_of = [&](uint32_t parity) -> unsigned long long {
+        unsigned long long bad = 0ull;
+        if constexpr (CODES) {
+            const u32x2 two = *(lds_u2)(kAside + parity * kAsideBytes + 1032);
+            bad = (unsigned long long)two[1] << 32 | two[0];
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) bad |= (unsigned long long)*(lds_u1)(kAside + parity * kAsideBytes + 4u * (uint32_t)i) << (16 * i);
+        }
+        return (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)bad) | (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(bad >> 32)) << 32;
+    };
+
+    // Codes: a thread's part of a tile, loaded two tiles ahead and widened into LDS one tile ahead.
+    constexpr int kPart = CODES ? kKeys * D * SOURCE / 8 / kThreads : 16, kLoad = kPart < 16 ? kPart : 16, kPasses = kPart / kLoad;
+    constexpr int kLanesRow = CODES ? D * SOURCE / 8 / kLoad : 1, kPassRows = kThreads / kLanesRow, kCodes = CODES ? kLoad * 8 / SOURCE : 8;
+    struct Raw {
+        uint32_t k[kPasses][kLoad / 4], v[kPasses][kLoad / 4];
+        u32x2 scales;
+    };
+    Raw raw;
+    auto load_raw = [&](int t, int page) {
+        if constexpr (CODES) {
+            const int k0 = span.real(t) * kKeys, pages = there(page) ? page : 0;
+#pragma unroll
+            for (int i = 0; i < kPasses; ++i) {
+                const int r = i * kPassRows + (int)threadIdx.x / kLanesRow, first = i * kPassRows + 64 / kLanesRow * wave;
+                const int64_t at = a.c.first_token(__builtin_amdgcn_readlane(pages, first / 16), (int)kv_head) * (D * SOURCE / 8);
+                const uint32_t off = (uint32_t)(min(k0 + r, lk - 1) & page_mask) * (D * SOURCE / 8) + (uint32_t)(threadIdx.x % kLanesRow) * kLoad;
+                load_bytes(a.c.k + at + off, raw.k[i]);
+                load_bytes(a.c.v + at + off, raw.v[i]);
+            }
+            if (wave == (t & (kWaves - 1))) {
+                const int64_t at = a.c.first_token(__shfl(pages, lane >> 4), (int)kv_head) + (min(k0 + lane, lk - 1) & page_mask);
+                raw.scales = *reinterpret_cast<const u32x2*>(a.c.scales + 4 * at);
+            }
+        }
+    };
+    auto stage = [&](int t, uint32_t parity) {
+        if constexpr (CODES) {
+#pragma unroll
+            for (int i = 0; i < kPasses; ++i) {
+                const int r = i * kPassRows + (int)threadIdx.x / kLanesRow;
+                uint32_t wide[kCodes / 2];
+#pragma unroll
+                for (int of_v = 0; of_v < 2; ++of_v) {
+#pragma unroll
+                    for (int x = 0; x < kLoad / 4; ++x) {
+                        if (of_v) widen<CODES ? SOURCE : 8, true>(raw.v[i][x], wide + x * 16 / (CODES ? SOURCE : 8));
+                        else widen<CODES ? SOURCE : 8, false>(raw.k[i][x], wide + x * 16 / (CODES ? SOURCE : 8));
+                    }
+#pragma unroll
+                    for (int x = 0; x < kCodes / 8; ++x) {
+                        const int piece = (int)(threadIdx.x % kLanesRow) * (kCodes / 8) + x;
+                        const uint32_t to = (uint32_t)(r * T::kRow) + 16u * (uint32_t)(piece ^ (of_v ? T::swizzle_v(r) : T::swizzle_k(r)));
+                        *(lds_u4)((2 * of_v + parity) * T::kBytes + to) = u32x4{wide[4 * x], wide[4 * x + 1], wide[4 * x + 2], wide[4 * x + 3]};
+                    }
+                }
+            }
+            if (wave == (t & (kWaves - 1))) {
+                using C = Codes<CODES ? SOURCE : 8>;
+                const float ks = bf16lo_to_f32(raw.scales[0]), ko = bf16hi_to_f32(raw.scales[0]), vs = bf16lo_to_f32(raw.scales[1]), vo = bf16hi_to_f32(raw.scales[1]);
+                const float mid = fmaf(C::kCentre, vs, vo);
+                const bool fine = fabsf(mid) < __builtin_inff();   // (a v without numbers counts for nothing here; see below)
+                const uint32_t aside = kAside + parity * kAsideBytes, to = aside + 4u * (uint32_t)lane;
+                *(lds_f)(to) = ks;
+                *(lds_f)(to + 256) = fmaf(-C::kBias, ks, ko);
+                *(lds_f)(to + 512) = fine ? vs : 0.0f;
+                *(lds_f)(to + 768) = fine ? mid : 0.0f;
+                float big = lanes_reduce<16>(fine ? fabsf(vs) : 0.0f, [](float u, float v) { return fmaxf(u, v); });
+                big = fmaxf(big, __shfl_xor(big, 16));
+                big = fmaxf(big, __shfl_xor(big, 32));
+                const unsigned long long bad = __builtin_amdgcn_ballot_w64(!fine);
+                if (lane == 0) {
+                    *(lds_f)(aside + 1024) = big;
+                    *(lds_u2)(aside + 1032) = u32x2{(uint32_t)bad, (uint32_t)(bad >> 32)};
+                }
+            }
+        }
+    };
+
+    // operand addresses within a tile: the swizzles are exclusive ors, so that pieces further along the head are the first one's with two or four
+    // times 16 bytes put in the same way
+    const int i16 = lane & 15, v_row = 4 * g + (i16 >> 2);
+    const uint32_t k_lane = (uint32_t)(n * T::kRow + ((g ^ T::swizzle_k(n)) << 4));
+    const uint32_t v_lane = (uint32_t)(v_row * T::kRow + 8 * (i16 & 1) + (((2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1)) ^ T::swizzle_v(v_row)) << 4));
+    auto v_operand = [&](uint32_t buf, int c, int m) -> u32x4 {
+        const uint32_t at = ((v_lane + buf + 2 * T::kBytes) ^ (uint32_t)(m << 6)) + (uint32_t)(c * 16 * T::kRow);
+        const u32x2 lo = lds_read_transposed(at), hi = lds_read_transposed(at + 8 * T::kRow);
+        return u32x4{lo[0], lo[1], hi[0], hi[1]};
+    };
+    // four tokens' of an array of scales: keys 32 u + 8 c + 4 g ..
+    auto four_of = [&](uint32_t parity, int array, int u, int c) -> f32x4 {
+        return *(lds_f4)(kAside + parity * kAsideBytes + (uint32_t)(256 * array + 4 * (32 * u + 8 * c)) + 16u * (uint32_t)g);
+    };
+
+    float m_ref = -__builtin_inff(), l = 0.0f, v_sum = 0.0f;
+    int exponent = -100;                                        // of the largest vs seen; it is part of m_sub
+    f32x16 o[OM];
+#pragma unroll
+    for (int m = 0; m < OM; ++m)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[m][r] = 0.0f;
+
+    // One tile; `whole`: all rows see all of its keys.
+    auto tile_of = [&](int t, uint32_t parity, unsigned valid, bool whole) {
+        const uint32_t buf = parity * T::kBytes;
+        const int k0 = span.real(t) * kKeys;
+        f32x16 s[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[u][r] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < QM; ++i) {
+                const u32x4 k = *(lds_u4)(((k_lane + buf) ^ (uint32_t)(i << 5)) + (uint32_t)(u * 32 * T::kRow));
+                s[u] = mma32<MMA16>(k, q[i], s[u]);
+            }
+            if (CODES) __builtin_amdgcn_sched_barrier(0);       // (or operands of all products are fetched at once, into registers that are not there)
+        }
+        if constexpr (CODES) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const f32x4 ks = four_of(parity, 0, u, c), ko = four_of(parity, 1, u, c);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[u][4 * c + r] = fmaf(ks[r], s[u][4 * c + r], ko[r] * sum_q);
+                    if (c & 1) __builtin_amdgcn_sched_barrier(0);
+                }
+        }
+        // (places relative to the tile's first key of this half, which may be those of no page)
+        const int base = k0 + 4 * g, lim_at = lim - base, lo_at = (max(lim, 0) + 1 - base) - a.window, sinks_at = a.sinks - base;
+        auto sees = [&](int u, int r) -> bool {
+            const int key = 32 * u + 8 * (r >> 2) + (r & 3), last = !PAGED || ((valid >> (2 * u + (r >> 3))) & 1u) ? lim_at : -0x7FFFFFFF;
+            return (bool)((int)(key <= last) & ((int)(key >= lo_at) | (int)(key < sinks_at)));
+        };
+        if (!whole) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[u][r] = sees(u, r) ? s[u][r] : -__builtin_inff();
+        }
+
+        // The maximum in use is raised only when a score exceeds it by 2^kSlack, which spares nearly all rescaling of o.
+        float top = s[0][0];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
+        top = fmaxf(top, other_half(top)) * scale;
+        bool moved = top > m_ref + kSlack;
+        int higher = exponent;
+        if constexpr (CODES) {
+            float big = *(lds_f)(kAside + parity * kAsideBytes + 1024);
+            if (!whole) {
+                big = 0.0f;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const f32x4 vs = four_of(parity, 2, u, c);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) big = sees(u, 4 * c + r) ? fmaxf(big, fabsf(vs[r])) : big;
+                    }
+                big = fmaxf(big, other_half(big));
+            }
+            higher = max(exponent, min((int)(__float_as_uint(big) >> 23) - 127, 127));
+            moved |= higher > exponent;
+        }
+        // A weight's exponent is scale s - m_sub: a product that is not rounded, less a maximum that is.  Beyond 2^31 that rounding alone would leave
+        // the exponents' range: where some row's maximum lies beyond kFar, the scores are replaced by their distance from it, both rounded alike.
+        auto m_used = [&](float m, int e) -> float { return (m == -__builtin_inff() ? 0.0f : m) + (CODES ? (float)min(e, kFold) : 0.0f); };
+        if (__builtin_amdgcn_ballot_w64(moved)) {
+            const float m_new = moved ? fmaxf(m_ref, top) : m_ref;
+            const float alpha = exp2_fast(m_new > m_ref ? m_ref - m_new : 0.0f);
+            const float less = CODES ? __builtin_ldexpf(1.0f, max(min(exponent, kFold) - min(higher, kFold), -140)) : 1.0f;
+            const float fold = CODES ? __builtin_ldexpf(1.0f, max(max(exponent - kFold, 0) - max(higher - kFold, 0), -140)) : 1.0f;
+            m_ref = m_new;
+            exponent = higher;
+            l *= alpha * less;
+            v_sum *= alpha * less;
+            const float f = alpha * less * fold;
+#pragma unroll
+            for (int m = 0; m < OM; ++m) o[m] *= f;
+        }
+        float m_sub = m_used(m_ref, exponent);
+        if (__builtin_amdgcn_ballot_w64(fabsf(m_sub) > kFar)) {
+            const float back = 1.0f / scale;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+#pragma clang fp contract(off)
+                    const float scaled = s[u][r] * scale;
+                    s[u][r] = (scaled - m_sub) * back;
+                }
+            m_sub = 0.0f;
+        }
+
+        u32x4 p[4];
+        const bool folds = CODES && __builtin_amdgcn_ballot_w64(exponent > kFold) != 0ull;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                f32x4 e;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    e[r] = exp2_fast(fmaf(s[u][4 * c + r], scale, -m_sub));
+                    l += e[r];
+                }
+                if constexpr (CODES) {
+                    f32x4 vs = four_of(parity, 2, u, c), vo = four_of(parity, 3, u, c);
+                    if (folds) vs *= __builtin_ldexpf(1.0f, -max(exponent - kFold, 0));
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        v_sum = fmaf(e[r], vo[r], v_sum);
+                        e[r] *= vs[r];
+                    }
+                }
+                p[2 * u + (c >> 1)][2 * (c & 1)] = pack<MMA16>(e[0], e[1]);
+                p[2 * u + (c >> 1)][2 * (c & 1) + 1] = pack<MMA16>(e[2], e[3]);
+                if (CODES && (c & 1)) __builtin_amdgcn_sched_barrier(0);
+            }
+
+        // 0 times what is not finite would be NaN: tokens with such a v (in tiles that not all rows see, with codes in all) are added one by one to
+        // the rows that see them, and are zeros in the product.
+        if (CODES || !whole) {
+            const unsigned long long bad = bad_of(parity);
+            if (bad) {
+#pragma unroll 1
+                for (unsigned long long left = bad; left; left &= left - 1) {
+                    const int key = __builtin_ctzll(left), at = k0 + key;
+                    const bool seen = at <= lim && (at >= max(lim, 0) + 1 - a.window || at < a.sinks) && (!PAGED || ((valid >> (key >> 4)) & 1u));
+                    if constexpr (CODES) {
+                        if (seen) v_sum = __builtin_nanf("");
+                    } else {
+                        const int c = key >> 4, half = (key >> 2) & 1, slot = (key & 3) | ((key >> 1) & 4);
+                        uint32_t pair = 0u;
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) pair = x == 4 * c + (slot >> 1) ? p[x >> 2][x & 3] : pair;
+                        const float mine = slot & 1 ? h16hi_to_f32<MMA16>(pair) : h16lo_to_f32<MMA16>(pair), other = other_half(mine);
+                        const float weight = g == half ? mine : other;
+#pragma unroll
+                        for (int m = 0; m < OM; ++m)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const uint32_t piece = (uint32_t)((4 * m + r) ^ T::swizzle_v(key));
+                                const u32x2 v = *(lds_u2)(buf + 2u * T::kBytes + (uint32_t)(key * T::kRow) + 16u * piece + 8u * (uint32_t)g);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const float x = e & 1 ? h16hi_to_f32<F16>(v[e >> 1]) : h16lo_to_f32<F16>(v[e >> 1]);
+                                    o[m][4 * r + e] = seen ? fmaf(weight, x, o[m][4 * r + e]) : o[m][4 * r + e];
+                                }
+                            }
+                    }
+                }
+                if constexpr (!CODES) take_out(parity, bad);
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int m = 0; m < OM; ++m) o[m] = mma32<MMA16>(v_operand(buf, c, m), p[c], o[m]);
+    };
+
+    // `page` is that of the tile whose loads go out next: the next tile's, with codes the one behind it.
+    int page = 0;
+    unsigned valid = 15u, valid_next = 15u;                     // of tiles t and t + 1
+    if (t_first < t_end) {
+        page = pages_of(t_first);
+        valid = valid_of(page);
+        if constexpr (CODES) {
+            load_raw(t_first, page);
+            stage(t_first, t_first & 1);
+            if (t_first + 1 < t_end) {
+                page = pages_of(t_first + 1);
+                valid_next = valid_of(page);
+                load_raw(t_first + 1, page);
+                if (t_first + 2 < t_end) page = pages_of(t_first + 2);
+            }
+        } else {
+            copy_tile(t_first, page, t_first & 1);
+            if (t_first + 1 < t_end) page = pages_of(t_first + 1);
+        }
+    }
+#pragma unroll 1
+    for (int t = t_first; t < t_end; ++t) {
+        const uint32_t parity = (uint32_t)(t & 1);
+        const int k0 = span.real(t) * kKeys;
+        const bool whole = k0 + kKeys - 1 <= all_lim && (k0 >= all_lo || k0 + kKeys <= a.sinks) && valid == 15u;
+        if constexpr (!CODES) {
+            loads_left<0>();
+            if (!whole) look_at_v(parity);
+        }
+        lds_barrier();                                          // tile t is there, and nobody reads the one in front of it any more
+        unsigned valid_after = 15u;
+        if constexpr (CODES) {
+            if (t + 1 < t_end) stage(t + 1, parity ^ 1u);
+            if (t + 2 < t_end) {
+                valid_after = valid_of(page);
+                load_raw(t + 2, page);
+                if (t + 3 < t_end) page = pages_of(t + 3);
+            }
+        } else if (t + 1 < t_end) {
+            valid_next = valid_of(page);
+            copy_tile(t + 1, page, parity ^ 1u);
+            if (t + 2 < t_end) page = pages_of(t + 2);
+        }
+        if (active) {
+            tile_of(t, parity, valid, whole);
+        } else if (!CODES && !whole) {
+            if (const unsigned long long bad = bad_of(parity)) take_out(parity, bad);
+        }
+        valid = valid_next;
+        valid_next = valid_after;
+    }
+    if (!active) return;
+
+    // (the lane's number anew: what follows from it is not to take registers from the loop above)
+    int thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));
+    const int n_e = thread & 31, g_e = (thread >> 5) & 1;
+
+    l += other_half(l);
+    if constexpr (CODES) {
+        v_sum += other_half(v_sum);
+        const float unfold = __builtin_ldexpf(1.0f, max(exponent - kFold, 0));
+#pragma unroll
+        for (int m = 0; m < OM; ++m)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[m][r] = fmaf(o[m][r], unfold, v_sum);
+    }
+    if (w.pieces > 1) {
+        float* to = a.partial + (int64_t)w.slot * kPieceFloats<D>;
+        f32x4* sums = reinterpret_cast<f32x4*>(to) + wave * (4 * OM) * 64 + (thread & 63);
+#pragma unroll
+        for (int m = 0; m < OM; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sums[(4 * m + r) * 64] = f32x4{o[m][4 * r], o[m][4 * r + 1], o[m][4 * r + 2], o[m][4 * r + 3]};
+        if (g_e == 0) {
+            const float m = m_ref == -__builtin_inff() ? m_ref : m_ref + (CODES ? (float)min(exponent, kFold) : 0.0f);
+            reinterpret_cast<f32x2*>(to + kRowTile * D)[32 * wave + n_e] = f32x2{m, l};
+        }
+        return;
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;              // (no key seen: o is 0 as well)
+    if (row0 + n_e < rows) {
+        const int query_e = (int)((unsigned)(row0 + n_e) / (unsigned)a.shared), head = (int)kv_head * a.shared + (row0 + n_e - query_e * a.shared);
+        uint16_t* out = a.out + ((int64_t)(w.r.q_at + query_e) * a.heads + head) * D + 4 * g_e;
+#pragma unroll
+        for (int m = 0; m < OM; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                *reinterpret_cast<u32x2*>(out + 32 * m + 8 * r) =
+                    u32x2{pack<F16>(o[m][4 * r] * inv, o[m][4 * r + 1] * inv), pack<F16>(o[m][4 * r + 2] * inv, o[m][4 * r + 3] * inv)};
+    }
+}
+
+// Joins the pieces of tiles of rows that were cut: a wavefront has 32 rows and four values of each, in the pieces' own order of lanes.
+constexpr int kAtOnce = 16;                                     // pieces whose loads are out at a time
+template <int SOURCE, int D, bool F16>
+__global__ __launch_bounds__(256) void attn_chunk_join_kernel(Args a) {
+    const int lane = threadIdx.x & 63, n = lane & 31, g = lane >> 5;
+    const unsigned place = blockIdx.x / (unsigned)a.kv_heads, kv_head = blockIdx.x - place * (unsigned)a.kv_heads;
+    const Work w = work_of<SOURCE, true>(a, place, kv_head, lane);
+    if (w.request < 0) return;
+    const int rows = w.r.lq * a.shared, part = blockIdx.y % kWaves, row = w.tile * kRowTile + 32 * part + n;
+    const int four = 4 * (int)(blockIdx.y / kWaves) + (int)(threadIdx.x >> 6);
+    if (w.tile * kRowTile + 32 * part >= rows) return;
+    const Span span = span_of(a, w.r, w.tile);
+    const int each = (span.tiles + w.pieces - 1) / w.pieces, pieces = each > 0 ? min(w.pieces, (span.tiles + each - 1) / each) : 0;
+    const int64_t step = (int64_t)a.kv_heads * kPieceFloats<D>;
+    const float* first = a.partial + (int64_t)w.slot * kPieceFloats<D>;
+    const float* ml = first + kRowTile * D + 2 * (32 * part + n);
+    const float* sums = first + 4 * ((part * (D / 8) + four) * 64 + lane);
+    float top = -__builtin_inff(), sum = 0.0f;
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int p0 = 0; p0 < pieces; p0 += kAtOnce) {
+        f32x2 x[kAtOnce];
+        f32x4 y[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int64_t at = min(p0 + i, pieces - 1) * step;
+            x[i] = *reinterpret_cast<const f32x2*>(ml + at);
+            y[i] = *reinterpret_cast<const f32x4*>(sums + at);
+        }
+        float higher = top;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) higher = fmaxf(higher, x[i][0]);
+        const float use = higher == -__builtin_inff() ? 0.0f : higher, f = exp2_fast(top - use);
+        sum *= f;
+        v *= f;
+        top = higher;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const float e = p0 + i < pieces ? exp2_fast(x[i][0] - use) : 0.0f;
+            if (e != 0.0f) {
+                sum = fmaf(e, x[i][1], sum);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = fmaf(e, y[i][j], v[j]);
+            }
+        }
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    if (row < rows) {
+        const int query = (int)((unsigned)row / (unsigned)a.shared), head = (int)kv_head * a.shared + (row - query * a.shared);
+        uint16_t* out = a.out + ((int64_t)(w.r.q_at + query) * a.heads + head) * D + 8 * four + 4 * g;
+        *reinterpret_cast<u32x2*>(out) = u32x2{pack<F16>(v[0] * inv, v[1] * inv), pack<F16>(v[2] * inv, v[3] * inv)};
+    }
+}
+
+template <int SOURCE, int D, bool F16> hipError_t launch(Args a, const ChunkPlan& pl, hipStream_t stream) {
+    constexpr auto kernel = attn_chunk_kernel<SOURCE, D, F16>;
+    constexpr int bytes = 4 * Tile<D, kWaves>::kBytes + 2 * (SOURCE == 8 || SOURCE == 4 ? 4 * 256 + 16 : 16);
+    if (hipError_t e = ensure_lds<kernel>(bytes); e != hipSuccess) return e;
+    a.target = pl.target;
+    a.slots = pl.slots;
+    const hipError_t e = launch_blocks(pl.blocks, kThreads, hipSuccess, [&](int64_t first, int64_t count) {
+        a.first_block = (unsigned)first;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(kThreads), bytes, stream, a);
+        return hipGetLastError();
+    });
+    if (e != hipSuccess || pl.target == 0) return e;
+    hipLaunchKernelGGL((attn_chunk_join_kernel<SOURCE, D, F16>), dim3((unsigned)pl.cut_tiles, (unsigned)(kWaves * D / 32)), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+ChunkPlan plan_attn_chunk(int64_t requests, int64_t q_tokens, int heads, int kv_heads, int head_dim, int64_t max_tokens, int cus) {
+    ChunkPlan p{};
+    const int64_t shared = heads / kv_heads, some = requests < q_tokens ? requests : q_tokens;
+    const int64_t tiles = (q_tokens * shared / kRowTile + some) * kv_heads, units = (max_tokens + kKeys - 1) / kKeys;
+    p.blocks = tiles;
+    if (units <= kLeastPiece) return p;
+    p.target = 2 * cus;
+    // A request is cut where its tiles of rows have more tiles of keys than a piece; a piece has so many that all pieces would be `target`, so that
+    // there are fewer than twice as many of the cut ones; and no more than the longest requests' own.
+    const int64_t most = 2 * (int64_t)p.target + kv_heads, own = tiles * ((units + kLeastPiece - 1) / kLeastPiece);
+    p.slots = (int)(own < most ? own : most);
+    p.cut_tiles = (int)(tiles < p.target + kv_heads ? tiles : p.target + kv_heads);
+    p.blocks = tiles + p.slots;
+    p.workspace = (size_t)p.slots * kRowTile * (head_dim + 2) * sizeof(float);
+    return p;
+}
+
+hipError_t launch_attn_chunk(const ChunkArgs& c, const any4_kv_cache* cache, const ChunkPlan& pl, void* workspace, hipStream_t stream) {
+    Args a{c.q, c.k, c.v, {}, c.table, c.table_stride, (int)c.table_width, c.q_starts, c.k_starts, c.lengths, (int)c.q_tokens, (int)c.k_tokens, c.requests,
+           c.heads, c.kv_heads, c.heads / c.kv_heads, c.window > 0 ? c.window : kNoWindow, c.sinks, 0, 0, 0u, c.softmax_scale * kLog2e, c.out,
+           static_cast<float*>(workspace)};
+    if (cache) a.c = kv_pages(*cache);
+    auto types = [&](auto source, auto dim) {
+        return c.f16 ? launch<decltype(source)::value, decltype(dim)::value, true>(a, pl, stream)
+                     : launch<decltype(source)::value, decltype(dim)::value, false>(a, pl, stream);
+    };
+    auto dims = [&](auto source) {
+        return c.head_dim == 128 ? types(source, std::integral_constant<int, 128>{}) : types(source, std::integral_constant<int, 64>{});
+    };
+    if (!cache) return dims(std::integral_constant<int, kRows>{});
+    return cache->bits == 16 ? dims(std::integral_constant<int, 16>{}) : cache->bits == 8 ? dims(std::integral_constant<int, 8>{})
+                                                                        : dims(std::integral_constant<int, 4>{});
+}
+
+}  // namespace any4

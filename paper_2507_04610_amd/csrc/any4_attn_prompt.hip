@@ -31,6 +31,7 @@
 //
 // Rounding: scores, maxima, sums and accumulators are fp32; the weights are rounded to 16 bits for the matrix cores, once.
 #include "any4_attn.h"
+#include "any4_attn_tile.h"
 #include "any4_internal.h"
 #include "any4_launches.h"
 #include "any4_lds_copy.h"
@@ -39,15 +40,7 @@ namespace any4 {
 
 namespace {
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves, kKeys = 64;
-constexpr float kSlack = 8.0f;
-constexpr float kFar = 1048576.0f;        // 2^20: up to there a maximum's rounding moves the exponents by 2^-4 at most, for all keys of a query alike
-
-#pragma clang diagnostic ignored "-Wint-to-pointer-cast"          // LDS offsets as pointers
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) u32x4* lds_u4;
-typedef __attribute__((address_space(3))) u32x2* lds_u2;
-typedef __attribute__((address_space(3))) s16x4* lds_s4;
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
 
 struct Args {
     Rows q, k, v;
@@ -59,22 +52,9 @@ struct Args {
     uint16_t* out;
 };
 
-// 4 rows x 16 columns: lane i of 16 gives the address of row i / 4, columns 4 * (i % 4) .., and gets column i of the four rows
-__device__ __forceinline__ u32x2 lds_read_transposed(uint32_t at) {
-    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at)));
-}
-
-// the part of a tile that a wavefront copies: 16-byte pieces, 64 an instruction
-template <int D> struct Tile {
-    static constexpr int kRow = 2 * D, kBytes = kKeys * kRow, kPieces = D / 8, kRows = 64 / kPieces;     // rows an instruction
-    static constexpr int kCopies = kKeys / kRows / kWaves;                                                // of a wavefront
-    __device__ static __forceinline__ int swizzle_k(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
-    __device__ static __forceinline__ int swizzle_v(int row) { return D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; }
-};
-
 template <int D, bool F16>
 __global__ __launch_bounds__(kThreads, 2) void attn_prompt_kernel(Args a) {
-    using T = Tile<D>;
+    using T = Tile<D, kWaves>;
     constexpr int QM = D / 16, OM = D / 32, ROWS = 32 * kWaves;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, g = lane >> 5;
@@ -368,7 +348,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_prompt_kernel(Args a) {
 
 template <int D, bool F16> hipError_t launch(Args a, int64_t blocks, hipStream_t stream) {
     constexpr auto kernel = attn_prompt_kernel<D, F16>;
-    constexpr int bytes = 4 * Tile<D>::kBytes;
+    constexpr int bytes = 4 * Tile<D, kWaves>::kBytes;
     if (hipError_t e = ensure_lds<kernel>(bytes); e != hipSuccess) return e;
     return launch_blocks(blocks, kThreads, hipSuccess, [&](int64_t first, int64_t count) {
         a.first_block = (unsigned)first;

@@ -244,6 +244,10 @@ PyMethodDef methods[] = {
      "attn_decode(q, cache_k, cache_v, page_table, lengths, scales, bits, softmax_scale, out, workspace)"},
     {"attn_decode_window", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attn_decode_window)), METH_FASTCALL,
      "attn_decode_window(q, cache_k, cache_v, page_table, lengths, scales, bits, softmax_scale, out, workspace, window, sinks)"},
+    {"attn_chunk", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attn_chunk)), METH_FASTCALL,
+     "attn_chunk(q, cache_k, cache_v, page_table, q_starts, lengths, scales, bits, window, sinks, softmax_scale, out, workspace)"},
+    {"attn_prompt_window", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attn_prompt_window)), METH_FASTCALL,
+     "attn_prompt_window(q, k, v, q_starts, k_starts, window, sinks, softmax_scale, out)"},
     {"rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(rope)), METH_FASTCALL,
      "rope(q, k, positions, freqs, q_norm, k_norm, eps, interleaved, axis_of, out_q, out_k)"},
     {"rope_kv_write", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(rope_kv_write)), METH_FASTCALL,

@@ -81,5 +81,7 @@ inline PyObject* answer(int rc, PyObject* given, at::Tensor&& made) {
 PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n);
 PyObject* rope_kv_write(PyObject*, PyObject* const* a, Py_ssize_t n);
 PyObject* attn_decode_window(PyObject*, PyObject* const* a, Py_ssize_t n);
+PyObject* attn_chunk(PyObject*, PyObject* const* a, Py_ssize_t n);
+PyObject* attn_prompt_window(PyObject*, PyObject* const* a, Py_ssize_t n);
 
 }  // namespace any4_torch

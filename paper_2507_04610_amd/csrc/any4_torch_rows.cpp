@@ -148,4 +148,84 @@ PyObject* attn_decode_window(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// attn_chunk(q, cache_k, cache_v, page_table, q_starts, lengths, scales, bits, window, sinks, softmax_scale, out, workspace)
+PyObject* attn_chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 13) Py_RETURN_NONE;
+    const at::Tensor *q = tensor(a[0]), *ck = tensor(a[1]), *cv = tensor(a[2]), *table = tensor(a[3]), *starts = tensor(a[4]), *lengths = tensor(a[5]), *scales, *out, *ws;
+    long bits, window, sinks;
+    float scale;
+    any4_kv_cache c;
+    if (!q || !ck || !cv || !table || !starts || !lengths || !optional_tensor(a[6], scales) || !whole(a[7], bits) || !optional_tensor(a[11], out) ||
+        !optional_tensor(a[12], ws) || !whole(a[8], window) || !whole(a[9], sinks) || q->dim() != 3)
+        Py_RETURN_NONE;
+    const at::ScalarType ty = q->scalar_type();
+    const int64_t tokens = q->size(0), heads = q->size(1);
+    if (!kv_cache(*ck, *cv, scales, bits, ty, c) || !rows(*q, ty, tokens, heads, c.head_dim, *ck) || !scale_of(a[10], c.head_dim, scale)) Py_RETURN_NONE;
+    if (heads < 1 || heads > 0xFFFF || c.kv_heads < 1 || heads % c.kv_heads) Py_RETURN_NONE;
+    if (!list(*lengths, at::kInt, *ck) || !list(*starts, at::kInt, *ck) || starts->size(0) != lengths->size(0) + 1) Py_RETURN_NONE;
+    const int64_t requests = lengths->size(0);
+    if (!table->is_cuda() || table->scalar_type() != at::kInt || table->layout() != at::kStrided || table->dim() != 2 || table->size(0) != requests ||
+        table->stride(1) != 1 || table->device() != ck->device())
+        Py_RETURN_NONE;
+    if (out && !(plain(*out, ty) && rows(*out, ty, tokens, heads, c.head_dim, *ck))) Py_RETURN_NONE;
+    if (ws && !(ws->layout() == at::kStrided && ws->device() == ck->device() && ws->is_non_overlapping_and_dense())) Py_RETURN_NONE;
+    const int64_t width = table->size(1), table_stride = table->stride(0);
+    c10::OptionalDeviceGuard guard;
+    void* const stream = stream_on(ck->device(), guard);
+    at::Tensor o = out ? *out : at::empty({tokens, heads, c.head_dim}, q->options().requires_grad(false));
+    at::Tensor scratch;
+    void* wp = nullptr;
+    size_t wbytes = 0;
+    if (ws) {
+        wp = ws->data_ptr();
+        wbytes = (size_t)ws->numel() * ws->element_size();
+    } else if (const size_t need = any4_attn_chunk_workspace_bytes(requests, tokens, (int)heads, c.kv_heads, c.head_dim, width * c.page_size)) {
+        scratch = at::empty({(int64_t)need}, q->options().dtype(at::kByte).requires_grad(false));
+        wp = scratch.data_ptr();
+        wbytes = need;
+    }
+    const Rows qr(*q);
+    const int32_t *pt = static_cast<const int32_t*>(table->data_ptr()), *ps = static_cast<const int32_t*>(starts->data_ptr()), *pl = static_cast<const int32_t*>(lengths->data_ptr());
+    uint16_t* po = static_cast<uint16_t*>(o.data_ptr());
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = any4_attn_chunk(qr.p, qr.token, qr.head, &c, pt, table_stride, width, ps, pl, tokens, requests, (int)heads, window, sinks, scale, po, wp, wbytes, stream);
+    Py_END_ALLOW_THREADS
+    return answer(rc, a[11], std::move(o));
+    END_HANDLE_TH_ERRORS
+}
+
+// attn_prompt_window(q, k, v, q_starts, k_starts, window, sinks, softmax_scale, out)
+PyObject* attn_prompt_window(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 9) Py_RETURN_NONE;
+    const at::Tensor *q = tensor(a[0]), *k = tensor(a[1]), *v = tensor(a[2]), *qs = tensor(a[3]), *ks, *out;
+    float scale;
+    long window, sinks;
+    if (!q || !k || !v || !qs || !optional_tensor(a[4], ks) || !optional_tensor(a[8], out) || !whole(a[5], window) || !whole(a[6], sinks) || q->dim() != 3 || k->dim() != 3) Py_RETURN_NONE;
+    const at::ScalarType ty = q->scalar_type();
+    if (ty != at::kBFloat16 && ty != at::kHalf) Py_RETURN_NONE;
+    const int64_t nq = q->size(0), heads = q->size(1), dim = q->size(2), nk = k->size(0), kv_heads = k->size(1);
+    if (heads < 1 || heads > 0xFFFF || kv_heads < 1 || kv_heads > 0xFFFF || heads % kv_heads || dim > 0xFFFF) Py_RETURN_NONE;
+    if (!rows(*q, ty, nq, heads, dim, *q) || !rows(*k, ty, nk, kv_heads, dim, *q) || !rows(*v, ty, nk, kv_heads, dim, *q)) Py_RETURN_NONE;
+    if (!list(*qs, at::kInt, *q) || qs->size(0) < 1 || (ks && (!list(*ks, at::kInt, *q) || ks->size(0) != qs->size(0)))) Py_RETURN_NONE;
+    if ((!ks && nk != nq) || !scale_of(a[7], dim, scale)) Py_RETURN_NONE;
+    if (out && !(plain(*out, ty) && rows(*out, ty, nq, heads, dim, *q))) Py_RETURN_NONE;
+    c10::OptionalDeviceGuard guard;
+    void* const stream = stream_on(q->device(), guard);
+    at::Tensor o = out ? *out : at::empty({nq, heads, dim}, q->options().requires_grad(false));
+    const Rows qr(*q), kr(*k), vr(*v);
+    const int32_t *pqs = static_cast<const int32_t*>(qs->data_ptr()), *pks = static_cast<const int32_t*>((ks ? ks : qs)->data_ptr());
+    const int64_t requests = qs->size(0) - 1;
+    uint16_t* po = static_cast<uint16_t*>(o.data_ptr());
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = any4_attn_prompt_window(qr.p, qr.token, qr.head, kr.p, kr.token, kr.head, vr.p, vr.token, vr.head, nq, nk, pqs, pks, requests, (int)heads, (int)kv_heads,
+                          (int)dim, ty == at::kHalf, window, sinks, scale, po, stream);
+    Py_END_ALLOW_THREADS
+    return answer(rc, a[8], std::move(o));
+    END_HANDLE_TH_ERRORS
+}
+
 }  // namespace any4_torch

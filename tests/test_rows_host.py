@@ -71,6 +71,48 @@ def test_windows_are_refused(lib):  # noqa: F811
     assert decode(n=0) == 0
 
 
+def chunk(lib, q=A, qt=512, qh=128, c=None, table=A, stride=4, width=4, starts=A, lengths=A, tokens=5, n=1, heads=4, window=0, sinks=0, scale=0.1, out=A, ws=None, size=0):  # noqa: F811
+    return lib.any4_attn_chunk(q, qt, qh, c or cache(), table, stride, width, starts, lengths, tokens, n, heads, window, sinks, scale, out, ws, size, None)
+
+
+def test_chunk_refuses(lib):  # noqa: F811
+    assert chunk(lib, q=None) == chunk(lib, table=None) == chunk(lib, starts=None) == chunk(lib, lengths=None) == chunk(lib, out=None) == NULL
+    assert chunk(lib, n=-1) == chunk(lib, tokens=-1) == chunk(lib, tokens=1 << 31) == chunk(lib, heads=3) == chunk(lib, heads=0) == chunk(lib, heads=65538) == SHAPE
+    assert chunk(lib, window=-1) == chunk(lib, sinks=-1) == chunk(lib, width=0) == chunk(lib, width=1 << 28) == chunk(lib, stride=-1) == chunk(lib, qt=-8) == SHAPE
+    assert chunk(lib, scale=0.0) == chunk(lib, scale=NAN) == chunk(lib, scale=INF) == chunk(lib, scale=-1.0) == SHAPE
+    assert chunk(lib, tokens=1 << 30, heads=8) == SHAPE                                    # 2^32 rows of a KV head
+    assert chunk(lib, tokens=1 << 29, heads=4 * 512, c=cache(kv_heads=1024)) == SHAPE      # 2^33 blocks
+    assert chunk(lib, q=A + 8) == chunk(lib, table=A + 2) == chunk(lib, starts=A + 1) == chunk(lib, lengths=A + 2) == chunk(lib, out=A + 8) == chunk(lib, qt=516) == ALIGN
+    assert chunk(lib, n=0) == chunk(lib, tokens=0) == 0 and chunk(lib, n=0, q=None) == 0
+    need = lib.any4_attn_chunk_workspace_bytes(1, 5, 4, 2, 128, 64 * 16)
+    assert need > 0 and chunk(lib, width=64) == WORKSPACE == chunk(lib, width=64, ws=A, size=need - 1) and chunk(lib, width=64, ws=A + 8, size=need) == ALIGN
+
+
+@pytest.mark.parametrize("change,code", BAD_CACHES)
+def test_chunk_refuses_bad_caches(lib, change, code):  # noqa: F811
+    assert chunk(lib, c=cache(**change)) == code
+
+
+def test_chunk_workspace(lib):  # noqa: F811
+    def need(requests=3, tokens=40, heads=32, kv_heads=8, dim=128, longest=4096):
+        return lib.any4_attn_chunk_workspace_bytes(requests, tokens, heads, kv_heads, dim, longest)
+    assert need(longest=256) == 0 < need(longest=257)                                       # nothing to cut in four tiles of keys
+    assert need(requests=0) == need(tokens=0) == need(heads=30) == need(dim=96) == need(longest=0) == need(longest=1 << 31) == need(tokens=1 << 30) == 0
+    # room for the pieces that a call can have, however it grows
+    assert need(longest=1 << 20) <= need(tokens=1 << 20, longest=1 << 20) == need(tokens=1 << 22, longest=1 << 22) < 160 << 20
+    assert need(dim=64) < need()
+
+
+def test_prompt_window_refuses(lib):  # noqa: F811
+    def prompt(q=A, qt=512, qh=128, k=A, kt=256, kh=128, v=A, vt=256, vh=128, nq=5, nk=7, qs=A, ks=A, n=1, heads=4, kv=2, dim=128, window=4, sinks=0, scale=0.1, out=A):
+        return lib.any4_attn_prompt_window(q, qt, qh, k, kt, kh, v, vt, vh, nq, nk, qs, ks, n, heads, kv, dim, 0, window, sinks, scale, out, None)
+    assert prompt(q=None) == prompt(k=None) == prompt(v=None) == prompt(qs=None) == prompt(ks=None) == prompt(out=None) == NULL
+    assert prompt(window=0) == prompt(window=-1) == prompt(sinks=-1) == prompt(n=-1) == prompt(nq=-1) == prompt(nk=1 << 31) == prompt(heads=3) == prompt(dim=96) == SHAPE
+    assert prompt(scale=0.0) == prompt(kt=1 << 23) == prompt(vt=1 << 23) == prompt(vh=-8) == prompt(nq=1 << 30, heads=8) == SHAPE
+    assert prompt(q=A + 8) == prompt(k=A + 2) == prompt(qs=A + 2) == prompt(vh=4) == prompt(out=A + 4) == ALIGN
+    assert prompt(n=0) == prompt(nq=0) == 0
+
+
 def test_the_binding_names_the_mistake():
     q, k, where, freqs = torch.zeros(3, 4, 128, dtype=torch.bfloat16), torch.zeros(3, 2, 128, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int64), torch.ones(64, dtype=torch.float64)
     with pytest.raises(any4.Any4Error, match="device memory"):
@@ -117,8 +159,11 @@ def test_calls_run_where_the_tensors_lie(calls):  # noqa: F811
     q, k, i64 = there(3, 4, 128), there(3, 2, 128), there(3, dtype=torch.int64)
     any4.any4_rope_kv_write(q, k, k, there(3, 3, dtype=torch.int64), there(64, dtype=torch.float64), i64, ck, cv, axis_of=there(64, dtype=torch.uint8))
     any4.any4_attn_decode(q, ck, cv, table, i32, window=7, sinks=2)
+    any4.any4_attn_chunk(q, ck, cv, table, there(4, dtype=torch.int32), i32)
+    any4.any4_attn_prompt(q, k, k, i32, window=7)
     names = [name for name, _, _ in calls]
-    assert names == ["any4_rope", "any4_rope", "any4_rope_kv_write", "any4_attn_decode_workspace_bytes", "any4_attn_decode_window"]
+    assert names == ["any4_rope", "any4_rope", "any4_rope_kv_write", "any4_attn_decode_workspace_bytes", "any4_attn_decode_window",
+                     "any4_attn_chunk_workspace_bytes", "any4_attn_chunk", "any4_attn_prompt_window"]
     assert all(device == 1 and stream in (101, None) for _, device, stream in calls) and torch.cuda.current_device() == 0
 
 
@@ -126,7 +171,7 @@ def test_native_calls_switch_to_the_tensors_device_and_let_go_of_the_lock():
     with open(SOURCE) as f:
         text = f.read()
     bodies = re.findall(r"(?ms)^PyObject\* (\w+)\(PyObject\*, PyObject\* const\* a, Py_ssize_t n\) \{(.*?)^\}", text)
-    assert {"rope", "rope_kv_write", "attn_decode_window"} <= {name for name, _ in bodies}
+    assert {"rope", "rope_kv_write", "attn_decode_window", "attn_chunk", "attn_prompt_window"} == {name for name, _ in bodies}
     for name, body in bodies:
         switch = body.index("stream_on(")
         for later in ("at::empty(", "_workspace_bytes("):
@@ -142,4 +187,24 @@ def test_host_tensors_are_left_to_the_checked_calls():
     ck = torch.zeros(2, 2, 16, 128, dtype=torch.bfloat16)
     assert n.rope(q, k, i64, f, None, None, 1e-6, False, None, None, None) is None
     assert n.rope_kv_write(q, k, k, i64, f, i64, ck, ck, None, 16, None, None, 1e-6, False, None, None, None) is None
+    assert n.attn_chunk(q, ck, ck, i64[:, None].int(), torch.zeros(4).int(), i64.int(), None, 16, 0, 0, None, None, None) is None
+    assert n.attn_prompt_window(q, k, k, i64.int(), None, 4, 0, None, None) is None
     assert n.attn_decode_window(q, ck, ck, i64[:, None].int(), i64.int(), None, 16, None, None, None, 5, 0) is None
+
+
+BAD_CHUNKS = [("3 dimensions", dict(q=there(3, 128))), ("multiple", dict(q=there(3, 3, 128))), ("lengths", dict(lengths=there(2, dtype=torch.int64))),
+              ("lengths", dict(lengths=there(2, 1, dtype=torch.int32))), ("q_starts", dict(q_starts=there(2, dtype=torch.int32))), ("q_starts", dict(q_starts=there(3, dtype=torch.int64))),
+              ("page_table", dict(page_table=there(2, 2))), ("page_table", dict(page_table=there(3, 2, dtype=torch.int32))), ("out", dict(out=there(3, 4, 64))),
+              ("cache_v", dict(cache_v=there(4, 2, 16, 64))), ("bits", dict(bits=5)), ("scales", dict(bits=8, cache_k=there(4, 2, 16, 128, dtype=torch.uint8), cache_v=there(4, 2, 16, 128, dtype=torch.uint8),
+                                                                                                     scales=there(4, 2, 16, 2))),
+              ("workspace", dict(workspace=torch.zeros(8))), ("sinks", dict(sinks=4)), ("window", dict(window=0))]
+
+
+@pytest.mark.parametrize("words,change", BAD_CHUNKS)
+def test_bad_chunks_are_refused(calls, words, change):  # noqa: F811
+    a = dict(q=there(3, 4, 128), cache_k=there(4, 2, 16, 128), cache_v=there(4, 2, 16, 128), page_table=there(2, 2, dtype=torch.int32), q_starts=there(3, dtype=torch.int32),
+             lengths=there(2, dtype=torch.int32))
+    a.update(change)
+    with pytest.raises(any4.Any4Error, match=words):
+        any4.any4_attn_chunk(**a)
+    assert not [name for name, _, _ in calls if "bytes" not in name]
