@@ -31,9 +31,12 @@ namespace any4 {
 namespace {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kRowTile = 32 * kWaves;
+constexpr int kNarrow = 4;                                      // tiles of keys for up to 32 rows that take as long as one for 128
 constexpr int kLeastPiece = 4;                                  // key tiles of a piece: a join costs as much as a few of them
 constexpr int kNoWindow = 0x7FFFF800;                           // more than any request's tokens
-constexpr int kFold = 60;                                       // exponents of vs_j beyond this one are taken off p_j vs_j apart from the maximum
+// The exponent of the largest vs_j goes with the maximum as far as 2^+-kFold: beyond, weights of tokens whose scales differ by 2^126 and more would
+// be lost, to each other and to the sum of weights.  The rest is taken off vs_j itself.
+constexpr int kFold = 40;
 typedef __attribute__((address_space(3))) float* lds_f;
 typedef __attribute__((address_space(3))) f32x4* lds_f4;
 typedef __attribute__((address_space(3))) uint32_t* lds_u1;
@@ -77,7 +80,7 @@ template <int SOURCE> __device__ __forceinline__ Request request_of(const Args& 
 // The tiles of keys that a tile of rows sees: the first `front`, then from the one in which the window begins, `gap` tiles further on.
 struct Span {
     int first, last;                   // first and last query
-    int front, gap, tiles;
+    int front, gap, tiles, end;        // end: of the keys that the last query sees
     __device__ __forceinline__ int real(int t) const { return t < front ? t : t + gap; }
 };
 __device__ __forceinline__ Span span_of(const Args& a, const Request& r, int tile) {
@@ -85,7 +88,7 @@ __device__ __forceinline__ Span span_of(const Args& a, const Request& r, int til
     const int rows = r.lq * a.shared, ahead = r.lk - r.lq;
     s.first = (int)((unsigned)(tile * kRowTile) / (unsigned)a.shared);
     s.last = (int)((unsigned)(min(tile * kRowTile + kRowTile, rows) - 1) / (unsigned)a.shared);
-    const int end = max(ahead + s.last + 1, 0), start = max(max(ahead + s.first, 0) + 1 - a.window, 0);
+    const int end = s.end = max(ahead + s.last + 1, 0), start = max(max(ahead + s.first, 0) + 1 - a.window, 0);
     const int begin = start / kKeys;
     s.front = min((int)(((unsigned)min(a.sinks, end) + kKeys - 1) / kKeys), begin);
     s.gap = begin - s.front;
@@ -102,13 +105,18 @@ struct Shares {                        // of 64 requests, a lane each
     Request r;
     int tiles, pieces;
 };
+// what the last (and longest) of its tiles of rows costs, in tiles of keys for 128 rows
+__device__ __forceinline__ int costs_of(const Args& a, const Shares& s) {
+    const int tiles = span_of(a, s.r, s.tiles - 1).tiles;
+    return s.r.lq * a.shared <= 32 ? (tiles + kNarrow - 1) / kNarrow : tiles;
+}
 template <int SOURCE> __device__ __forceinline__ Shares shares_of(const Args& a, int r0, int least, int lane) {
     Shares s{};
     s.pieces = 1;
     if (r0 + lane < a.requests) {
         s.r = request_of<SOURCE>(a, r0 + lane);
         s.tiles = (int)(((unsigned)(s.r.lq * a.shared) + kRowTile - 1) / kRowTile);
-        if (s.tiles > 0 && least > 0) s.pieces = max((span_of(a, s.r, s.tiles - 1).tiles + least - 1) / least, 1);
+        if (s.tiles > 0 && least > 0) s.pieces = max((costs_of(a, s) + least - 1) / least, 1);
     }
     return s;
 }
@@ -119,7 +127,7 @@ template <int SOURCE> __device__ __forceinline__ int piece_tiles(const Args& a, 
     for (int r0 = 0; r0 < a.requests; r0 += 64) {
         const Shares s = shares_of<SOURCE>(a, r0, 0, lane);
         float mine = 0.0f;
-        if (s.tiles > 0) mine = (float)s.tiles * (float)span_of(a, s.r, s.tiles - 1).tiles;
+        if (s.tiles > 0) mine = (float)s.tiles * (float)costs_of(a, s);
         all += wave_sum(mine);
     }
     return __builtin_amdgcn_readfirstlane(max((int)fminf(ceilf(all * (float)a.kv_heads / (float)a.target), 1073741824.0f), kLeastPiece));
@@ -160,8 +168,15 @@ template <int SOURCE, bool JOIN> __device__ __forceinline__ Work work_of(const A
     return w;
 }
 
+// LDS aside from the tiles.  Scales of TOKENS tokens: k's scale and offset, v's likewise, the largest of the third, whose v's are not finite.
+template <int TOKENS> constexpr int kScaleBytes = 16 * TOKENS + 16;
+template <bool CODES> constexpr int kAsideAll = CODES ? kWaves * kScaleBytes<32> : kWaves * 32 * 8;
+
 // floats of a piece: sums [wavefront][4 values of a row][lane][4], then [row] maximum and sum of weights
 template <int D> constexpr int kPieceFloats = kRowTile * (D + 2);
+
+__device__ __forceinline__ int with_maximum(int e) { return min(max(e, -kFold), kFold); }
+__device__ __forceinline__ int folded(int e) { return e - with_maximum(e); }
 
 template <int BITS> struct Codes {
     static constexpr float kBias = BITS == 8 ? 1024.0f : 64.0f, kCentre = (float)(1 << (BITS - 1));
@@ -233,7 +248,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     constexpr bool CODES = SOURCE == 8 || SOURCE == 4, PAGED = SOURCE != kRows, MMA16 = F16 || CODES;
     constexpr int QM = D / 16, OM = D / 32;
     // LDS: two tiles of k, two of v; per tile either rows of v that are not finite (16 bits a wavefront), or the tokens' scales, the largest, and whose are not finite
-    constexpr uint32_t kAside = 4 * T::kBytes, kAsideBytes = CODES ? 4 * 256 + 16 : 16;
+    constexpr uint32_t kAside = 4 * T::kBytes, kAsideBytes = CODES ? kScaleBytes<kKeys> : 16;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, g = lane >> 5;
 
@@ -247,7 +262,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     const int t_first = w.piece * each, t_end = min(span.tiles, t_first + each);
     if (w.pieces > 1 && t_first >= t_end) return;               // (the join knows)
 
-    const int row0 = w.tile * kRowTile + 32 * wave, row = min(row0 + n, rows - 1);
+    // Up to 32 rows: each wavefront takes all of them and every fourth 32 keys, otherwise 32 rows and all keys.
+    const bool narrow = rows - w.tile * kRowTile <= 32;
+    const int row0 = w.tile * kRowTile + (narrow ? 0 : 32 * wave), row = min(row0 + n, rows - 1);
     const bool active = row0 < rows;
     const int query = (int)((unsigned)row / (unsigned)a.shared);
     // this row sees keys up to `lim` that lie in its window or are among the first `sinks`
@@ -366,10 +383,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         lds_barrier();
     };
     // tokens of a tile whose v is not finite (codes: whose scale or offset is not), where the tile was looked at
-    auto bad_of = [&](uint32_t parity) -> unsigned long long {
+    auto bad_of_tile = [&](uint32_t parity) -> unsigned long long {
         unsigned long long bad = 0ull;
         if constexpr (CODES) {
-            const u32x2 two = *(lds_u2)(kAside + parity * kAsideBytes + 1032);
+            const u32x2 two = *(lds_u2)(kAside + parity * kAsideBytes + 16 * kKeys + 8);
             bad = (unsigned long long)two[1] << 32 | two[0];
         } else {
 #pragma unroll
@@ -403,11 +420,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
             }
         }
     };
+    // (the first row's first piece; the others' follow from it by an exclusive or and a constant)
+    const int stage_row = (int)threadIdx.x / kLanesRow, stage_piece = (int)(threadIdx.x % kLanesRow) * (kCodes / 8);
+    const uint32_t to_k = (uint32_t)(stage_row * T::kRow) + 16u * (uint32_t)(stage_piece ^ T::swizzle_k(stage_row));
+    const uint32_t to_v = 2 * T::kBytes + (uint32_t)(stage_row * T::kRow) + 16u * (uint32_t)(stage_piece ^ T::swizzle_v(stage_row));
     auto stage = [&](int t, uint32_t parity) {
         if constexpr (CODES) {
 #pragma unroll
             for (int i = 0; i < kPasses; ++i) {
-                const int r = i * kPassRows + (int)threadIdx.x / kLanesRow;
                 uint32_t wide[kCodes / 2];
 #pragma unroll
                 for (int of_v = 0; of_v < 2; ++of_v) {
@@ -418,9 +438,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                     }
 #pragma unroll
                     for (int x = 0; x < kCodes / 8; ++x) {
-                        const int piece = (int)(threadIdx.x % kLanesRow) * (kCodes / 8) + x;
-                        const uint32_t to = (uint32_t)(r * T::kRow) + 16u * (uint32_t)(piece ^ (of_v ? T::swizzle_v(r) : T::swizzle_k(r)));
-                        *(lds_u4)((2 * of_v + parity) * T::kBytes + to) = u32x4{wide[4 * x], wide[4 * x + 1], wide[4 * x + 2], wide[4 * x + 3]};
+                        const uint32_t other = 16u * (uint32_t)(x ^ (of_v ? T::swizzle_v(i * kPassRows) : T::swizzle_k(i * kPassRows)));
+                        *(lds_u4)((((of_v ? to_v : to_k) + parity * T::kBytes) ^ other) + (uint32_t)(i * kPassRows * T::kRow)) = u32x4{wide[4 * x], wide[4 * x + 1], wide[4 * x + 2], wide[4 * x + 3]};
                     }
                 }
             }
@@ -439,8 +458,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 big = fmaxf(big, __shfl_xor(big, 32));
                 const unsigned long long bad = __builtin_amdgcn_ballot_w64(!fine);
                 if (lane == 0) {
-                    *(lds_f)(aside + 1024) = big;
-                    *(lds_u2)(aside + 1032) = u32x2{(uint32_t)bad, (uint32_t)(bad >> 32)};
+                    *(lds_f)(aside + 16 * kKeys) = big;
+                    *(lds_u2)(aside + 16 * kKeys + 8) = u32x2{(uint32_t)bad, (uint32_t)(bad >> 32)};
                 }
             }
         }
@@ -451,51 +470,53 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     const int i16 = lane & 15, v_row = 4 * g + (i16 >> 2);
     const uint32_t k_lane = (uint32_t)(n * T::kRow + ((g ^ T::swizzle_k(n)) << 4));
     const uint32_t v_lane = (uint32_t)(v_row * T::kRow + 8 * (i16 & 1) + (((2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1)) ^ T::swizzle_v(v_row)) << 4));
-    auto v_operand = [&](uint32_t buf, int c, int m) -> u32x4 {
-        const uint32_t at = ((v_lane + buf + 2 * T::kBytes) ^ (uint32_t)(m << 6)) + (uint32_t)(c * 16 * T::kRow);
+    auto v_operand = [&](uint32_t first, int c, int m) -> u32x4 {
+        const uint32_t at = (first ^ (uint32_t)(m << 6)) + (uint32_t)(c * 16 * T::kRow);
         const u32x2 lo = lds_read_transposed(at), hi = lds_read_transposed(at + 8 * T::kRow);
         return u32x4{lo[0], lo[1], hi[0], hi[1]};
     };
-    // four tokens' of an array of scales: keys 32 u + 8 c + 4 g ..
-    auto four_of = [&](uint32_t parity, int array, int u, int c) -> f32x4 {
-        return *(lds_f4)(kAside + parity * kAsideBytes + (uint32_t)(256 * array + 4 * (32 * u + 8 * c)) + 16u * (uint32_t)g);
-    };
 
     float m_ref = -__builtin_inff(), l = 0.0f, v_sum = 0.0f;
-    int exponent = -100;                                        // of the largest vs seen; it is part of m_sub
+    int exponent = -126;                                        // of the largest vs seen; it is part of m_sub
     f32x16 o[OM];
 #pragma unroll
     for (int m = 0; m < OM; ++m)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[m][r] = 0.0f;
 
-    // One tile; `whole`: all rows see all of its keys.
-    auto tile_of = [&](int t, uint32_t parity, unsigned valid, bool whole) {
-        const uint32_t buf = parity * T::kBytes;
-        const int k0 = span.real(t) * kKeys;
-        f32x16 s[2];
+    // 32 U keys from k0 on, whose k, v and scales lie in LDS; `whole`: all rows see all of them; valid: a bit for each 16 whose page exists.  The
+    // steps: after_scores, before_product (v has to be there then), bad_of the keys whose v is not finite, take_out of them.
+    auto attend = [&](auto blocks, int k0, uint32_t k_buf, uint32_t v_buf, uint32_t scales, unsigned valid, bool whole, auto after_scores, auto before_product,
+                      auto bad_of, auto take_out) {
+        constexpr int U = decltype(blocks)::value;
+        // four tokens' of an array of scales: keys 32 u + 8 c + 4 g ..
+        auto four_of = [&](int array, int u, int c) -> f32x4 { return *(lds_f4)(scales + (uint32_t)(128 * U * array + 4 * (32 * u + 8 * c)) + 16u * (uint32_t)g); };
+        f32x16 s[U];
+        uint32_t k_at = k_lane + k_buf, v_at = v_lane + v_buf;
+        asm volatile("" : "+v"(k_at), "+v"(v_at));               // (or every operand's address is kept in a register)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < U; ++u) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[u][r] = 0.0f;
 #pragma unroll
             for (int i = 0; i < QM; ++i) {
-                const u32x4 k = *(lds_u4)(((k_lane + buf) ^ (uint32_t)(i << 5)) + (uint32_t)(u * 32 * T::kRow));
+                const u32x4 k = *(lds_u4)((k_at ^ (uint32_t)(i << 5)) + (uint32_t)(u * 32 * T::kRow));
                 s[u] = mma32<MMA16>(k, q[i], s[u]);
             }
             if (CODES) __builtin_amdgcn_sched_barrier(0);       // (or operands of all products are fetched at once, into registers that are not there)
         }
         if constexpr (CODES) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    const f32x4 ks = four_of(parity, 0, u, c), ko = four_of(parity, 1, u, c);
+                    const f32x4 ks = four_of(0, u, c), ko = four_of(1, u, c);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) s[u][4 * c + r] = fmaf(ks[r], s[u][4 * c + r], ko[r] * sum_q);
                     if (c & 1) __builtin_amdgcn_sched_barrier(0);
                 }
         }
+        after_scores();
         // (places relative to the tile's first key of this half, which may be those of no page)
         const int base = k0 + 4 * g, lim_at = lim - base, lo_at = (max(lim, 0) + 1 - base) - a.window, sinks_at = a.sinks - base;
         auto sees = [&](int u, int r) -> bool {
@@ -504,7 +525,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         };
         if (!whole) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[u][r] = sees(u, r) ? s[u][r] : -__builtin_inff();
         }
@@ -512,21 +533,21 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         // The maximum in use is raised only when a score exceeds it by 2^kSlack, which spares nearly all rescaling of o.
         float top = s[0][0];
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
         top = fmaxf(top, other_half(top)) * scale;
         bool moved = top > m_ref + kSlack;
         int higher = exponent;
         if constexpr (CODES) {
-            float big = *(lds_f)(kAside + parity * kAsideBytes + 1024);
+            float big = *(lds_f)(scales + 512 * U);
             if (!whole) {
                 big = 0.0f;
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const f32x4 vs = four_of(parity, 2, u, c);
+                        const f32x4 vs = four_of(2, u, c);
 #pragma unroll
                         for (int r = 0; r < 4; ++r) big = sees(u, 4 * c + r) ? fmaxf(big, fabsf(vs[r])) : big;
                     }
@@ -537,12 +558,12 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         }
         // A weight's exponent is scale s - m_sub: a product that is not rounded, less a maximum that is.  Beyond 2^31 that rounding alone would leave
         // the exponents' range: where some row's maximum lies beyond kFar, the scores are replaced by their distance from it, both rounded alike.
-        auto m_used = [&](float m, int e) -> float { return (m == -__builtin_inff() ? 0.0f : m) + (CODES ? (float)min(e, kFold) : 0.0f); };
+        auto m_used = [&](float m, int e) -> float { return (m == -__builtin_inff() ? 0.0f : m) + (CODES ? (float)with_maximum(e) : 0.0f); };
         if (__builtin_amdgcn_ballot_w64(moved)) {
             const float m_new = moved ? fmaxf(m_ref, top) : m_ref;
             const float alpha = exp2_fast(m_new > m_ref ? m_ref - m_new : 0.0f);
-            const float less = CODES ? __builtin_ldexpf(1.0f, max(min(exponent, kFold) - min(higher, kFold), -140)) : 1.0f;
-            const float fold = CODES ? __builtin_ldexpf(1.0f, max(max(exponent - kFold, 0) - max(higher - kFold, 0), -140)) : 1.0f;
+            const float less = CODES ? __builtin_ldexpf(1.0f, with_maximum(exponent) - with_maximum(higher)) : 1.0f;
+            const float fold = CODES ? __builtin_ldexpf(1.0f, max(folded(exponent) - folded(higher), -140)) : 1.0f;
             m_ref = m_new;
             exponent = higher;
             l *= alpha * less;
@@ -555,7 +576,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         if (__builtin_amdgcn_ballot_w64(fabsf(m_sub) > kFar)) {
             const float back = 1.0f / scale;
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
 #pragma clang fp contract(off)
@@ -565,10 +586,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
             m_sub = 0.0f;
         }
 
-        u32x4 p[4];
-        const bool folds = CODES && __builtin_amdgcn_ballot_w64(exponent > kFold) != 0ull;
+        u32x4 p[2 * U];
+        const bool folds = CODES && __builtin_amdgcn_ballot_w64(folded(exponent) != 0) != 0ull;
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 f32x4 e;
@@ -578,8 +599,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                     l += e[r];
                 }
                 if constexpr (CODES) {
-                    f32x4 vs = four_of(parity, 2, u, c), vo = four_of(parity, 3, u, c);
-                    if (folds) vs *= __builtin_ldexpf(1.0f, -max(exponent - kFold, 0));
+                    f32x4 vs = four_of(2, u, c), vo = four_of(3, u, c);
+                    if (folds) vs *= __builtin_ldexpf(1.0f, -folded(exponent));
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         v_sum = fmaf(e[r], vo[r], v_sum);
@@ -593,8 +614,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
 
         // 0 times what is not finite would be NaN: tokens with such a v (in tiles that not all rows see, with codes in all) are added one by one to
         // the rows that see them, and are zeros in the product.
+        before_product();
         if (CODES || !whole) {
-            const unsigned long long bad = bad_of(parity);
+            const unsigned long long bad = bad_of();
             if (bad) {
 #pragma unroll 1
                 for (unsigned long long left = bad; left; left &= left - 1) {
@@ -606,7 +628,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                         const int c = key >> 4, half = (key >> 2) & 1, slot = (key & 3) | ((key >> 1) & 4);
                         uint32_t pair = 0u;
 #pragma unroll
-                        for (int x = 0; x < 16; ++x) pair = x == 4 * c + (slot >> 1) ? p[x >> 2][x & 3] : pair;
+                        for (int x = 0; x < 8 * U; ++x) pair = x == 4 * c + (slot >> 1) ? p[x >> 2][x & 3] : pair;
                         const float mine = slot & 1 ? h16hi_to_f32<MMA16>(pair) : h16lo_to_f32<MMA16>(pair), other = other_half(mine);
                         const float weight = g == half ? mine : other;
 #pragma unroll
@@ -614,7 +636,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
                                 const uint32_t piece = (uint32_t)((4 * m + r) ^ T::swizzle_v(key));
-                                const u32x2 v = *(lds_u2)(buf + 2u * T::kBytes + (uint32_t)(key * T::kRow) + 16u * piece + 8u * (uint32_t)g);
+                                const u32x2 v = *(lds_u2)(v_buf + (uint32_t)(key * T::kRow) + 16u * piece + 8u * (uint32_t)g);
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) {
                                     const float x = e & 1 ? h16hi_to_f32<F16>(v[e >> 1]) : h16lo_to_f32<F16>(v[e >> 1]);
@@ -623,67 +645,261 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                             }
                     }
                 }
-                if constexpr (!CODES) take_out(parity, bad);
+                if constexpr (!CODES) take_out(bad);
             }
         }
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+        for (int c = 0; c < 2 * U; ++c)
 #pragma unroll
-            for (int m = 0; m < OM; ++m) o[m] = mma32<MMA16>(v_operand(buf, c, m), p[c], o[m]);
+            for (int m = 0; m < OM; ++m) o[m] = mma32<MMA16>(v_operand(v_at, c, m), p[c], o[m]);
     };
 
-    // `page` is that of the tile whose loads go out next: the next tile's, with codes the one behind it.
-    int page = 0;
-    unsigned valid = 15u, valid_next = 15u;                     // of tiles t and t + 1
-    if (t_first < t_end) {
-        page = pages_of(t_first);
-        valid = valid_of(page);
-        if constexpr (CODES) {
-            load_raw(t_first, page);
-            stage(t_first, t_first & 1);
-            if (t_first + 1 < t_end) {
-                page = pages_of(t_first + 1);
-                valid_next = valid_of(page);
-                load_raw(t_first + 1, page);
-                if (t_first + 2 < t_end) page = pages_of(t_first + 2);
+    auto wide_rows = [&] {
+        // `page` is that of the tile whose loads go out next: the next tile's, with codes the one behind it.
+        int page = 0;
+        unsigned valid = 15u, valid_next = 15u;                     // of tiles t and t + 1
+        if (t_first < t_end) {
+            page = pages_of(t_first);
+            valid = valid_of(page);
+            if constexpr (CODES) {
+                load_raw(t_first, page);
+                stage(t_first, t_first & 1);
+                if (t_first + 1 < t_end) {
+                    page = pages_of(t_first + 1);
+                    valid_next = valid_of(page);
+                    load_raw(t_first + 1, page);
+                    if (t_first + 2 < t_end) page = pages_of(t_first + 2);
+                }
+            } else {
+                copy_tile(t_first, page, t_first & 1);
+                if (t_first + 1 < t_end) page = pages_of(t_first + 1);
             }
-        } else {
-            copy_tile(t_first, page, t_first & 1);
-            if (t_first + 1 < t_end) page = pages_of(t_first + 1);
         }
-    }
 #pragma unroll 1
-    for (int t = t_first; t < t_end; ++t) {
-        const uint32_t parity = (uint32_t)(t & 1);
-        const int k0 = span.real(t) * kKeys;
-        const bool whole = k0 + kKeys - 1 <= all_lim && (k0 >= all_lo || k0 + kKeys <= a.sinks) && valid == 15u;
-        if constexpr (!CODES) {
-            loads_left<0>();
-            if (!whole) look_at_v(parity);
-        }
-        lds_barrier();                                          // tile t is there, and nobody reads the one in front of it any more
-        unsigned valid_after = 15u;
-        if constexpr (CODES) {
-            if (t + 1 < t_end) stage(t + 1, parity ^ 1u);
-            if (t + 2 < t_end) {
-                valid_after = valid_of(page);
-                load_raw(t + 2, page);
-                if (t + 3 < t_end) page = pages_of(t + 3);
+        for (int t = t_first; t < t_end; ++t) {
+            const uint32_t parity = (uint32_t)(t & 1);
+            const int k0 = span.real(t) * kKeys;
+            const bool whole = k0 + kKeys - 1 <= all_lim && (k0 >= all_lo || k0 + kKeys <= a.sinks) && valid == 15u;
+            if constexpr (!CODES) {
+                loads_left<0>();
+                if (!whole) look_at_v(parity);
             }
-        } else if (t + 1 < t_end) {
-            valid_next = valid_of(page);
-            copy_tile(t + 1, page, parity ^ 1u);
-            if (t + 2 < t_end) page = pages_of(t + 2);
+            lds_barrier();                                          // tile t is there, and nobody reads the one in front of it any more
+            unsigned valid_after = 15u;
+            if constexpr (CODES) {
+                if (t + 1 < t_end) stage(t + 1, parity ^ 1u);
+                if (t + 2 < t_end) {
+                    valid_after = valid_of(page);
+                    load_raw(t + 2, page);
+                    if (t + 3 < t_end) page = pages_of(t + 3);
+                }
+            } else if (t + 1 < t_end) {
+                valid_next = valid_of(page);
+                copy_tile(t + 1, page, parity ^ 1u);
+                if (t + 2 < t_end) page = pages_of(t + 2);
+            }
+            if (active) {
+                attend(std::integral_constant<int, 2>{}, k0, parity * T::kBytes, (2 + parity) * T::kBytes, kAside + parity * kAsideBytes, valid, whole, [] {}, [] {},
+                       [&] { return bad_of_tile(parity); }, [&](unsigned long long bad) { take_out(parity, bad); });
+            } else if (!CODES && !whole) {
+                if (const unsigned long long bad = bad_of_tile(parity)) take_out(parity, bad);
+            }
+            valid = valid_next;
+            valid_next = valid_after;
         }
-        if (active) {
-            tile_of(t, parity, valid, whole);
-        } else if (!CODES && !whole) {
-            if (const unsigned long long bad = bad_of(parity)) take_out(parity, bad);
+    };
+
+    // Up to 32 rows.  A wavefront's own part of LDS: 32 keys of k, 32 of v; k's next 32 are on their way while v's are used, and the other way round.
+    auto narrow_rows = [&] {
+        constexpr uint32_t kHalf = 32 * T::kRow, kCopies = kHalf / 1024;
+        const uint32_t k_buf = (uint32_t)wave * 2 * kHalf, v_buf = k_buf + kHalf, scales = kAside + (uint32_t)wave * kScaleBytes<32>;
+        const int h_end = 2 * t_end - (t_end > t_first && span.real(t_end - 1) * kKeys + 32 >= span.end ? 1 : 0);
+        auto key_of = [&](int h) -> int { return span.real(h >> 1) * kKeys + 32 * (h & 1); };
+        // the pages of its two 16 tokens
+        struct Two {
+            int page[2];
+        };
+        auto pages_of_half = [&](int h) -> Two {
+            Two two{{0, 0}};
+            if constexpr (PAGED) {
+                const auto entries = (const __attribute__((address_space(4))) int32_t*)reinterpret_cast<uintptr_t>(table);
+                const int k0 = key_of(h);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) two.page[i] = entries[min(k0 + 16 * i, lk - 1) >> a.c.page_shift];
+            }
+            return two;
+        };
+        auto valid_of_half = [&](const Two& two) -> unsigned { return (there(two.page[0]) ? 1u : 0u) | (there(two.page[1]) ? 2u : 0u); };
+        auto first_of = [&](const Two& two, int i) -> int64_t { return PAGED ? a.c.first_token(there(two.page[i]) ? two.page[i] : 0, (int)kv_head) : 0; };
+
+        // 16 bits: 64 lanes copy kRows rows at a time
+        auto copy_half = [&](int h, const Two& two, bool of_v) {
+            const int k0 = key_of(h);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // (what is read from there has been read)
+#pragma unroll
+            for (int j = 0; j < (int)kCopies; ++j) {
+                const int first = j * T::kRows, r = first + lane / T::kPieces, i = first / 16;
+                const int tok = min(k0 + r, lk - 1);
+                const uint32_t piece = 16u * (uint32_t)(copy_piece ^ (of_v ? T::swizzle_v(r) : T::swizzle_k(r)));
+                const uint32_t to = (of_v ? v_buf : k_buf) + 1024u * (uint32_t)j;
+                if constexpr (SOURCE == kRows) {
+                    const Rows& rows_of = of_v ? a.v : a.k;
+                    const uint32_t step = of_v ? v_step : k_step;
+                    const char* base = reinterpret_cast<const char*>(rows_of.p + (int64_t)w.r.k_at * rows_of.token + (int64_t)kv_head * rows_of.head) + (int64_t)k0 * step;
+                    copy_to_lds(to, base, (uint32_t)(tok - k0) * step + piece);
+                } else {
+                    const char* base = reinterpret_cast<const char*>(of_v ? a.c.v : a.c.k) + first_of(two, i) * T::kRow;
+                    copy_to_lds(to, base, (uint32_t)(tok & page_mask) * (uint32_t)T::kRow + piece);
+                }
+            }
+        };
+        auto bad_of_half = [&]() -> unsigned long long {
+            constexpr uint32_t kExp = F16 ? 0x7C007C00u : 0x7F807F80u, kOne = F16 ? 0x04000400u : 0x00800080u;
+            unsigned long long bad = 0ull;
+#pragma unroll 1
+            for (int j = 0; j < (int)kCopies; ++j) {
+                const u32x4 v = *(lds_u4)(v_buf + 1024u * (uint32_t)j + 16u * (uint32_t)lane);
+                uint32_t bits = 0u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) bits |= (v[i] & kExp) + kOne;
+                const unsigned long long lanes = __builtin_amdgcn_ballot_w64((bits & 0x80008000u) != 0u);
+                if (lanes) {
+#pragma unroll
+                    for (int r = 0; r < T::kRows; ++r) bad |= ((lanes >> (r * T::kPieces)) & ((1ull << T::kPieces) - 1) ? 1ull : 0ull) << (j * T::kRows + r);
+                }
+            }
+            return bad;
+        };
+        auto take_out_of_half = [&](unsigned long long bad) {
+#pragma unroll 1
+            for (int j = 0; j < (int)kCopies; ++j)
+                if ((bad >> (j * T::kRows + lane / T::kPieces)) & 1ull) *(lds_u4)(v_buf + 1024u * (uint32_t)j + 16u * (uint32_t)lane) = u32x4{0u, 0u, 0u, 0u};
+        };
+
+        // codes: 16 bytes a lane at a time
+        constexpr int kRowBytes = CODES ? D * SOURCE / 8 : 64, kRowLanes = kRowBytes / 16, kLoads = 32 / (64 / kRowLanes), kRowsAtOnce = 64 / kRowLanes;
+        constexpr int kPer = CODES ? 16 * 8 / SOURCE : 8;          // codes of a load
+        uint32_t raw_k[kLoads][4], raw_v[kLoads][4];
+        u32x2 raw_scales = {0u, 0u};
+        auto load_half = [&](int h, const Two& two, bool of_v, uint32_t (&to)[kLoads][4]) {
+            const int k0 = key_of(h);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int r = i * kRowsAtOnce + lane / kRowLanes;
+                const int64_t first = (kRowsAtOnce <= 16 ? (i * kRowsAtOnce < 16) : r < 16) ? first_of(two, 0) : first_of(two, 1);
+                const uint8_t* p = (of_v ? a.c.v : a.c.k) + (first + (min(k0 + r, lk - 1) & page_mask)) * kRowBytes + 16 * (lane % kRowLanes);
+                load_bytes(p, to[i]);
+            }
+        };
+        auto load_scales = [&](int h, const Two& two) {
+            if (lane < 32) raw_scales = *reinterpret_cast<const u32x2*>(a.c.scales + 4 * ((lane < 16 ? first_of(two, 0) : first_of(two, 1)) + (min(key_of(h) + lane, lk - 1) & page_mask)));
+        };
+        auto stage_half = [&](auto of_v, const uint32_t (&from)[kLoads][4]) {
+            constexpr bool V = decltype(of_v)::value;
+            constexpr int BITS = CODES ? SOURCE : 8;
+            // (the first row's first piece; a register of its own in each round, as the others' would be if they were kept)
+            const int r0 = lane / kRowLanes, piece0 = (lane % kRowLanes) * (kPer / 8);
+            uint32_t to = (V ? v_buf : k_buf) + (uint32_t)(r0 * T::kRow) + 16u * (uint32_t)(piece0 ^ (V ? T::swizzle_v(r0) : T::swizzle_k(r0)));
+            asm volatile("" : "+v"(to));
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                uint32_t wide[kPer / 2];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) widen<BITS, V>(from[i][x], wide + x * 16 / BITS);
+#pragma unroll
+                for (int x = 0; x < kPer / 8; ++x) {
+                    const uint32_t other = 16u * (uint32_t)(x ^ (V ? T::swizzle_v(i * kRowsAtOnce) : T::swizzle_k(i * kRowsAtOnce)));
+                    *(lds_u4)((to ^ other) + (uint32_t)(i * kRowsAtOnce * T::kRow)) = u32x4{wide[4 * x], wide[4 * x + 1], wide[4 * x + 2], wide[4 * x + 3]};
+                }
+            }
+            using C = Codes<BITS>;
+            const float by = bf16lo_to_f32(raw_scales[V ? 1 : 0]), off = bf16hi_to_f32(raw_scales[V ? 1 : 0]);
+            const float mid = fmaf(V ? C::kCentre : -C::kBias, by, off);
+            const bool fine = !V || fabsf(mid) < __builtin_inff();
+            if (lane < 32) {
+                *(lds_f)(scales + (V ? 256 : 0) + 4u * (uint32_t)lane) = fine ? by : 0.0f;
+                *(lds_f)(scales + (V ? 384 : 128) + 4u * (uint32_t)lane) = fine ? mid : 0.0f;
+            }
+            if constexpr (V) {
+                float big = lanes_reduce<16>(fine && lane < 32 ? fabsf(by) : 0.0f, [](float u, float v) { return fmaxf(u, v); });
+                big = fmaxf(big, __shfl_xor(big, 16));
+                const unsigned long long bad = __builtin_amdgcn_ballot_w64(!fine && lane < 32);
+                if (lane == 0) {
+                    *(lds_f)(scales + 512) = big;
+                    *(lds_u2)(scales + 520) = u32x2{(uint32_t)bad, 0u};
+                }
+            }
+        };
+
+        int h = 2 * t_first + wave;
+        Two two{{0, 0}}, two_next{{0, 0}};
+        unsigned valid = 3u, valid_next = 3u;
+        if (h < h_end) {
+            two = pages_of_half(h);
+            valid = valid_of_half(two);
+            if constexpr (CODES) {
+                load_half(h, two, false, raw_k);
+                load_half(h, two, true, raw_v);
+                load_scales(h, two);
+                if (h + kWaves < h_end) two = pages_of_half(h + kWaves);
+                stage_half(std::false_type{}, raw_k);
+                stage_half(std::true_type{}, raw_v);
+                if (h + kWaves < h_end) {
+                    valid_next = valid_of_half(two);
+                    load_half(h + kWaves, two, false, raw_k);
+                    load_half(h + kWaves, two, true, raw_v);
+                    load_scales(h + kWaves, two);
+                }
+            } else {
+                copy_half(h, two, false);
+                copy_half(h, two, true);
+            }
         }
-        valid = valid_next;
-        valid_next = valid_after;
-    }
-    if (!active) return;
+#pragma unroll 1
+        for (; h < h_end; h += kWaves) {
+            const int next = h + kWaves, after = h + 2 * kWaves, k0 = key_of(h);
+            const bool whole = k0 + 31 <= all_lim && (k0 >= all_lo || k0 + 32 <= a.sinks) && valid == 3u;
+            unsigned valid_after = 3u;
+            if constexpr (CODES) {
+                if (after < h_end) two_next = pages_of_half(after);
+                attend(std::integral_constant<int, 1>{}, k0, k_buf, v_buf, scales, valid, whole,
+                       [&] {
+                           if (next < h_end) stage_half(std::false_type{}, raw_k);
+                           if (after < h_end) load_half(after, two_next, false, raw_k);
+                       },
+                       [] {},
+                       [&]() -> unsigned long long { return (unsigned)__builtin_amdgcn_readfirstlane((int)*(lds_u1)(scales + 520)); }, [](unsigned long long) {});
+                if (next < h_end) stage_half(std::true_type{}, raw_v);
+                if (after < h_end) {
+                    valid_after = valid_of_half(two_next);
+                    load_half(after, two_next, true, raw_v);
+                    load_scales(after, two_next);
+                }
+            } else {
+                if (next < h_end) {
+                    two_next = pages_of_half(next);
+                    valid_next = valid_of_half(two_next);
+                }
+                loads_left<(int)kCopies>();                         // k is there; v's copies may be on their way
+                attend(std::integral_constant<int, 1>{}, k0, k_buf, v_buf, scales, valid, whole,
+                       [&] {
+                           if (next < h_end) copy_half(next, two_next, false);
+                       },
+                       [&] {
+                           if (next < h_end) loads_left<(int)kCopies>();
+                           else loads_left<0>();
+                       },
+                       bad_of_half, take_out_of_half);
+                if (next < h_end) copy_half(next, two_next, true);
+            }
+            valid = valid_next;
+            valid_next = valid_after;
+        }
+    };
+
+    if (narrow) narrow_rows();
+    else wide_rows();
+    if (!active) return;                                        // (of a narrow tile all are)
 
     // (the lane's number anew: what follows from it is not to take registers from the loop above)
     int thread = threadIdx.x;
@@ -693,11 +909,59 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     l += other_half(l);
     if constexpr (CODES) {
         v_sum += other_half(v_sum);
-        const float unfold = __builtin_ldexpf(1.0f, max(exponent - kFold, 0));
+        const float unfold = __builtin_ldexpf(1.0f, folded(exponent));
 #pragma unroll
         for (int m = 0; m < OM; ++m)
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[m][r] = fmaf(o[m][r], unfold, v_sum);
+    }
+    auto store_row = [&](int row, int four, f32x4 v) {           // four of 4 * OM, for this lane's half
+        const int query_e = (int)((unsigned)row / (unsigned)a.shared), head = (int)kv_head * a.shared + (row - query_e * a.shared);
+        uint16_t* out = a.out + ((int64_t)(w.r.q_at + query_e) * a.heads + head) * D + 4 * g_e + 8 * four;
+        *reinterpret_cast<u32x2*>(out) = u32x2{pack<F16>(v[0], v[1]), pack<F16>(v[2], v[3])};
+    };
+    const float m_own = m_ref == -__builtin_inff() ? m_ref : m_ref + (CODES ? (float)with_maximum(exponent) : 0.0f);
+    if (narrow) {
+        // the wavefronts' sums meet in LDS, [wavefront][4 OM][lane], and each adds up a quarter of the places
+        lds_barrier();
+        const uint32_t at = 16u * (uint32_t)(thread & 63);
+#pragma unroll
+        for (int m = 0; m < OM; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                *(lds_f4)((uint32_t)(wave * 4 * OM + 4 * m + r) * 1024u + at) = f32x4{o[m][4 * r], o[m][4 * r + 1], o[m][4 * r + 2], o[m][4 * r + 3]};
+        if (g_e == 0) *(lds_u2)(kAside + (uint32_t)(8 * (32 * wave + n_e))) = u32x2{__float_as_uint(m_own), __float_as_uint(l)};
+        lds_barrier();
+        float m[kWaves], top = -__builtin_inff(), sum = 0.0f;
+        u32x2 ml[kWaves];
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+            ml[i] = *(lds_u2)(kAside + (uint32_t)(8 * (32 * i + n_e)));
+            top = fmaxf(top, __uint_as_float(ml[i][0]));
+        }
+        const float use = top == -__builtin_inff() ? 0.0f : top;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+            m[i] = exp2_fast(__uint_as_float(ml[i][0]) - use);
+            sum = fmaf(m[i], __uint_as_float(ml[i][1]), sum);
+        }
+        const float inv = w.pieces > 1 ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum;
+        float* to = a.partial + (int64_t)w.slot * kPieceFloats<D>;
+#pragma unroll
+        for (int x = 0; x < OM; ++x) {
+            const int four = wave * OM + x;
+            f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) {
+                const f32x4 y = *(lds_f4)((uint32_t)(i * 4 * OM + four) * 1024u + at);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = fmaf(m[i], y[e], v[e]);
+            }
+            if (w.pieces > 1) reinterpret_cast<f32x4*>(to)[four * 64 + (thread & 63)] = v;
+            else if (row0 + n_e < rows) store_row(row0 + n_e, four, f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv});
+        }
+        if (w.pieces > 1 && wave == 0 && g_e == 0) reinterpret_cast<f32x2*>(to + kRowTile * D)[n_e] = f32x2{top, sum};
+        return;
     }
     if (w.pieces > 1) {
         float* to = a.partial + (int64_t)w.slot * kPieceFloats<D>;
@@ -706,22 +970,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         for (int m = 0; m < OM; ++m)
 #pragma unroll
             for (int r = 0; r < 4; ++r) sums[(4 * m + r) * 64] = f32x4{o[m][4 * r], o[m][4 * r + 1], o[m][4 * r + 2], o[m][4 * r + 3]};
-        if (g_e == 0) {
-            const float m = m_ref == -__builtin_inff() ? m_ref : m_ref + (CODES ? (float)min(exponent, kFold) : 0.0f);
-            reinterpret_cast<f32x2*>(to + kRowTile * D)[32 * wave + n_e] = f32x2{m, l};
-        }
+        if (g_e == 0) reinterpret_cast<f32x2*>(to + kRowTile * D)[32 * wave + n_e] = f32x2{m_own, l};
         return;
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;              // (no key seen: o is 0 as well)
     if (row0 + n_e < rows) {
-        const int query_e = (int)((unsigned)(row0 + n_e) / (unsigned)a.shared), head = (int)kv_head * a.shared + (row0 + n_e - query_e * a.shared);
-        uint16_t* out = a.out + ((int64_t)(w.r.q_at + query_e) * a.heads + head) * D + 4 * g_e;
 #pragma unroll
         for (int m = 0; m < OM; ++m)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                *reinterpret_cast<u32x2*>(out + 32 * m + 8 * r) =
-                    u32x2{pack<F16>(o[m][4 * r] * inv, o[m][4 * r + 1] * inv), pack<F16>(o[m][4 * r + 2] * inv, o[m][4 * r + 3] * inv)};
+            for (int r = 0; r < 4; ++r) store_row(row0 + n_e, 4 * m + r, f32x4{o[m][4 * r] * inv, o[m][4 * r + 1] * inv, o[m][4 * r + 2] * inv, o[m][4 * r + 3] * inv});
     }
 }
 
@@ -780,7 +1037,8 @@ __global__ __launch_bounds__(256) void attn_chunk_join_kernel(Args a) {
 
 template <int SOURCE, int D, bool F16> hipError_t launch(Args a, const ChunkPlan& pl, hipStream_t stream) {
     constexpr auto kernel = attn_chunk_kernel<SOURCE, D, F16>;
-    constexpr int bytes = 4 * Tile<D, kWaves>::kBytes + 2 * (SOURCE == 8 || SOURCE == 4 ? 4 * 256 + 16 : 16);
+    constexpr int bytes = 4 * Tile<D, kWaves>::kBytes + kAsideAll<SOURCE == 8 || SOURCE == 4>;
+    static_assert(kAsideAll<true> >= 2 * kScaleBytes<kKeys>, "two tiles' scales");
     if (hipError_t e = ensure_lds<kernel>(bytes); e != hipSuccess) return e;
     a.target = pl.target;
     a.slots = pl.slots;
