@@ -192,7 +192,7 @@ int any4_attn_prompt_window(const uint16_t* q, int64_t q_token_stride, int64_t q
         !strides_ok(q_token_stride, q_head_stride) || !strides_ok(k_token_stride, k_head_stride) || !strides_ok(v_token_stride, v_head_stride) ||
         k_token_stride >= kMaxStride || v_token_stride >= kMaxStride || !rows_ok(q_tokens, heads, kv_heads))
         return ANY4_ERR_SHAPE;
-    const ChunkPlan pl = plan_attn_chunk(requests, q_tokens, heads, kv_heads, head_dim, 0, device_compute_units());
+    const ChunkPlan pl = plan_attn_chunk(requests, q_tokens, heads, kv_heads, head_dim, k_tokens, false, device_compute_units());
     if (pl.blocks > 0x7FFFFFFF) return ANY4_ERR_SHAPE;
     if (requests == 0 || q_tokens == 0) return ANY4_OK;
     // (without a single key k and v are not read)
@@ -210,7 +210,7 @@ size_t any4_attn_chunk_workspace_bytes(int64_t requests, int64_t q_tokens, int h
     if (requests < 1 || requests > kMaxTokens || q_tokens < 1 || q_tokens > kMaxTokens || !heads_ok(heads, kv_heads) || (head_dim != 64 && head_dim != 128) ||
         max_tokens < 1 || max_tokens > kMaxTokens || !rows_ok(q_tokens, heads, kv_heads))
         return 0;
-    return plan_attn_chunk(requests, q_tokens, heads, kv_heads, head_dim, max_tokens, device_compute_units()).workspace;
+    return plan_attn_chunk(requests, q_tokens, heads, kv_heads, head_dim, max_tokens, true, device_compute_units()).workspace;
 }
 
 int any4_attn_chunk(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const any4_kv_cache* cache, const int32_t* page_table,
@@ -221,7 +221,7 @@ int any4_attn_chunk(const uint16_t* q, int64_t q_token_stride, int64_t q_head_st
         !strides_ok(q_token_stride, q_head_stride) || table_width < 1 || table_width > kMaxTokens / cache->page_size || table_stride < 0 || window < 0 ||
         sinks < 0 || !rows_ok(q_tokens, heads, cache->kv_heads))
         return ANY4_ERR_SHAPE;
-    const ChunkPlan pl = plan_attn_chunk(requests, q_tokens, heads, cache->kv_heads, cache->head_dim, table_width * cache->page_size, device_compute_units());
+    const ChunkPlan pl = plan_attn_chunk(requests, q_tokens, heads, cache->kv_heads, cache->head_dim, table_width * cache->page_size, true, device_compute_units());
     if (pl.blocks > 0x7FFFFFFF) return ANY4_ERR_SHAPE;
     if (requests == 0 || q_tokens == 0) return ANY4_OK;
     if (!q || !page_table || !q_starts || !lengths || !out) return ANY4_ERR_NULL;

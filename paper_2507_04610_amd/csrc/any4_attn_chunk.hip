@@ -32,7 +32,9 @@ namespace {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kRowTile = 32 * kWaves;
 constexpr int kNarrow = 4;                                      // tiles of keys for up to 32 rows that take as long as one for 128
-constexpr int kLeastPiece = 4;                                  // key tiles of a piece: a join costs as much as a few of them
+constexpr int kLeastPiece = 4;                                  // least tiles of keys of a piece
+constexpr int kWhole = 10;                                      // keys of so many tiles are not cut: the join costs as much as a few of them
+constexpr int kSmall = 1024;                                    // calls of so many tiles of keys take 32 rows at a time: more blocks, each done sooner
 constexpr int kNoWindow = 0x7FFFF800;                           // more than any request's tokens
 // The exponent of the largest vs_j goes with the maximum as far as 2^+-kFold: beyond, weights of tokens whose scales differ by 2^126 and more would
 // be lost, to each other and to the sum of weights.  The rest is taken off vs_j itself.
@@ -53,6 +55,7 @@ struct Args {
     const int32_t* lengths;            // cache
     int q_tokens, k_tokens, requests, heads, kv_heads, shared, window, sinks;
     int target, slots;                 // blocks that fill the chip (0: nothing is cut); pieces that the workspace has room for
+    int small;                         // whether the call may be one that takes 32 rows at a time
     unsigned first_block;              // of this launch
     float scale_log2;
     uint16_t* out;
@@ -83,11 +86,11 @@ struct Span {
     int front, gap, tiles, end;        // end: of the keys that the last query sees
     __device__ __forceinline__ int real(int t) const { return t < front ? t : t + gap; }
 };
-__device__ __forceinline__ Span span_of(const Args& a, const Request& r, int tile) {
+__device__ __forceinline__ Span span_of(const Args& a, const Request& r, int tile, int height) {
     Span s;
     const int rows = r.lq * a.shared, ahead = r.lk - r.lq;
-    s.first = (int)((unsigned)(tile * kRowTile) / (unsigned)a.shared);
-    s.last = (int)((unsigned)(min(tile * kRowTile + kRowTile, rows) - 1) / (unsigned)a.shared);
+    s.first = (int)((unsigned)(tile * height) / (unsigned)a.shared);
+    s.last = (int)((unsigned)(min(tile * height + height, rows) - 1) / (unsigned)a.shared);
     const int end = s.end = max(ahead + s.last + 1, 0), start = max(max(ahead + s.first, 0) + 1 - a.window, 0);
     const int begin = start / kKeys;
     s.front = min((int)(((unsigned)min(a.sinks, end) + kKeys - 1) / kKeys), begin);
@@ -98,46 +101,78 @@ __device__ __forceinline__ Span span_of(const Args& a, const Request& r, int til
 
 // Which rows and keys a block has.  Blocks of a request: tile of rows by tile of rows, each tile's pieces side by side.
 struct Work {
-    int request, tile, piece, pieces, slot;
+    int request, tile, piece, pieces, slot, height;
     Request r;
 };
 struct Shares {                        // of 64 requests, a lane each
     Request r;
     int tiles, pieces;
 };
-// what the last (and longest) of its tiles of rows costs, in tiles of keys for 128 rows
-__device__ __forceinline__ int costs_of(const Args& a, const Shares& s) {
-    const int tiles = span_of(a, s.r, s.tiles - 1).tiles;
-    return s.r.lq * a.shared <= 32 ? (tiles + kNarrow - 1) / kNarrow : tiles;
+// what a request's last (and longest) tile of rows costs, in tiles of keys for 128 rows
+__device__ __forceinline__ int costs_of(const Args& a, const Request& r, int tiles, int height) {
+    const int of_keys = span_of(a, r, tiles - 1, height).tiles;
+    return height == 32 || r.lq * a.shared <= 32 ? (of_keys + kNarrow - 1) / kNarrow : of_keys;
 }
-template <int SOURCE> __device__ __forceinline__ Shares shares_of(const Args& a, int r0, int least, int lane) {
+__device__ __forceinline__ int tiles_of(const Args& a, const Request& r, int height) {
+    return (int)(((unsigned)(r.lq * a.shared) + (unsigned)height - 1) / (unsigned)height);
+}
+// How a call is cut: rows of a tile, and the most that a piece costs (0: nothing is cut).  Sums in fp32, in one order everywhere.
+struct Cut {
+    int height, least;
+};
+template <int SOURCE> __device__ __forceinline__ Cut cut_of(const Args& a, int lane) {
+    Cut cut{a.small ? 32 : kRowTile, 0};
+    if (a.target == 0) return cut;                              // (then the host knows)
+    // costs and tiles with 128 rows, and with 32
+    float cost[2] = {0.0f, 0.0f}, tiles[2] = {0.0f, 0.0f};
+    for (int r0 = 0; r0 < a.requests; r0 += 64) {
+        float mine[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (r0 + lane < a.requests) {
+            const Request r = request_of<SOURCE>(a, r0 + lane);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int height = i ? 32 : kRowTile, n = tiles_of(a, r, height);
+                if (n > 0) {
+                    mine[i] = (float)n * (float)costs_of(a, r, n, height);
+                    mine[2 + i] = (float)n;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            cost[i] += wave_sum(mine[i]);
+            tiles[i] += wave_sum(mine[2 + i]);
+        }
+    }
+    const float heads = (float)a.kv_heads, target = (float)a.target;
+    const int small = a.small && cost[0] * heads <= (float)kSmall ? 1 : 0;
+    cut.height = small ? 32 : kRowTile;
+    // pieces of all: at most cost / least and one for each tile, together no more than fill the chip, as far as that leaves pieces to cut
+    const float least = ceilf(cost[small] * heads / fmaxf(target - tiles[small] * heads, 0.5f * target));
+    cut.least = max((int)fminf(least, 1073741824.0f), kLeastPiece);
+    cut.height = __builtin_amdgcn_readfirstlane(cut.height);
+    cut.least = __builtin_amdgcn_readfirstlane(cut.least);
+    return cut;
+}
+template <int SOURCE> __device__ __forceinline__ Shares shares_of(const Args& a, int r0, const Cut& cut, int lane) {
     Shares s{};
     s.pieces = 1;
     if (r0 + lane < a.requests) {
         s.r = request_of<SOURCE>(a, r0 + lane);
-        s.tiles = (int)(((unsigned)(s.r.lq * a.shared) + kRowTile - 1) / kRowTile);
-        if (s.tiles > 0 && least > 0) s.pieces = max((costs_of(a, s) + least - 1) / least, 1);
+        s.tiles = tiles_of(a, s.r, cut.height);
+        if (s.tiles > 0 && cut.least > 0) {
+            const int cost = costs_of(a, s.r, s.tiles, cut.height);
+            if (cost > kWhole) s.pieces = (cost + cut.least - 1) / cut.least;
+        }
     }
     return s;
 }
-// key tiles of a piece where all requests' fill the chip: sums of tiles in fp32, in one order everywhere
-template <int SOURCE> __device__ __forceinline__ int piece_tiles(const Args& a, int lane) {
-    if (a.target == 0) return 0;
-    float all = 0.0f;
-    for (int r0 = 0; r0 < a.requests; r0 += 64) {
-        const Shares s = shares_of<SOURCE>(a, r0, 0, lane);
-        float mine = 0.0f;
-        if (s.tiles > 0) mine = (float)s.tiles * (float)costs_of(a, s);
-        all += wave_sum(mine);
-    }
-    return __builtin_amdgcn_readfirstlane(max((int)fminf(ceilf(all * (float)a.kv_heads / (float)a.target), 1073741824.0f), kLeastPiece));
-}
 // JOIN: place counts the tiles of rows that are cut, otherwise blocks; both without KV heads
 template <int SOURCE, bool JOIN> __device__ __forceinline__ Work work_of(const Args& a, unsigned place, unsigned kv_head, int lane) {
-    const int least = piece_tiles<SOURCE>(a, lane);
-    Work w{-1, 0, 0, 1, 0, {}};
+    const Cut how = cut_of<SOURCE>(a, lane);
+    Work w{-1, 0, 0, 1, 0, how.height, {}};
     for (int r0 = 0, before = 0, cut_before = 0; r0 < a.requests && w.request < 0; r0 += 64) {
-        Shares s = shares_of<SOURCE>(a, r0, least, lane);
+        Shares s = shares_of<SOURCE>(a, r0, how, lane);
         int cut = s.pieces > 1 ? s.tiles * s.pieces : 0;
         const int cut_sum = lanes_scan(cut);
         // (as many as were planned for; were there more, they would be left whole)
@@ -185,7 +220,8 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t add_f16(uint32_t x, float y) {
     return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, x) + f16x2{(_Float16)y, (_Float16)y});
 }
-// codes of a word as fp16, k: c + kBias, with 4 bits in the order 0 4 1 5 2 6 3 7; v: c - kCentre
+// codes of a word as fp16, k: c + kBias, v: c - kCentre; with 4 bits in the order 0 4 1 5 2 6 3 7 (q's values are put in it beforehand, the
+// result's out of it afterwards)
 template <int BITS, bool V> __device__ __forceinline__ void widen(uint32_t w, uint32_t* to) {
     if constexpr (BITS == 8) {
         to[0] = __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u);
@@ -202,17 +238,16 @@ template <int BITS, bool V> __device__ __forceinline__ void widen(uint32_t w, ui
         for (int i = 0; i < 4; ++i) {
             if constexpr (V) x[i] = add_f16(x[i], i & 1 ? -72.0f : -1032.0f);
             else if (!(i & 1)) x[i] = add_f16(x[i], -960.0f);
-        }
-        if constexpr (V) {
-            to[0] = __builtin_amdgcn_perm(x[1], x[0], 0x05040100u);
-            to[1] = __builtin_amdgcn_perm(x[3], x[2], 0x05040100u);
-            to[2] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302u);
-            to[3] = __builtin_amdgcn_perm(x[3], x[2], 0x07060302u);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) to[i] = x[i];
+            to[i] = x[i];
         }
     }
+}
+
+// four sums of a row in each half of the wavefront, out of the order of 4 bits
+__device__ __forceinline__ f32x4 in_order(const f32x4& v) {
+    const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(v[0]), __float_as_uint(v[1]), false, false));
+    const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(v[2]), __float_as_uint(v[3]), false, false));
+    return f32x4{__uint_as_float(a[0]), __uint_as_float(b[0]), __uint_as_float(a[1]), __uint_as_float(b[1])};
 }
 
 // bytes that a thread loads at a time, as words
@@ -236,6 +271,9 @@ template <bool F16> __device__ __forceinline__ uint32_t pack(float a, float b) {
     else return f32x2_to_h16x2<false>(a, b);
 }
 
+// (what is seldom so is kept out of the way: copies of sums that the compiler puts around a branch go into it)
+__device__ __forceinline__ bool seldom(bool x) { return __builtin_expect(x, 0); }
+
 // the other half of the wavefront's
 __device__ __forceinline__ float other_half(float v) {
     const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
@@ -257,14 +295,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     const Work w = work_of<SOURCE, false>(a, place, kv_head, lane);
     if (w.request < 0) return;
     const int lq = w.r.lq, lk = w.r.lk, rows = lq * a.shared, ahead = lk - lq;
-    const Span span = span_of(a, w.r, w.tile);
+    const Span span = span_of(a, w.r, w.tile, w.height);
     const int each = (span.tiles + w.pieces - 1) / w.pieces;
     const int t_first = w.piece * each, t_end = min(span.tiles, t_first + each);
     if (w.pieces > 1 && t_first >= t_end) return;               // (the join knows)
 
     // Up to 32 rows: each wavefront takes all of them and every fourth 32 keys, otherwise 32 rows and all keys.
-    const bool narrow = rows - w.tile * kRowTile <= 32;
-    const int row0 = w.tile * kRowTile + (narrow ? 0 : 32 * wave), row = min(row0 + n, rows - 1);
+    const bool narrow = w.height == 32 || rows - w.tile * kRowTile <= 32;
+    const int row0 = w.tile * w.height + (narrow ? 0 : 32 * wave), row = min(row0 + n, rows - 1);
     const bool active = row0 < rows;
     const int query = (int)((unsigned)row / (unsigned)a.shared);
     // this row sees keys up to `lim` that lie in its window or are among the first `sinks`
@@ -477,7 +515,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     };
 
     float m_ref = -__builtin_inff(), l = 0.0f, v_sum = 0.0f;
-    int exponent = -126;                                        // of the largest vs seen; it is part of m_sub
+    int exponent = -126;                                        // of the largest vs seen
+    float m_used = CODES ? (float)with_maximum(-126) : 0.0f;    // what is taken off the scores: maximum and exponent
+    int far = 0, folds = CODES ? 1 : 0;                         // whether that is so for some row
     f32x16 o[OM];
 #pragma unroll
     for (int m = 0; m < OM; ++m)
@@ -523,7 +563,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
             const int key = 32 * u + 8 * (r >> 2) + (r & 3), last = !PAGED || ((valid >> (2 * u + (r >> 3))) & 1u) ? lim_at : -0x7FFFFFFF;
             return (bool)((int)(key <= last) & ((int)(key >= lo_at) | (int)(key < sinks_at)));
         };
-        if (!whole) {
+        if (seldom(!whole)) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -541,7 +581,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         int higher = exponent;
         if constexpr (CODES) {
             float big = *(lds_f)(scales + 512 * U);
-            if (!whole) {
+            if (seldom(!whole)) {
                 big = 0.0f;
 #pragma unroll
                 for (int u = 0; u < U; ++u)
@@ -558,8 +598,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         }
         // A weight's exponent is scale s - m_sub: a product that is not rounded, less a maximum that is.  Beyond 2^31 that rounding alone would leave
         // the exponents' range: where some row's maximum lies beyond kFar, the scores are replaced by their distance from it, both rounded alike.
-        auto m_used = [&](float m, int e) -> float { return (m == -__builtin_inff() ? 0.0f : m) + (CODES ? (float)with_maximum(e) : 0.0f); };
-        if (__builtin_amdgcn_ballot_w64(moved)) {
+        // (All that follows from the maximum and the exponent is set here: set after the branch, the compiler has the sums copied around it.)
+        if (seldom(__builtin_amdgcn_ballot_w64(moved) != 0ull)) {
             const float m_new = moved ? fmaxf(m_ref, top) : m_ref;
             const float alpha = exp2_fast(m_new > m_ref ? m_ref - m_new : 0.0f);
             const float less = CODES ? __builtin_ldexpf(1.0f, with_maximum(exponent) - with_maximum(higher)) : 1.0f;
@@ -571,9 +611,12 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
             const float f = alpha * less * fold;
 #pragma unroll
             for (int m = 0; m < OM; ++m) o[m] *= f;
+            m_used = (m_new == -__builtin_inff() ? 0.0f : m_new) + (CODES ? (float)with_maximum(higher) : 0.0f);
+            far = __builtin_amdgcn_ballot_w64(fabsf(m_used) > kFar) != 0ull ? 1 : 0;
+            if constexpr (CODES) folds = __builtin_amdgcn_ballot_w64(folded(higher) != 0) != 0ull ? 1 : 0;
         }
-        float m_sub = m_used(m_ref, exponent);
-        if (__builtin_amdgcn_ballot_w64(fabsf(m_sub) > kFar)) {
+        float m_sub = m_used;
+        if (seldom(far != 0)) {
             const float back = 1.0f / scale;
 #pragma unroll
             for (int u = 0; u < U; ++u)
@@ -587,7 +630,6 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         }
 
         u32x4 p[2 * U];
-        const bool folds = CODES && __builtin_amdgcn_ballot_w64(folded(exponent) != 0) != 0ull;
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -600,7 +642,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 }
                 if constexpr (CODES) {
                     f32x4 vs = four_of(2, u, c), vo = four_of(3, u, c);
-                    if (folds) vs *= __builtin_ldexpf(1.0f, -folded(exponent));
+                    if (seldom(folds != 0)) vs *= __builtin_ldexpf(1.0f, -folded(exponent));
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         v_sum = fmaf(e[r], vo[r], v_sum);
@@ -617,7 +659,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         before_product();
         if (CODES || !whole) {
             const unsigned long long bad = bad_of();
-            if (bad) {
+            if (seldom(bad != 0ull)) {
 #pragma unroll 1
                 for (unsigned long long left = bad; left; left &= left - 1) {
                     const int key = __builtin_ctzll(left), at = k0 + key;
@@ -675,17 +717,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 if (t_first + 1 < t_end) page = pages_of(t_first + 1);
             }
         }
-#pragma unroll 1
-        for (int t = t_first; t < t_end; ++t) {
-            const uint32_t parity = (uint32_t)(t & 1);
+        // up to where tile t is there and the loads for those behind it are on their way; whether all rows see all of it
+        auto begin = [&](int t, uint32_t parity, unsigned& valid_after) -> bool {
             const int k0 = span.real(t) * kKeys;
             const bool whole = k0 + kKeys - 1 <= all_lim && (k0 >= all_lo || k0 + kKeys <= a.sinks) && valid == 15u;
             if constexpr (!CODES) {
                 loads_left<0>();
                 if (!whole) look_at_v(parity);
             }
-            lds_barrier();                                          // tile t is there, and nobody reads the one in front of it any more
-            unsigned valid_after = 15u;
+            lds_barrier();                                          // (and nobody reads the one in front of it any more)
             if constexpr (CODES) {
                 if (t + 1 < t_end) stage(t + 1, parity ^ 1u);
                 if (t + 2 < t_end) {
@@ -698,14 +738,32 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 copy_tile(t + 1, page, parity ^ 1u);
                 if (t + 2 < t_end) page = pages_of(t + 2);
             }
-            if (active) {
-                attend(std::integral_constant<int, 2>{}, k0, parity * T::kBytes, (2 + parity) * T::kBytes, kAside + parity * kAsideBytes, valid, whole, [] {}, [] {},
-                       [&] { return bad_of_tile(parity); }, [&](unsigned long long bad) { take_out(parity, bad); });
-            } else if (!CODES && !whole) {
-                if (const unsigned long long bad = bad_of_tile(parity)) take_out(parity, bad);
+            return whole;
+        };
+        // (a loop of their own for wavefronts without rows: a branch around the sums would have them copied in every round)
+        if (active) {
+#pragma unroll 1
+            for (int t = t_first; t < t_end; ++t) {
+                const uint32_t parity = (uint32_t)(t & 1);
+                unsigned valid_after = 15u;
+                const bool whole = begin(t, parity, valid_after);
+                attend(std::integral_constant<int, 2>{}, span.real(t) * kKeys, parity * T::kBytes, (2 + parity) * T::kBytes, kAside + parity * kAsideBytes, valid,
+                       whole, [] {}, [] {}, [&] { return bad_of_tile(parity); }, [&](unsigned long long bad) { take_out(parity, bad); });
+                valid = valid_next;
+                valid_next = valid_after;
             }
-            valid = valid_next;
-            valid_next = valid_after;
+        } else {
+#pragma unroll 1
+            for (int t = t_first; t < t_end; ++t) {
+                const uint32_t parity = (uint32_t)(t & 1);
+                unsigned valid_after = 15u;
+                const bool whole = begin(t, parity, valid_after);
+                if (!CODES && !whole) {
+                    if (const unsigned long long bad = bad_of_tile(parity)) take_out(parity, bad);
+                }
+                valid = valid_next;
+                valid_next = valid_after;
+            }
         }
     };
 
@@ -914,6 +972,16 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         for (int m = 0; m < OM; ++m)
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[m][r] = fmaf(o[m][r], unfold, v_sum);
+        if constexpr (SOURCE == 4) {
+#pragma unroll
+            for (int m = 0; m < OM; ++m)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const f32x4 v = in_order(f32x4{o[m][r], o[m][r + 1], o[m][r + 2], o[m][r + 3]});
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[m][r + e] = v[e];
+                }
+        }
     }
     auto store_row = [&](int row, int four, f32x4 v) {           // four of 4 * OM, for this lane's half
         const int query_e = (int)((unsigned)row / (unsigned)a.shared), head = (int)kv_head * a.shared + (row - query_e * a.shared);
@@ -990,48 +1058,49 @@ __global__ __launch_bounds__(256) void attn_chunk_join_kernel(Args a) {
     const unsigned place = blockIdx.x / (unsigned)a.kv_heads, kv_head = blockIdx.x - place * (unsigned)a.kv_heads;
     const Work w = work_of<SOURCE, true>(a, place, kv_head, lane);
     if (w.request < 0) return;
-    const int rows = w.r.lq * a.shared, part = blockIdx.y % kWaves, row = w.tile * kRowTile + 32 * part + n;
-    const int four = 4 * (int)(blockIdx.y / kWaves) + (int)(threadIdx.x >> 6);
-    if (w.tile * kRowTile + 32 * part >= rows) return;
-    const Span span = span_of(a, w.r, w.tile);
+    const int rows = w.r.lq * a.shared, part = (int)(blockIdx.y % kWaves), row = w.tile * w.height + 32 * part + n;
+    if (32 * part >= w.height || w.tile * w.height + 32 * part >= rows) return;
+    const Span span = span_of(a, w.r, w.tile, w.height);
     const int each = (span.tiles + w.pieces - 1) / w.pieces, pieces = each > 0 ? min(w.pieces, (span.tiles + each - 1) / each) : 0;
     const int64_t step = (int64_t)a.kv_heads * kPieceFloats<D>;
     const float* first = a.partial + (int64_t)w.slot * kPieceFloats<D>;
     const float* ml = first + kRowTile * D + 2 * (32 * part + n);
-    const float* sums = first + 4 * ((part * (D / 8) + four) * 64 + lane);
-    float top = -__builtin_inff(), sum = 0.0f;
-    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int p0 = 0; p0 < pieces; p0 += kAtOnce) {
-        f32x2 x[kAtOnce];
-        f32x4 y[kAtOnce];
+    const int query = (int)((unsigned)min(row, rows - 1) / (unsigned)a.shared), head = (int)kv_head * a.shared + (min(row, rows - 1) - query * a.shared);
+    for (int four = (int)(blockIdx.y / kWaves) * 4 + (int)(threadIdx.x >> 6); four < D / 8; four += (int)(gridDim.y / kWaves) * 4) {
+        const float* sums = first + 4 * ((part * (D / 8) + four) * 64 + lane);
+        float top = -__builtin_inff(), sum = 0.0f;
+        f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int p0 = 0; p0 < pieces; p0 += kAtOnce) {
+            f32x2 x[kAtOnce];
+            f32x4 y[kAtOnce];
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            const int64_t at = min(p0 + i, pieces - 1) * step;
-            x[i] = *reinterpret_cast<const f32x2*>(ml + at);
-            y[i] = *reinterpret_cast<const f32x4*>(sums + at);
-        }
-        float higher = top;
+            for (int i = 0; i < kAtOnce; ++i) {
+                const int64_t at = min(p0 + i, pieces - 1) * step;
+                x[i] = *reinterpret_cast<const f32x2*>(ml + at);
+                y[i] = *reinterpret_cast<const f32x4*>(sums + at);
+            }
+            float higher = top;
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) higher = fmaxf(higher, x[i][0]);
-        const float use = higher == -__builtin_inff() ? 0.0f : higher, f = exp2_fast(top - use);
-        sum *= f;
-        v *= f;
-        top = higher;
+            for (int i = 0; i < kAtOnce; ++i) higher = fmaxf(higher, x[i][0]);
+            const float use = higher == -__builtin_inff() ? 0.0f : higher, f = exp2_fast(top - use);
+            sum *= f;
+            v *= f;
+            top = higher;
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            const float e = p0 + i < pieces ? exp2_fast(x[i][0] - use) : 0.0f;
-            if (e != 0.0f) {
-                sum = fmaf(e, x[i][1], sum);
+            for (int i = 0; i < kAtOnce; ++i) {
+                const float e = p0 + i < pieces ? exp2_fast(x[i][0] - use) : 0.0f;
+                if (e != 0.0f) {
+                    sum = fmaf(e, x[i][1], sum);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = fmaf(e, y[i][j], v[j]);
+                    for (int j = 0; j < 4; ++j) v[j] = fmaf(e, y[i][j], v[j]);
+                }
             }
         }
-    }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    if (row < rows) {
-        const int query = (int)((unsigned)row / (unsigned)a.shared), head = (int)kv_head * a.shared + (row - query * a.shared);
-        uint16_t* out = a.out + ((int64_t)(w.r.q_at + query) * a.heads + head) * D + 8 * four + 4 * g;
-        *reinterpret_cast<u32x2*>(out) = u32x2{pack<F16>(v[0] * inv, v[1] * inv), pack<F16>(v[2] * inv, v[3] * inv)};
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        if (row < rows) {
+            uint16_t* out = a.out + ((int64_t)(w.r.q_at + query) * a.heads + head) * D + 8 * four + 4 * g;
+            *reinterpret_cast<u32x2*>(out) = u32x2{pack<F16>(v[0] * inv, v[1] * inv), pack<F16>(v[2] * inv, v[3] * inv)};
+        }
     }
 }
 
@@ -1042,30 +1111,40 @@ template <int SOURCE, int D, bool F16> hipError_t launch(Args a, const ChunkPlan
     if (hipError_t e = ensure_lds<kernel>(bytes); e != hipSuccess) return e;
     a.target = pl.target;
     a.slots = pl.slots;
+    a.small = pl.small;
     const hipError_t e = launch_blocks(pl.blocks, kThreads, hipSuccess, [&](int64_t first, int64_t count) {
         a.first_block = (unsigned)first;
         hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(kThreads), bytes, stream, a);
         return hipGetLastError();
     });
     if (e != hipSuccess || pl.target == 0) return e;
-    hipLaunchKernelGGL((attn_chunk_join_kernel<SOURCE, D, F16>), dim3((unsigned)pl.cut_tiles, (unsigned)(kWaves * D / 32)), dim3(256), 0, stream, a);
+    // 32 rows and all places a block; few tiles of rows: a quarter (half) of the places each
+    const unsigned parts = pl.cut_tiles <= 256 ? D / 32 : 1;
+    hipLaunchKernelGGL((attn_chunk_join_kernel<SOURCE, D, F16>), dim3((unsigned)pl.cut_tiles, kWaves * parts), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-ChunkPlan plan_attn_chunk(int64_t requests, int64_t q_tokens, int heads, int kv_heads, int head_dim, int64_t max_tokens, int cus) {
+ChunkPlan plan_attn_chunk(int64_t requests, int64_t q_tokens, int heads, int kv_heads, int head_dim, int64_t max_tokens, bool cut, int cus) {
     ChunkPlan p{};
     const int64_t shared = heads / kv_heads, some = requests < q_tokens ? requests : q_tokens;
-    const int64_t tiles = (q_tokens * shared / kRowTile + some) * kv_heads, units = (max_tokens + kKeys - 1) / kKeys;
+    auto tiles_of = [&](int height) { return (q_tokens * shared / height + some) * kv_heads; };
+    int64_t tiles = tiles_of(kRowTile);
+    const int64_t units = (max_tokens + kKeys - 1) / kKeys;
+    const bool cuts = cut && units > kWhole;
+    // small for sure, or (a call of so few rows) if its requests are short
+    p.small = (cuts ? q_tokens * shared / kRowTile * kv_heads : tiles * units) <= kSmall;
+    if (p.small) tiles = tiles_of(32);
     p.blocks = tiles;
-    if (units <= kLeastPiece) return p;
+    if (!cuts) return p;
     p.target = 2 * cus;
-    // A request is cut where its tiles of rows have more tiles of keys than a piece; a piece has so many that all pieces would be `target`, so that
-    // there are fewer than twice as many of the cut ones; and no more than the longest requests' own.
-    const int64_t most = 2 * (int64_t)p.target + kv_heads, own = tiles * ((units + kLeastPiece - 1) / kLeastPiece);
+    // (pieces of tiles that are cut: cut_of() has it that there are no more than that, but for the rounding of its sums)
+    const int64_t most = (int64_t)p.target + kv_heads, own = tiles * ((units + kLeastPiece - 1) / kLeastPiece);
     p.slots = (int)(own < most ? own : most);
-    p.cut_tiles = (int)(tiles < p.target + kv_heads ? tiles : p.target + kv_heads);
+    // (each in two pieces and more)
+    const int64_t cut_tiles = p.slots / 2 + kv_heads;
+    p.cut_tiles = (int)(tiles < cut_tiles ? tiles : cut_tiles);
     p.blocks = tiles + p.slots;
     p.workspace = (size_t)p.slots * kRowTile * (head_dim + 2) * sizeof(float);
     return p;
@@ -1073,7 +1152,7 @@ ChunkPlan plan_attn_chunk(int64_t requests, int64_t q_tokens, int heads, int kv_
 
 hipError_t launch_attn_chunk(const ChunkArgs& c, const any4_kv_cache* cache, const ChunkPlan& pl, void* workspace, hipStream_t stream) {
     Args a{c.q, c.k, c.v, {}, c.table, c.table_stride, (int)c.table_width, c.q_starts, c.k_starts, c.lengths, (int)c.q_tokens, (int)c.k_tokens, c.requests,
-           c.heads, c.kv_heads, c.heads / c.kv_heads, c.window > 0 ? c.window : kNoWindow, c.sinks, 0, 0, 0u, c.softmax_scale * kLog2e, c.out,
+           c.heads, c.kv_heads, c.heads / c.kv_heads, c.window > 0 ? c.window : kNoWindow, c.sinks, 0, 0, 0, 0u, c.softmax_scale * kLog2e, c.out,
            static_cast<float*>(workspace)};
     if (cache) a.c = kv_pages(*cache);
     auto types = [&](auto source, auto dim) {
