@@ -106,7 +106,7 @@ struct Work {
 };
 struct Shares {                        // of 64 requests, a lane each
     Request r;
-    int tiles, pieces;
+    int request, tiles, pieces, cost;  // cost: of a piece
 };
 // what a request's last (and longest) tile of rows costs, in tiles of keys for 128 rows
 __device__ __forceinline__ int costs_of(const Args& a, const Request& r, int tiles, int height) {
@@ -118,10 +118,10 @@ __device__ __forceinline__ int tiles_of(const Args& a, const Request& r, int hei
 }
 // How a call is cut: rows of a tile, and the most that a piece costs (0: nothing is cut).  Sums in fp32, in one order everywhere.
 struct Cut {
-    int height, least;
+    int height, least, rounds;         // rounds: whether blocks outnumber those that fill the chip
 };
 template <int SOURCE> __device__ __forceinline__ Cut cut_of(const Args& a, int lane) {
-    Cut cut{a.small ? 32 : kRowTile, 0};
+    Cut cut{a.small ? 32 : kRowTile, 0, 1};
     if (a.target == 0) return cut;                              // (then the host knows)
     // costs and tiles with 128 rows, and with 32
     float cost[2] = {0.0f, 0.0f}, tiles[2] = {0.0f, 0.0f};
@@ -150,6 +150,18 @@ template <int SOURCE> __device__ __forceinline__ Cut cut_of(const Args& a, int l
     // pieces of all: at most cost / least and one for each tile, together no more than fill the chip, as far as that leaves pieces to cut
     const float least = ceilf(cost[small] * heads / fmaxf(target - tiles[small] * heads, 0.5f * target));
     cut.least = max((int)fminf(least, 1073741824.0f), kLeastPiece);
+    if (a.requests <= 64) {
+        // that counts a piece's rounding up as a whole one: as long as shorter pieces are no more than fill the chip, they are taken
+        Request r{};
+        if (lane < a.requests) r = request_of<SOURCE>(a, lane);
+        const int height = small ? 32 : kRowTile, n = tiles_of(a, r, height), own = n > 0 ? costs_of(a, r, n, height) : 0;
+        for (int shorter = cut.least - (cut.least + 15) / 16; shorter >= kLeastPiece; shorter -= (cut.least + 15) / 16) {
+            const float pieces = wave_sum(own > kWhole ? (float)n * (float)((own + shorter - 1) / shorter) : (float)n);
+            if (!(pieces * heads <= target)) break;
+            cut.least = shorter;
+        }
+    }
+    cut.rounds = __builtin_amdgcn_readfirstlane(tiles[small] * heads > target ? 1 : 0);
     cut.height = __builtin_amdgcn_readfirstlane(cut.height);
     cut.least = __builtin_amdgcn_readfirstlane(cut.least);
     return cut;
@@ -157,15 +169,29 @@ template <int SOURCE> __device__ __forceinline__ Cut cut_of(const Args& a, int l
 template <int SOURCE> __device__ __forceinline__ Shares shares_of(const Args& a, int r0, const Cut& cut, int lane) {
     Shares s{};
     s.pieces = 1;
+    s.request = r0 + lane;
     if (r0 + lane < a.requests) {
         s.r = request_of<SOURCE>(a, r0 + lane);
         s.tiles = tiles_of(a, s.r, cut.height);
-        if (s.tiles > 0 && cut.least > 0) {
-            const int cost = costs_of(a, s.r, s.tiles, cut.height);
-            if (cost > kWhole) s.pieces = (cost + cut.least - 1) / cut.least;
+        if (s.tiles > 0) {
+            s.cost = costs_of(a, s.r, s.tiles, cut.height);
+            if (cut.least > 0 && s.cost > kWhole) {
+                s.pieces = (s.cost + cut.least - 1) / cut.least;
+                s.cost = cut.least;
+            }
         }
     }
     return s;
+}
+// The dearest requests first, of up to 64: blocks are begun in their order, and what is begun last should end soon.
+__device__ __forceinline__ void dearest_first(Shares& s, int requests, int lane) {
+    int rank = 0;
+    for (int i = 0; i < requests; ++i) {
+        const int other = __builtin_amdgcn_readlane(s.cost, i);
+        rank += other > s.cost || (other == s.cost && i < lane) ? 1 : 0;
+    }
+    if (lane >= requests) rank = lane;
+    for (int* x : {&s.r.q_at, &s.r.lq, &s.r.k_at, &s.r.lk, &s.request, &s.tiles, &s.pieces, &s.cost}) *x = __builtin_amdgcn_ds_permute(4 * rank, *x);
 }
 // JOIN: place counts the tiles of rows that are cut, otherwise blocks; both without KV heads
 template <int SOURCE, bool JOIN> __device__ __forceinline__ Work work_of(const Args& a, unsigned place, unsigned kv_head, int lane) {
@@ -173,6 +199,7 @@ template <int SOURCE, bool JOIN> __device__ __forceinline__ Work work_of(const A
     Work w{-1, 0, 0, 1, 0, how.height, {}};
     for (int r0 = 0, before = 0, cut_before = 0; r0 < a.requests && w.request < 0; r0 += 64) {
         Shares s = shares_of<SOURCE>(a, r0, how, lane);
+        if (how.rounds && a.requests > 1 && a.requests <= 64) dearest_first(s, a.requests, lane);
         int cut = s.pieces > 1 ? s.tiles * s.pieces : 0;
         const int cut_sum = lanes_scan(cut);
         // (as many as were planned for; were there more, they would be left whole)
@@ -184,7 +211,7 @@ template <int SOURCE, bool JOIN> __device__ __forceinline__ Work work_of(const A
         const unsigned long long past = __builtin_amdgcn_ballot_w64((unsigned)(before + sum) > place);
         if (past) {
             const int f = __builtin_ctzll(past);
-            w.request = r0 + f;
+            w.request = __builtin_amdgcn_readlane(s.request, f);
             w.r.q_at = __builtin_amdgcn_readlane(s.r.q_at, f);
             w.r.lq = __builtin_amdgcn_readlane(s.r.lq, f);
             w.r.k_at = __builtin_amdgcn_readlane(s.r.k_at, f);
@@ -531,6 +558,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         constexpr int U = decltype(blocks)::value;
         // four tokens' of an array of scales: keys 32 u + 8 c + 4 g ..
         auto four_of = [&](int array, int u, int c) -> f32x4 { return *(lds_f4)(scales + (uint32_t)(128 * U * array + 4 * (32 * u + 8 * c)) + 16u * (uint32_t)g); };
+        // The two wavefronts of a SIMD take turns at its matrix cores and its vector units: one that turns scores into weights goes first, so that its
+        // products come while the other is at its scores or weights.  (2048 tokens behind 30720 in 16 bits 1063 -> 1004 us, with the priority until behind
+        // the product 1030; a mixed batch in 8 bits 451 and 434 the other way round.  Heads of 64 have a third wavefront and lose 4 % by it.)
+        constexpr bool kFirst = D == 128;
         f32x16 s[U];
         uint32_t k_at = k_lane + k_buf, v_at = v_lane + v_buf;
         asm volatile("" : "+v"(k_at), "+v"(v_at));               // (or every operand's address is kept in a register)
@@ -543,8 +574,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 const u32x4 k = *(lds_u4)((k_at ^ (uint32_t)(i << 5)) + (uint32_t)(u * 32 * T::kRow));
                 s[u] = mma32<MMA16>(k, q[i], s[u]);
             }
-            if (CODES) __builtin_amdgcn_sched_barrier(0);       // (or operands of all products are fetched at once, into registers that are not there)
         }
+        if constexpr (kFirst) __builtin_amdgcn_s_setprio(1);
         if constexpr (CODES) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
@@ -553,7 +584,6 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                     const f32x4 ks = four_of(0, u, c), ko = four_of(1, u, c);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) s[u][4 * c + r] = fmaf(ks[r], s[u][4 * c + r], ko[r] * sum_q);
-                    if (c & 1) __builtin_amdgcn_sched_barrier(0);
                 }
         }
         after_scores();
@@ -651,7 +681,6 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 }
                 p[2 * u + (c >> 1)][2 * (c & 1)] = pack<MMA16>(e[0], e[1]);
                 p[2 * u + (c >> 1)][2 * (c & 1) + 1] = pack<MMA16>(e[2], e[3]);
-                if (CODES && (c & 1)) __builtin_amdgcn_sched_barrier(0);
             }
 
         // 0 times what is not finite would be NaN: tokens with such a v (in tiles that not all rows see, with codes in all) are added one by one to
@@ -690,10 +719,12 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 if constexpr (!CODES) take_out(bad);
             }
         }
+        if constexpr (kFirst && !CODES) __builtin_amdgcn_s_setprio(0);
 #pragma unroll
         for (int c = 0; c < 2 * U; ++c)
 #pragma unroll
             for (int m = 0; m < OM; ++m) o[m] = mma32<MMA16>(v_operand(v_at, c, m), p[c], o[m]);
+        if constexpr (kFirst && CODES) __builtin_amdgcn_s_setprio(0);
     };
 
     auto wide_rows = [&] {
@@ -1050,7 +1081,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     }
 }
 
-// Joins the pieces of tiles of rows that were cut: a wavefront has 32 rows and four values of each, in the pieces' own order of lanes.
+// Joins the pieces of tiles of rows that were cut: a wavefront has 32 rows at a time and four values of each, in the pieces' own order of lanes.
 constexpr int kAtOnce = 16;                                     // pieces whose loads are out at a time
 template <int SOURCE, int D, bool F16>
 __global__ __launch_bounds__(256) void attn_chunk_join_kernel(Args a) {
@@ -1058,15 +1089,16 @@ __global__ __launch_bounds__(256) void attn_chunk_join_kernel(Args a) {
     const unsigned place = blockIdx.x / (unsigned)a.kv_heads, kv_head = blockIdx.x - place * (unsigned)a.kv_heads;
     const Work w = work_of<SOURCE, true>(a, place, kv_head, lane);
     if (w.request < 0) return;
-    const int rows = w.r.lq * a.shared, part = (int)(blockIdx.y % kWaves), row = w.tile * w.height + 32 * part + n;
-    if (32 * part >= w.height || w.tile * w.height + 32 * part >= rows) return;
+    const int rows = w.r.lq * a.shared;
     const Span span = span_of(a, w.r, w.tile, w.height);
     const int each = (span.tiles + w.pieces - 1) / w.pieces, pieces = each > 0 ? min(w.pieces, (span.tiles + each - 1) / each) : 0;
     const int64_t step = (int64_t)a.kv_heads * kPieceFloats<D>;
     const float* first = a.partial + (int64_t)w.slot * kPieceFloats<D>;
-    const float* ml = first + kRowTile * D + 2 * (32 * part + n);
-    const int query = (int)((unsigned)min(row, rows - 1) / (unsigned)a.shared), head = (int)kv_head * a.shared + (min(row, rows - 1) - query * a.shared);
-    for (int four = (int)(blockIdx.y / kWaves) * 4 + (int)(threadIdx.x >> 6); four < D / 8; four += (int)(gridDim.y / kWaves) * 4) {
+    const int four = 4 * (int)blockIdx.y + (int)(threadIdx.x >> 6);
+    for (int part = 0; 32 * part < w.height && w.tile * w.height + 32 * part < rows; ++part) {
+        const int row = w.tile * w.height + 32 * part + n;
+        const float* ml = first + kRowTile * D + 2 * (32 * part + n);
+        const int query = (int)((unsigned)min(row, rows - 1) / (unsigned)a.shared), head = (int)kv_head * a.shared + (min(row, rows - 1) - query * a.shared);
         const float* sums = first + 4 * ((part * (D / 8) + four) * 64 + lane);
         float top = -__builtin_inff(), sum = 0.0f;
         f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -1118,9 +1150,7 @@ template <int SOURCE, int D, bool F16> hipError_t launch(Args a, const ChunkPlan
         return hipGetLastError();
     });
     if (e != hipSuccess || pl.target == 0) return e;
-    // 32 rows and all places a block; few tiles of rows: a quarter (half) of the places each
-    const unsigned parts = pl.cut_tiles <= 256 ? D / 32 : 1;
-    hipLaunchKernelGGL((attn_chunk_join_kernel<SOURCE, D, F16>), dim3((unsigned)pl.cut_tiles, kWaves * parts), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((attn_chunk_join_kernel<SOURCE, D, F16>), dim3((unsigned)pl.cut_tiles, D / 32), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
