@@ -60,6 +60,10 @@ struct Args {
     float scale_log2;
     uint16_t* out;
     float* partial;
+    // row / shared by a product: with 2^(s - 1) < shared <= 2^s and mul = 2^(31 + s) / shared rounded up, below 2^32, exact for rows below 2^31
+    uint32_t shared_mul;
+    int shared_shift;                  // 31 + s
+    __device__ __forceinline__ int query_of(int row) const { return (int)(((uint64_t)(uint32_t)row * shared_mul) >> shared_shift); }
 };
 
 // A request's rows and keys.
@@ -89,8 +93,8 @@ struct Span {
 __device__ __forceinline__ Span span_of(const Args& a, const Request& r, int tile, int height) {
     Span s;
     const int rows = r.lq * a.shared, ahead = r.lk - r.lq;
-    s.first = (int)((unsigned)(tile * height) / (unsigned)a.shared);
-    s.last = (int)((unsigned)(min(tile * height + height, rows) - 1) / (unsigned)a.shared);
+    s.first = a.query_of(tile * height);
+    s.last = a.query_of(min(tile * height + height, rows) - 1);
     const int end = s.end = max(ahead + s.last + 1, 0), start = max(max(ahead + s.first, 0) + 1 - a.window, 0);
     const int begin = start / kKeys;
     s.front = min((int)(((unsigned)min(a.sinks, end) + kKeys - 1) / kKeys), begin);
@@ -106,7 +110,7 @@ struct Work {
 };
 struct Shares {                        // of 64 requests, a lane each
     Request r;
-    int request, tiles, pieces, cost;  // cost: of a piece
+    int tiles, pieces;
 };
 // what a request's last (and longest) tile of rows costs, in tiles of keys for 128 rows
 __device__ __forceinline__ int costs_of(const Args& a, const Request& r, int tiles, int height) {
@@ -118,88 +122,79 @@ __device__ __forceinline__ int tiles_of(const Args& a, const Request& r, int hei
 }
 // How a call is cut: rows of a tile, and the most that a piece costs (0: nothing is cut).  Sums in fp32, in one order everywhere.
 struct Cut {
-    int height, least, rounds;         // rounds: whether blocks outnumber those that fill the chip
+    int height, least;
 };
-template <int SOURCE> __device__ __forceinline__ Cut cut_of(const Args& a, int lane) {
-    Cut cut{a.small ? 32 : kRowTile, 0, 1};
+// over all lanes, in each of them
+__device__ __forceinline__ float lanes_total(float v) {
+    auto add = [&](auto ctrl, auto rows) { v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), decltype(ctrl)::value, decltype(rows)::value, 0xF, true)); };
+    add(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xF>{});       // row_shr:1
+    add(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xF>{});
+    add(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xF>{});
+    add(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xF>{});
+    add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});       // row_bcast:15
+    add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});       // row_bcast:31
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
+}
+// `first`: this lane's of the first 64 requests
+template <int SOURCE> __device__ __forceinline__ Cut cut_of(const Args& a, const Request& first, int lane) {
+    Cut cut{a.small ? 32 : kRowTile, 0};
     if (a.target == 0) return cut;                              // (then the host knows)
-    // costs and tiles with 128 rows, and with 32
-    float cost[2] = {0.0f, 0.0f}, tiles[2] = {0.0f, 0.0f};
-    for (int r0 = 0; r0 < a.requests; r0 += 64) {
-        float mine[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (r0 + lane < a.requests) {
-            const Request r = request_of<SOURCE>(a, r0 + lane);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int height = i ? 32 : kRowTile, n = tiles_of(a, r, height);
-                if (n > 0) {
-                    mine[i] = (float)n * (float)costs_of(a, r, n, height);
-                    mine[2 + i] = (float)n;
-                }
+    const float heads = (float)a.kv_heads, target = (float)a.target;
+    float cost = 0.0f, tiles = 0.0f;
+    auto add_up = [&](int height) {
+        cost = tiles = 0.0f;
+        for (int r0 = 0; r0 < a.requests; r0 += 64) {
+            Request r = first;
+            if (r0 > 0) r = r0 + lane < a.requests ? request_of<SOURCE>(a, r0 + lane) : Request{};
+            const int n = tiles_of(a, r, height);
+            cost += lanes_total(n > 0 ? (float)n * (float)costs_of(a, r, n, height) : 0.0f);
+            tiles += lanes_total((float)n);
+        }
+    };
+    add_up(kRowTile);
+    cut.height = kRowTile;
+    if (a.small && cost * heads <= (float)kSmall) {
+        cut.height = 32;
+        add_up(32);
+    }
+    // Pieces of all: at most cost / least and one for each tile, together no more than fill the chip, as far as that leaves pieces to cut.  That counts a
+    // piece's rounding up as a whole one: up to 64 requests' are counted, and shorter pieces taken as far as they are no more than that.
+    const float all = cost * heads, limit = 1073741824.0f;
+    const int most = max((int)fminf(ceilf(all / fmaxf(target - tiles * heads, 0.5f * target)), limit), kLeastPiece);
+    const int low = max((int)fminf(ceilf(all / target), limit), kLeastPiece);
+    cut.least = most;
+    if (a.requests <= 64) {
+        const int n = tiles_of(a, first, cut.height), own = n > 0 ? costs_of(a, first, n, cut.height) : 0;
+        for (int third = 0; third < 3; ++third) {
+            const int shorter = low + (most - low) * third / 3;
+            if (shorter >= most) break;
+            if (lanes_total(own > kWhole ? (float)n * (float)((own + shorter - 1) / shorter) : (float)n) * heads <= target) {
+                cut.least = shorter;
+                break;
             }
         }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            cost[i] += wave_sum(mine[i]);
-            tiles[i] += wave_sum(mine[2 + i]);
-        }
     }
-    const float heads = (float)a.kv_heads, target = (float)a.target;
-    const int small = a.small && cost[0] * heads <= (float)kSmall ? 1 : 0;
-    cut.height = small ? 32 : kRowTile;
-    // pieces of all: at most cost / least and one for each tile, together no more than fill the chip, as far as that leaves pieces to cut
-    const float least = ceilf(cost[small] * heads / fmaxf(target - tiles[small] * heads, 0.5f * target));
-    cut.least = max((int)fminf(least, 1073741824.0f), kLeastPiece);
-    if (a.requests <= 64) {
-        // that counts a piece's rounding up as a whole one: as long as shorter pieces are no more than fill the chip, they are taken
-        Request r{};
-        if (lane < a.requests) r = request_of<SOURCE>(a, lane);
-        const int height = small ? 32 : kRowTile, n = tiles_of(a, r, height), own = n > 0 ? costs_of(a, r, n, height) : 0;
-        for (int shorter = cut.least - (cut.least + 15) / 16; shorter >= kLeastPiece; shorter -= (cut.least + 15) / 16) {
-            const float pieces = wave_sum(own > kWhole ? (float)n * (float)((own + shorter - 1) / shorter) : (float)n);
-            if (!(pieces * heads <= target)) break;
-            cut.least = shorter;
-        }
-    }
-    cut.rounds = __builtin_amdgcn_readfirstlane(tiles[small] * heads > target ? 1 : 0);
     cut.height = __builtin_amdgcn_readfirstlane(cut.height);
     cut.least = __builtin_amdgcn_readfirstlane(cut.least);
     return cut;
 }
-template <int SOURCE> __device__ __forceinline__ Shares shares_of(const Args& a, int r0, const Cut& cut, int lane) {
-    Shares s{};
-    s.pieces = 1;
-    s.request = r0 + lane;
-    if (r0 + lane < a.requests) {
-        s.r = request_of<SOURCE>(a, r0 + lane);
-        s.tiles = tiles_of(a, s.r, cut.height);
-        if (s.tiles > 0) {
-            s.cost = costs_of(a, s.r, s.tiles, cut.height);
-            if (cut.least > 0 && s.cost > kWhole) {
-                s.pieces = (s.cost + cut.least - 1) / cut.least;
-                s.cost = cut.least;
-            }
-        }
+__device__ __forceinline__ Shares shares_of(const Args& a, const Request& r, const Cut& cut) {
+    Shares s{r, tiles_of(a, r, cut.height), 1};
+    if (s.tiles > 0 && cut.least > 0) {
+        const int cost = costs_of(a, r, s.tiles, cut.height);
+        if (cost > kWhole) s.pieces = (cost + cut.least - 1) / cut.least;
     }
     return s;
 }
-// The dearest requests first, of up to 64: blocks are begun in their order, and what is begun last should end soon.
-__device__ __forceinline__ void dearest_first(Shares& s, int requests, int lane) {
-    int rank = 0;
-    for (int i = 0; i < requests; ++i) {
-        const int other = __builtin_amdgcn_readlane(s.cost, i);
-        rank += other > s.cost || (other == s.cost && i < lane) ? 1 : 0;
-    }
-    if (lane >= requests) rank = lane;
-    for (int* x : {&s.r.q_at, &s.r.lq, &s.r.k_at, &s.r.lk, &s.request, &s.tiles, &s.pieces, &s.cost}) *x = __builtin_amdgcn_ds_permute(4 * rank, *x);
-}
 // JOIN: place counts the tiles of rows that are cut, otherwise blocks; both without KV heads
 template <int SOURCE, bool JOIN> __device__ __forceinline__ Work work_of(const Args& a, unsigned place, unsigned kv_head, int lane) {
-    const Cut how = cut_of<SOURCE>(a, lane);
+    const Request first = lane < a.requests ? request_of<SOURCE>(a, lane) : Request{};
+    const Cut how = cut_of<SOURCE>(a, first, lane);
     Work w{-1, 0, 0, 1, 0, how.height, {}};
     for (int r0 = 0, before = 0, cut_before = 0; r0 < a.requests && w.request < 0; r0 += 64) {
-        Shares s = shares_of<SOURCE>(a, r0, how, lane);
-        if (how.rounds && a.requests > 1 && a.requests <= 64) dearest_first(s, a.requests, lane);
+        Request r = first;
+        if (r0 > 0) r = r0 + lane < a.requests ? request_of<SOURCE>(a, r0 + lane) : Request{};
+        Shares s = shares_of(a, r, how);
         int cut = s.pieces > 1 ? s.tiles * s.pieces : 0;
         const int cut_sum = lanes_scan(cut);
         // (as many as were planned for; were there more, they would be left whole)
@@ -211,7 +206,7 @@ template <int SOURCE, bool JOIN> __device__ __forceinline__ Work work_of(const A
         const unsigned long long past = __builtin_amdgcn_ballot_w64((unsigned)(before + sum) > place);
         if (past) {
             const int f = __builtin_ctzll(past);
-            w.request = __builtin_amdgcn_readlane(s.request, f);
+            w.request = r0 + f;
             w.r.q_at = __builtin_amdgcn_readlane(s.r.q_at, f);
             w.r.lq = __builtin_amdgcn_readlane(s.r.lq, f);
             w.r.k_at = __builtin_amdgcn_readlane(s.r.k_at, f);
@@ -229,6 +224,10 @@ template <int SOURCE, bool JOIN> __device__ __forceinline__ Work work_of(const A
     }
     return w;
 }
+
+// How v's pieces of 16 bytes lie in a tile's row: four neighbouring rows' in different banks for the transposing reads, and in the last two bits in
+// different ones for the writes of widened codes, whose lanes have pieces four (two) apart.
+template <int D> __device__ __forceinline__ constexpr int swizzle_v(int row) { return D == 128 ? 5 * (row & 3) : ((row >> 1) & 1) << 2 | ((row >> 1) & 3); }
 
 // LDS aside from the tiles.  Scales of TOKENS tokens: k's scale and offset, v's likewise, the largest of the third, whose v's are not finite.
 template <int TOKENS> constexpr int kScaleBytes = 16 * TOKENS + 16;
@@ -331,7 +330,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     const bool narrow = w.height == 32 || rows - w.tile * kRowTile <= 32;
     const int row0 = w.tile * w.height + (narrow ? 0 : 32 * wave), row = min(row0 + n, rows - 1);
     const bool active = row0 < rows;
-    const int query = (int)((unsigned)row / (unsigned)a.shared);
+    const int query = a.query_of(row);
     // this row sees keys up to `lim` that lie in its window or are among the first `sinks`
     const int lim = ahead + query;
     // all rows see keys up to `all_lim` that lie at `all_lo` or behind it or are among the first
@@ -416,7 +415,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
             const uint32_t from = (uint32_t)min(r - base, lk - 1 - first);
             const uint32_t to = parity * T::kBytes + (uint32_t)(T::kCopies * wave + j) * 1024u;
             copy_to_lds(to, kb, from * k_step + 16u * (uint32_t)(copy_piece ^ T::swizzle_k(r)));
-            copy_to_lds(to + 2 * T::kBytes, vb, from * v_step + 16u * (uint32_t)(copy_piece ^ T::swizzle_v(r)));
+            copy_to_lds(to + 2 * T::kBytes, vb, from * v_step + 16u * (uint32_t)(copy_piece ^ swizzle_v<D>(r)));
         }
     };
     // which of this wavefront's 16 rows of a tile of v are not finite
@@ -488,7 +487,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     // (the first row's first piece; the others' follow from it by an exclusive or and a constant)
     const int stage_row = (int)threadIdx.x / kLanesRow, stage_piece = (int)(threadIdx.x % kLanesRow) * (kCodes / 8);
     const uint32_t to_k = (uint32_t)(stage_row * T::kRow) + 16u * (uint32_t)(stage_piece ^ T::swizzle_k(stage_row));
-    const uint32_t to_v = 2 * T::kBytes + (uint32_t)(stage_row * T::kRow) + 16u * (uint32_t)(stage_piece ^ T::swizzle_v(stage_row));
+    const uint32_t to_v = 2 * T::kBytes + (uint32_t)(stage_row * T::kRow) + 16u * (uint32_t)(stage_piece ^ swizzle_v<D>(stage_row));
     auto stage = [&](int t, uint32_t parity) {
         if constexpr (CODES) {
 #pragma unroll
@@ -503,7 +502,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                     }
 #pragma unroll
                     for (int x = 0; x < kCodes / 8; ++x) {
-                        const uint32_t other = 16u * (uint32_t)(x ^ (of_v ? T::swizzle_v(i * kPassRows) : T::swizzle_k(i * kPassRows)));
+                        const uint32_t other = 16u * (uint32_t)(x ^ (of_v ? swizzle_v<D>(i * kPassRows) : T::swizzle_k(i * kPassRows)));
                         *(lds_u4)((((of_v ? to_v : to_k) + parity * T::kBytes) ^ other) + (uint32_t)(i * kPassRows * T::kRow)) = u32x4{wide[4 * x], wide[4 * x + 1], wide[4 * x + 2], wide[4 * x + 3]};
                     }
                 }
@@ -534,7 +533,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     // times 16 bytes put in the same way
     const int i16 = lane & 15, v_row = 4 * g + (i16 >> 2);
     const uint32_t k_lane = (uint32_t)(n * T::kRow + ((g ^ T::swizzle_k(n)) << 4));
-    const uint32_t v_lane = (uint32_t)(v_row * T::kRow + 8 * (i16 & 1) + (((2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1)) ^ T::swizzle_v(v_row)) << 4));
+    const uint32_t v_lane = (uint32_t)(v_row * T::kRow + 8 * (i16 & 1) + (((2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1)) ^ swizzle_v<D>(v_row)) << 4));
     auto v_operand = [&](uint32_t first, int c, int m) -> u32x4 {
         const uint32_t at = (first ^ (uint32_t)(m << 6)) + (uint32_t)(c * 16 * T::kRow);
         const u32x2 lo = lds_read_transposed(at), hi = lds_read_transposed(at + 8 * T::kRow);
@@ -706,7 +705,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                         for (int m = 0; m < OM; ++m)
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
-                                const uint32_t piece = (uint32_t)((4 * m + r) ^ T::swizzle_v(key));
+                                const uint32_t piece = (uint32_t)((4 * m + r) ^ swizzle_v<D>(key));
                                 const u32x2 v = *(lds_u2)(v_buf + (uint32_t)(key * T::kRow) + 16u * piece + 8u * (uint32_t)g);
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) {
@@ -811,15 +810,26 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         auto pages_of_half = [&](int h) -> Two {
             Two two{{0, 0}};
             if constexpr (PAGED) {
+                // codes: loads of the lanes' (a scalar load would be waited for at the next wait for LDS); 16 bits: scalar ones (the others' wait would
+                // be one for the copies that the compiler does not see)
                 const auto entries = (const __attribute__((address_space(4))) int32_t*)reinterpret_cast<uintptr_t>(table);
                 const int k0 = key_of(h);
+                int zero = 0;
+                if constexpr (CODES) asm volatile("" : "+v"(zero));
 #pragma unroll
-                for (int i = 0; i < 2; ++i) two.page[i] = entries[min(k0 + 16 * i, lk - 1) >> a.c.page_shift];
+                for (int i = 0; i < 2; ++i) {
+                    const int at = min(k0 + 16 * i, lk - 1) >> a.c.page_shift;
+                    two.page[i] = CODES ? table[at + zero] : entries[at];
+                }
             }
             return two;
         };
-        auto valid_of_half = [&](const Two& two) -> unsigned { return (there(two.page[0]) ? 1u : 0u) | (there(two.page[1]) ? 2u : 0u); };
-        auto first_of = [&](const Two& two, int i) -> int64_t { return PAGED ? a.c.first_token(there(two.page[i]) ? two.page[i] : 0, (int)kv_head) : 0; };
+        auto page_of = [&](const Two& two, int i) -> int { return CODES ? __builtin_amdgcn_readfirstlane(two.page[i]) : two.page[i]; };
+        auto valid_of_half = [&](const Two& two) -> unsigned { return (there(page_of(two, 0)) ? 1u : 0u) | (there(page_of(two, 1)) ? 2u : 0u); };
+        auto first_of = [&](const Two& two, int i) -> int64_t {
+            const int page = page_of(two, i);
+            return PAGED ? a.c.first_token(there(page) ? page : 0, (int)kv_head) : 0;
+        };
 
         // 16 bits: 64 lanes copy kRows rows at a time
         auto copy_half = [&](int h, const Two& two, bool of_v) {
@@ -829,7 +839,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
             for (int j = 0; j < (int)kCopies; ++j) {
                 const int first = j * T::kRows, r = first + lane / T::kPieces, i = first / 16;
                 const int tok = min(k0 + r, lk - 1);
-                const uint32_t piece = 16u * (uint32_t)(copy_piece ^ (of_v ? T::swizzle_v(r) : T::swizzle_k(r)));
+                const uint32_t piece = 16u * (uint32_t)(copy_piece ^ (of_v ? swizzle_v<D>(r) : T::swizzle_k(r)));
                 const uint32_t to = (of_v ? v_buf : k_buf) + 1024u * (uint32_t)j;
                 if constexpr (SOURCE == kRows) {
                     const Rows& rows_of = of_v ? a.v : a.k;
@@ -888,7 +898,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
             constexpr int BITS = CODES ? SOURCE : 8;
             // (the first row's first piece; a register of its own in each round, as the others' would be if they were kept)
             const int r0 = lane / kRowLanes, piece0 = (lane % kRowLanes) * (kPer / 8);
-            uint32_t to = (V ? v_buf : k_buf) + (uint32_t)(r0 * T::kRow) + 16u * (uint32_t)(piece0 ^ (V ? T::swizzle_v(r0) : T::swizzle_k(r0)));
+            uint32_t to = (V ? v_buf : k_buf) + (uint32_t)(r0 * T::kRow) + 16u * (uint32_t)(piece0 ^ (V ? swizzle_v<D>(r0) : T::swizzle_k(r0)));
             asm volatile("" : "+v"(to));
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
@@ -897,7 +907,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 for (int x = 0; x < 4; ++x) widen<BITS, V>(from[i][x], wide + x * 16 / BITS);
 #pragma unroll
                 for (int x = 0; x < kPer / 8; ++x) {
-                    const uint32_t other = 16u * (uint32_t)(x ^ (V ? T::swizzle_v(i * kRowsAtOnce) : T::swizzle_k(i * kRowsAtOnce)));
+                    const uint32_t other = 16u * (uint32_t)(x ^ (V ? swizzle_v<D>(i * kRowsAtOnce) : T::swizzle_k(i * kRowsAtOnce)));
                     *(lds_u4)((to ^ other) + (uint32_t)(i * kRowsAtOnce * T::kRow)) = u32x4{wide[4 * x], wide[4 * x + 1], wide[4 * x + 2], wide[4 * x + 3]};
                 }
             }
@@ -938,10 +948,12 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                     load_half(h + kWaves, two, false, raw_k);
                     load_half(h + kWaves, two, true, raw_v);
                     load_scales(h + kWaves, two);
+                    if (h + 2 * kWaves < h_end) two = pages_of_half(h + 2 * kWaves);
                 }
             } else {
                 copy_half(h, two, false);
                 copy_half(h, two, true);
+                if (h + kWaves < h_end) two = pages_of_half(h + kWaves);
             }
         }
 #pragma unroll 1
@@ -950,36 +962,36 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
             const bool whole = k0 + 31 <= all_lim && (k0 >= all_lo || k0 + 32 <= a.sinks) && valid == 3u;
             unsigned valid_after = 3u;
             if constexpr (CODES) {
-                if (after < h_end) two_next = pages_of_half(after);
+                if (after + kWaves < h_end) two_next = pages_of_half(after + kWaves);
                 attend(std::integral_constant<int, 1>{}, k0, k_buf, v_buf, scales, valid, whole,
                        [&] {
                            if (next < h_end) stage_half(std::false_type{}, raw_k);
-                           if (after < h_end) load_half(after, two_next, false, raw_k);
+                           if (after < h_end) load_half(after, two, false, raw_k);
                        },
                        [] {},
                        [&]() -> unsigned long long { return (unsigned)__builtin_amdgcn_readfirstlane((int)*(lds_u1)(scales + 520)); }, [](unsigned long long) {});
                 if (next < h_end) stage_half(std::true_type{}, raw_v);
                 if (after < h_end) {
-                    valid_after = valid_of_half(two_next);
-                    load_half(after, two_next, true, raw_v);
-                    load_scales(after, two_next);
+                    valid_after = valid_of_half(two);
+                    load_half(after, two, true, raw_v);
+                    load_scales(after, two);
                 }
+                two = two_next;
             } else {
-                if (next < h_end) {
-                    two_next = pages_of_half(next);
-                    valid_next = valid_of_half(two_next);
-                }
+                if (next < h_end) valid_next = valid_of_half(two);
                 loads_left<(int)kCopies>();                         // k is there; v's copies may be on their way
                 attend(std::integral_constant<int, 1>{}, k0, k_buf, v_buf, scales, valid, whole,
                        [&] {
-                           if (next < h_end) copy_half(next, two_next, false);
+                           if (next < h_end) copy_half(next, two, false);
+                           if (after < h_end) two_next = pages_of_half(after);
                        },
                        [&] {
                            if (next < h_end) loads_left<(int)kCopies>();
                            else loads_left<0>();
                        },
                        bad_of_half, take_out_of_half);
-                if (next < h_end) copy_half(next, two_next, true);
+                if (next < h_end) copy_half(next, two, true);
+                two = two_next;
             }
             valid = valid_next;
             valid_next = valid_after;
@@ -1015,7 +1027,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         }
     }
     auto store_row = [&](int row, int four, f32x4 v) {           // four of 4 * OM, for this lane's half
-        const int query_e = (int)((unsigned)row / (unsigned)a.shared), head = (int)kv_head * a.shared + (row - query_e * a.shared);
+        const int query_e = a.query_of(row), head = (int)kv_head * a.shared + (row - query_e * a.shared);
         uint16_t* out = a.out + ((int64_t)(w.r.q_at + query_e) * a.heads + head) * D + 4 * g_e + 8 * four;
         *reinterpret_cast<u32x2*>(out) = u32x2{pack<F16>(v[0], v[1]), pack<F16>(v[2], v[3])};
     };
@@ -1098,7 +1110,7 @@ __global__ __launch_bounds__(256) void attn_chunk_join_kernel(Args a) {
     for (int part = 0; 32 * part < w.height && w.tile * w.height + 32 * part < rows; ++part) {
         const int row = w.tile * w.height + 32 * part + n;
         const float* ml = first + kRowTile * D + 2 * (32 * part + n);
-        const int query = (int)((unsigned)min(row, rows - 1) / (unsigned)a.shared), head = (int)kv_head * a.shared + (min(row, rows - 1) - query * a.shared);
+        const int query = a.query_of(min(row, rows - 1)), head = (int)kv_head * a.shared + (min(row, rows - 1) - query * a.shared);
         const float* sums = first + 4 * ((part * (D / 8) + four) * 64 + lane);
         float top = -__builtin_inff(), sum = 0.0f;
         f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -1183,7 +1195,9 @@ ChunkPlan plan_attn_chunk(int64_t requests, int64_t q_tokens, int heads, int kv_
 hipError_t launch_attn_chunk(const ChunkArgs& c, const any4_kv_cache* cache, const ChunkPlan& pl, void* workspace, hipStream_t stream) {
     Args a{c.q, c.k, c.v, {}, c.table, c.table_stride, (int)c.table_width, c.q_starts, c.k_starts, c.lengths, (int)c.q_tokens, (int)c.k_tokens, c.requests,
            c.heads, c.kv_heads, c.heads / c.kv_heads, c.window > 0 ? c.window : kNoWindow, c.sinks, 0, 0, 0, 0u, c.softmax_scale * kLog2e, c.out,
-           static_cast<float*>(workspace)};
+           static_cast<float*>(workspace), 0u, 31};
+    while ((int64_t)1 << (a.shared_shift - 31) < a.shared) ++a.shared_shift;
+    a.shared_mul = (uint32_t)((((uint64_t)1 << a.shared_shift) + (uint64_t)a.shared - 1) / (uint64_t)a.shared);
     if (cache) a.c = kv_pages(*cache);
     auto types = [&](auto source, auto dim) {
         return c.f16 ? launch<decltype(source)::value, decltype(dim)::value, true>(a, pl, stream)
