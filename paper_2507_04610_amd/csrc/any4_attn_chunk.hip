@@ -341,9 +341,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     float scale = a.scale_log2, sum_q = 0.0f;
     {
         const int head = (int)kv_head * a.shared + (row - query * a.shared);
-        const uint16_t* qp = a.q.p + (int64_t)(w.r.q_at + query) * a.q.token + (int64_t)head * a.q.head + 8 * g;
+        const uint16_t* qp = a.q.p + (int64_t)(w.r.q_at + query) * a.q.token + (int64_t)head * a.q.head;
+        // places 16 i + 8 g .. of product i, or, with codes in narrow tiles, those that a lane's 16 bytes of k hold one after the other
+        constexpr int kEach = SOURCE == 4 ? 4 : 2;
 #pragma unroll
-        for (int i = 0; i < QM; ++i) q[i] = *reinterpret_cast<const u32x4*>(qp + 16 * i);
+        for (int i = 0; i < QM; ++i) {
+            const int at = CODES && narrow ? 16 * kEach * (i / kEach) + 8 * kEach * g + 8 * (i % kEach) : 16 * i + 8 * g;
+            q[i] = *reinterpret_cast<const u32x4*>(qp + at);
+        }
         if constexpr (CODES) {
             if constexpr (!F16) {
                 float top = 0.0f;
@@ -550,9 +555,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[m][r] = 0.0f;
 
-    // 32 U keys from k0 on, whose k, v and scales lie in LDS; `whole`: all rows see all of them; valid: a bit for each 16 whose page exists.  The
+    // k's operands out of a tile in LDS
+    auto k_of = [&](uint32_t buf) {
+        uint32_t at = k_lane + buf;
+        asm volatile("" : "+v"(at));
+        return [at](int u, int i) -> u32x4 { return *(lds_u4)((at ^ (uint32_t)(i << 5)) + (uint32_t)(u * 32 * T::kRow)); };
+    };
+    // 32 U keys from k0 on, whose v and scales lie in LDS; `whole`: all rows see all of them; valid: a bit for each 16 whose page exists.  The
     // steps: after_scores, before_product (v has to be there then), bad_of the keys whose v is not finite, take_out of them.
-    auto attend = [&](auto blocks, int k0, uint32_t k_buf, uint32_t v_buf, uint32_t scales, unsigned valid, bool whole, auto after_scores, auto before_product,
+    auto attend = [&](auto blocks, int k0, auto k_operand, uint32_t v_buf, uint32_t scales, unsigned valid, bool whole, auto after_scores, auto before_product,
                       auto bad_of, auto take_out) {
         constexpr int U = decltype(blocks)::value;
         // four tokens' of an array of scales: keys 32 u + 8 c + 4 g ..
@@ -562,16 +573,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         // the product 1030; a mixed batch in 8 bits 451 and 434 the other way round.  Heads of 64 have a third wavefront and lose 4 % by it.)
         constexpr bool kFirst = D == 128;
         f32x16 s[U];
-        uint32_t k_at = k_lane + k_buf, v_at = v_lane + v_buf;
-        asm volatile("" : "+v"(k_at), "+v"(v_at));               // (or every operand's address is kept in a register)
+        uint32_t v_at = v_lane + v_buf;
+        asm volatile("" : "+v"(v_at));                           // (or every operand's address is kept in a register)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[u][r] = 0.0f;
 #pragma unroll
             for (int i = 0; i < QM; ++i) {
-                const u32x4 k = *(lds_u4)((k_at ^ (uint32_t)(i << 5)) + (uint32_t)(u * 32 * T::kRow));
-                s[u] = mma32<MMA16>(k, q[i], s[u]);
+                s[u] = mma32<MMA16>(k_operand(u, i), q[i], s[u]);
             }
         }
         if constexpr (kFirst) __builtin_amdgcn_s_setprio(1);
@@ -777,7 +787,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 const uint32_t parity = (uint32_t)(t & 1);
                 unsigned valid_after = 15u;
                 const bool whole = begin(t, parity, valid_after);
-                attend(std::integral_constant<int, 2>{}, span.real(t) * kKeys, parity * T::kBytes, (2 + parity) * T::kBytes, kAside + parity * kAsideBytes, valid,
+                attend(std::integral_constant<int, 2>{}, span.real(t) * kKeys, k_of(parity * T::kBytes), (2 + parity) * T::kBytes, kAside + parity * kAsideBytes, valid,
                        whole, [] {}, [] {}, [&] { return bad_of_tile(parity); }, [&](unsigned long long bad) { take_out(parity, bad); });
                 valid = valid_next;
                 valid_next = valid_after;
@@ -875,80 +885,87 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 if ((bad >> (j * T::kRows + lane / T::kPieces)) & 1ull) *(lds_u4)(v_buf + 1024u * (uint32_t)j + 16u * (uint32_t)lane) = u32x4{0u, 0u, 0u, 0u};
         };
 
-        // codes: 16 bytes a lane at a time
+        // codes: 16 bytes a lane at a time; k's as operands, without LDS (a lane has its token's every second 16 bytes), v's into LDS
         constexpr int kRowBytes = CODES ? D * SOURCE / 8 : 64, kRowLanes = kRowBytes / 16, kLoads = 32 / (64 / kRowLanes), kRowsAtOnce = 64 / kRowLanes;
         constexpr int kPer = CODES ? 16 * 8 / SOURCE : 8;          // codes of a load
         uint32_t raw_k[kLoads][4], raw_v[kLoads][4];
         u32x2 raw_scales = {0u, 0u};
-        auto load_half = [&](int h, const Two& two, bool of_v, uint32_t (&to)[kLoads][4]) {
+        auto load_k = [&](int h, const Two& two) {
+            const int64_t first = n < 16 ? first_of(two, 0) : first_of(two, 1);
+            const uint8_t* p = a.c.k + (first + (min(key_of(h) + n, lk - 1) & page_mask)) * kRowBytes + 16 * g;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) load_bytes(p + 32 * i, raw_k[i]);
+        };
+        auto k_raw = [&](int, int i) -> u32x4 {
+            constexpr int BITS = CODES ? SOURCE : 8, kWords = 8 * BITS / 32;
+            uint32_t wide[4];
+#pragma unroll
+            for (int x = 0; x < kWords; ++x) widen<BITS, false>(raw_k[i * kWords / 4][i * kWords % 4 + x], wide + x * 16 / BITS);
+            return u32x4{wide[0], wide[1], wide[2], wide[3]};
+        };
+        auto load_v = [&](int h, const Two& two) {
             const int k0 = key_of(h);
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int r = i * kRowsAtOnce + lane / kRowLanes;
                 const int64_t first = (kRowsAtOnce <= 16 ? (i * kRowsAtOnce < 16) : r < 16) ? first_of(two, 0) : first_of(two, 1);
-                const uint8_t* p = (of_v ? a.c.v : a.c.k) + (first + (min(k0 + r, lk - 1) & page_mask)) * kRowBytes + 16 * (lane % kRowLanes);
-                load_bytes(p, to[i]);
+                load_bytes(a.c.v + (first + (min(k0 + r, lk - 1) & page_mask)) * kRowBytes + 16 * (lane % kRowLanes), raw_v[i]);
             }
+            if (lane < 32) raw_scales = *reinterpret_cast<const u32x2*>(a.c.scales + 4 * ((lane < 16 ? first_of(two, 0) : first_of(two, 1)) + (min(k0 + lane, lk - 1) & page_mask)));
         };
-        auto load_scales = [&](int h, const Two& two) {
-            if (lane < 32) raw_scales = *reinterpret_cast<const u32x2*>(a.c.scales + 4 * ((lane < 16 ? first_of(two, 0) : first_of(two, 1)) + (min(key_of(h) + lane, lk - 1) & page_mask)));
-        };
-        auto stage_half = [&](auto of_v, const uint32_t (&from)[kLoads][4]) {
-            constexpr bool V = decltype(of_v)::value;
+        auto stage_v = [&] {
             constexpr int BITS = CODES ? SOURCE : 8;
             // (the first row's first piece; a register of its own in each round, as the others' would be if they were kept)
             const int r0 = lane / kRowLanes, piece0 = (lane % kRowLanes) * (kPer / 8);
-            uint32_t to = (V ? v_buf : k_buf) + (uint32_t)(r0 * T::kRow) + 16u * (uint32_t)(piece0 ^ (V ? swizzle_v<D>(r0) : T::swizzle_k(r0)));
+            uint32_t to = v_buf + (uint32_t)(r0 * T::kRow) + 16u * (uint32_t)(piece0 ^ swizzle_v<D>(r0));
             asm volatile("" : "+v"(to));
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 uint32_t wide[kPer / 2];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) widen<BITS, V>(from[i][x], wide + x * 16 / BITS);
+                for (int x = 0; x < 4; ++x) widen<BITS, true>(raw_v[i][x], wide + x * 16 / BITS);
 #pragma unroll
                 for (int x = 0; x < kPer / 8; ++x) {
-                    const uint32_t other = 16u * (uint32_t)(x ^ (V ? swizzle_v<D>(i * kRowsAtOnce) : T::swizzle_k(i * kRowsAtOnce)));
+                    const uint32_t other = 16u * (uint32_t)(x ^ swizzle_v<D>(i * kRowsAtOnce));
                     *(lds_u4)((to ^ other) + (uint32_t)(i * kRowsAtOnce * T::kRow)) = u32x4{wide[4 * x], wide[4 * x + 1], wide[4 * x + 2], wide[4 * x + 3]};
                 }
             }
             using C = Codes<BITS>;
-            const float by = bf16lo_to_f32(raw_scales[V ? 1 : 0]), off = bf16hi_to_f32(raw_scales[V ? 1 : 0]);
-            const float mid = fmaf(V ? C::kCentre : -C::kBias, by, off);
-            const bool fine = !V || fabsf(mid) < __builtin_inff();
+            const float ks = bf16lo_to_f32(raw_scales[0]), ko = bf16hi_to_f32(raw_scales[0]), vs = bf16lo_to_f32(raw_scales[1]), vo = bf16hi_to_f32(raw_scales[1]);
+            const float mid = fmaf(C::kCentre, vs, vo);
+            const bool fine = fabsf(mid) < __builtin_inff();
             if (lane < 32) {
-                *(lds_f)(scales + (V ? 256 : 0) + 4u * (uint32_t)lane) = fine ? by : 0.0f;
-                *(lds_f)(scales + (V ? 384 : 128) + 4u * (uint32_t)lane) = fine ? mid : 0.0f;
+                const uint32_t at = scales + 4u * (uint32_t)lane;
+                *(lds_f)(at) = ks;
+                *(lds_f)(at + 128) = fmaf(-C::kBias, ks, ko);
+                *(lds_f)(at + 256) = fine ? vs : 0.0f;
+                *(lds_f)(at + 384) = fine ? mid : 0.0f;
             }
-            if constexpr (V) {
-                float big = lanes_reduce<16>(fine && lane < 32 ? fabsf(by) : 0.0f, [](float u, float v) { return fmaxf(u, v); });
-                big = fmaxf(big, __shfl_xor(big, 16));
-                const unsigned long long bad = __builtin_amdgcn_ballot_w64(!fine && lane < 32);
-                if (lane == 0) {
-                    *(lds_f)(scales + 512) = big;
-                    *(lds_u2)(scales + 520) = u32x2{(uint32_t)bad, 0u};
-                }
+            float big = lanes_reduce<16>(fine && lane < 32 ? fabsf(vs) : 0.0f, [](float u, float v) { return fmaxf(u, v); });
+            big = fmaxf(big, __shfl_xor(big, 16));
+            const unsigned long long bad = __builtin_amdgcn_ballot_w64(!fine && lane < 32);
+            if (lane == 0) {
+                *(lds_f)(scales + 512) = big;
+                *(lds_u2)(scales + 520) = u32x2{(uint32_t)bad, 0u};
             }
         };
 
         int h = 2 * t_first + wave;
-        Two two{{0, 0}}, two_next{{0, 0}};
+        // pages of the half whose loads go out next (codes: k's), and of the one behind it (codes: v's)
+        Two two{{0, 0}}, two_next{{0, 0}}, two_after{{0, 0}};
         unsigned valid = 3u, valid_next = 3u;
         if (h < h_end) {
             two = pages_of_half(h);
             valid = valid_of_half(two);
             if constexpr (CODES) {
-                load_half(h, two, false, raw_k);
-                load_half(h, two, true, raw_v);
-                load_scales(h, two);
+                load_v(h, two);
+                load_k(h, two);
                 if (h + kWaves < h_end) two = pages_of_half(h + kWaves);
-                stage_half(std::false_type{}, raw_k);
-                stage_half(std::true_type{}, raw_v);
+                if (h + 2 * kWaves < h_end) two_next = pages_of_half(h + 2 * kWaves);
+                stage_v();
                 if (h + kWaves < h_end) {
                     valid_next = valid_of_half(two);
-                    load_half(h + kWaves, two, false, raw_k);
-                    load_half(h + kWaves, two, true, raw_v);
-                    load_scales(h + kWaves, two);
-                    if (h + 2 * kWaves < h_end) two = pages_of_half(h + 2 * kWaves);
+                    load_v(h + kWaves, two);
                 }
             } else {
                 copy_half(h, two, false);
@@ -962,25 +979,24 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
             const bool whole = k0 + 31 <= all_lim && (k0 >= all_lo || k0 + 32 <= a.sinks) && valid == 3u;
             unsigned valid_after = 3u;
             if constexpr (CODES) {
-                if (after + kWaves < h_end) two_next = pages_of_half(after + kWaves);
-                attend(std::integral_constant<int, 1>{}, k0, k_buf, v_buf, scales, valid, whole,
+                if (after + kWaves < h_end) two_after = pages_of_half(after + kWaves);
+                attend(std::integral_constant<int, 1>{}, k0, k_raw, v_buf, scales, valid, whole,
                        [&] {
-                           if (next < h_end) stage_half(std::false_type{}, raw_k);
-                           if (after < h_end) load_half(after, two, false, raw_k);
+                           if (next < h_end) load_k(next, two);
                        },
                        [] {},
                        [&]() -> unsigned long long { return (unsigned)__builtin_amdgcn_readfirstlane((int)*(lds_u1)(scales + 520)); }, [](unsigned long long) {});
-                if (next < h_end) stage_half(std::true_type{}, raw_v);
+                if (next < h_end) stage_v();
                 if (after < h_end) {
-                    valid_after = valid_of_half(two);
-                    load_half(after, two, true, raw_v);
-                    load_scales(after, two);
+                    valid_after = valid_of_half(two_next);
+                    load_v(after, two_next);
                 }
                 two = two_next;
+                two_next = two_after;
             } else {
                 if (next < h_end) valid_next = valid_of_half(two);
                 loads_left<(int)kCopies>();                         // k is there; v's copies may be on their way
-                attend(std::integral_constant<int, 1>{}, k0, k_buf, v_buf, scales, valid, whole,
+                attend(std::integral_constant<int, 1>{}, k0, k_of(k_buf), v_buf, scales, valid, whole,
                        [&] {
                            if (next < h_end) copy_half(next, two, false);
                            if (after < h_end) two_next = pages_of_half(after);
