@@ -213,7 +213,11 @@ template <int SOURCE, bool JOIN> __device__ __forceinline__ Work work_of(const A
             w.r.lk = __builtin_amdgcn_readlane(s.r.lk, f);
             w.pieces = __builtin_amdgcn_readlane(s.pieces, f);
             const int tiles = __builtin_amdgcn_readlane(s.tiles, f);
-            const int at = (int)place - (before + __builtin_amdgcn_readlane(sum, f) - __builtin_amdgcn_readlane(own, f));
+            const int all = __builtin_amdgcn_readlane(own, f), at = (int)place - (before + __builtin_amdgcn_readlane(sum, f) - all);
+            if ((unsigned)at >= (unsigned)all) {                // (starts that do not ascend can add up to more than 32 bits hold)
+                w.request = -1;
+                break;
+            }
             const int tile = JOIN ? at : at / w.pieces;
             w.piece = JOIN ? 0 : at - tile * w.pieces;
             w.tile = tiles - 1 - tile;                          // the most keys first
@@ -598,15 +602,24 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         after_scores();
         // (places relative to the tile's first key of this half, which may be those of no page)
         const int base = k0 + 4 * g, lim_at = lim - base, lo_at = (max(lim, 0) + 1 - base) - a.window, sinks_at = a.sinks - base;
-        auto sees = [&](int u, int r) -> bool {
-            const int key = 32 * u + 8 * (r >> 2) + (r & 3), last = !PAGED || ((valid >> (2 * u + (r >> 3))) & 1u) ? lim_at : -0x7FFFFFFF;
-            return (bool)((int)(key <= last) & ((int)(key >= lo_at) | (int)(key < sinks_at)));
-        };
+        auto key_of = [](int u, int r) -> int { return 32 * u + 8 * (r >> 2) + (r & 3); };
+        auto last_of = [&](int u, int r) -> int { return !PAGED || ((valid >> (2 * u + (r >> 3))) & 1u) ? lim_at : -0x7FFFFFFF; };
+        auto in_part = [&](int u, int r) -> bool { return (bool)((int)(key_of(u, r) >= lo_at) | (int)(key_of(u, r) < sinks_at)); };
+        auto sees = [&](int u, int r) -> bool { return (bool)((int)(key_of(u, r) <= last_of(u, r)) & (int)in_part(u, r)); };
         if (seldom(!whole)) {
+            // (behind the last one or on a page that does not exist; in front of the window)
+            if (k0 + 32 * U - 1 > all_lim || valid != (1u << 2 * U) - 1u) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[u][r] = sees(u, r) ? s[u][r] : -__builtin_inff();
+                    for (int r = 0; r < 16; ++r) s[u][r] = key_of(u, r) <= last_of(u, r) ? s[u][r] : -__builtin_inff();
+            }
+            if (k0 < all_lo && k0 + 32 * U > a.sinks) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[u][r] = in_part(u, r) ? s[u][r] : -__builtin_inff();
+            }
         }
 
         // The maximum in use is raised only when a score exceeds it by 2^kSlack, which spares nearly all rescaling of o.
