@@ -142,7 +142,7 @@ struct ChunkPlan {
     int64_t blocks;
     int target, slots, cut_tiles;
     bool small;               // whether it may be one that takes 32 rows at a time
-    size_t workspace;
+    size_t plan_bytes, workspace;      // of these in front: what a first launch finds out for more than 64 requests
 };
 ChunkPlan plan_attn_chunk(int64_t requests, int64_t q_tokens, int heads, int kv_heads, int head_dim, int64_t max_tokens, bool cut, int cus);
 hipError_t launch_attn_chunk(const ChunkArgs& a, const any4_kv_cache* cache, const ChunkPlan& pl, void* workspace, hipStream_t stream);

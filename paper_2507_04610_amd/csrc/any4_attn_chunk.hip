@@ -16,7 +16,7 @@
 // bf16 queries become fp16 for that, exactly too: a row is scaled by a power of two.  The product p_j vs_j is rounded to fp16; the exponent of the
 // largest vs_j that a row has seen is taken off it together with the running maximum.
 //
-// Who does what.  Lengths are the device's, so each block finds its rows itself.  Where whole tiles of rows do not fill the chip, their keys are cut
+// Who does what.  Lengths are the device's, so each block finds its rows itself (of more than 64 requests, in what a first launch writes down).  Where whole tiles of rows do not fill the chip, their keys are cut
 // into pieces, no more than it takes; pieces leave sums, maximum and sum of weights in the workspace, and a second launch joins them.
 //
 // Rounding: scores, maxima, sums and accumulators are fp32; the weights (times vs_j) are rounded to 16 bits for the matrix cores, once.
@@ -32,6 +32,8 @@ namespace {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kRowTile = 32 * kWaves;
 constexpr int kNarrow = 4;                                      // tiles of keys for up to 32 rows that take as long as one for 128
+constexpr int kFewRows = 64;                                    // requests of up to so many rows have tiles of 32, as small calls (65 requests of 64 rows
+                                                                // over 1000 tokens in 8 bits: 81 us, in tiles of 128 98)
 constexpr int kLeastPiece = 4;                                  // least tiles of keys of a piece
 constexpr int kWhole = 10;                                      // keys of so many tiles are not cut: the join costs as much as a few of them
 constexpr int kSmall = 1024;                                    // calls of so many tiles of keys take 32 rows at a time: more blocks, each done sooner
@@ -56,6 +58,7 @@ struct Args {
     int q_tokens, k_tokens, requests, heads, kv_heads, shared, window, sinks;
     int target, slots;                 // blocks that fill the chip (0: nothing is cut); pieces that the workspace has room for
     int small;                         // whether the call may be one that takes 32 rows at a time
+    const int* plan;                   // more than 64 requests: where each one's blocks end (see Plan); NULL: blocks look for themselves
     unsigned first_block;              // of this launch
     float scale_log2;
     uint16_t* out;
@@ -112,13 +115,16 @@ struct Shares {                        // of 64 requests, a lane each
     Request r;
     int tiles, pieces;
 };
-// what a request's last (and longest) tile of rows costs, in tiles of keys for 128 rows
-__device__ __forceinline__ int costs_of(const Args& a, const Request& r, int tiles, int height) {
-    const int of_keys = span_of(a, r, tiles - 1, height).tiles;
-    return height == 32 || r.lq * a.shared <= 32 ? (of_keys + kNarrow - 1) / kNarrow : of_keys;
+// rows of a request's tiles, in a call whose requests of many rows have tiles of `most`
+__device__ __forceinline__ int height_of(const Args& a, const Request& r, int most) { return r.lq * a.shared <= kFewRows ? 32 : most; }
+__device__ __forceinline__ int tiles_of(const Args& a, const Request& r, int most) {
+    const int height = height_of(a, r, most);
+    return (int)(((unsigned)(r.lq * a.shared) + (unsigned)height - 1) >> (height == 32 ? 5 : 7));
 }
-__device__ __forceinline__ int tiles_of(const Args& a, const Request& r, int height) {
-    return (int)(((unsigned)(r.lq * a.shared) + (unsigned)height - 1) / (unsigned)height);
+// what its last (and longest) tile of rows costs, in tiles of keys for 128 rows
+__device__ __forceinline__ int costs_of(const Args& a, const Request& r, int tiles, int most) {
+    const int height = height_of(a, r, most), of_keys = span_of(a, r, tiles - 1, height).tiles;
+    return height == 32 ? (of_keys + kNarrow - 1) / kNarrow : of_keys;
 }
 // How a call is cut: rows of a tile, and the most that a piece costs (0: nothing is cut).  Sums in fp32, in one order everywhere.
 struct Cut {
@@ -135,43 +141,39 @@ __device__ __forceinline__ float lanes_total(float v) {
     add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});       // row_bcast:31
     return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
-// `first`: this lane's of the first 64 requests
-template <int SOURCE> __device__ __forceinline__ Cut cut_of(const Args& a, const Request& first, int lane) {
+// sum(f): f of all requests, added up
+template <class Sum> __device__ __forceinline__ Cut cut_of(const Args& a, Sum sum) {
     Cut cut{a.small ? 32 : kRowTile, 0};
     if (a.target == 0) return cut;                              // (then the host knows)
     const float heads = (float)a.kv_heads, target = (float)a.target;
-    float cost = 0.0f, tiles = 0.0f;
-    auto add_up = [&](int height) {
-        cost = tiles = 0.0f;
-        for (int r0 = 0; r0 < a.requests; r0 += 64) {
-            Request r = first;
-            if (r0 > 0) r = r0 + lane < a.requests ? request_of<SOURCE>(a, r0 + lane) : Request{};
+    auto costs = [&](int height) {
+        return sum([&](const Request& r) -> float {
             const int n = tiles_of(a, r, height);
-            cost += lanes_total(n > 0 ? (float)n * (float)costs_of(a, r, n, height) : 0.0f);
-            tiles += lanes_total((float)n);
-        }
+            return n > 0 ? (float)n * (float)costs_of(a, r, n, height) : 0.0f;
+        }) * heads;
     };
-    add_up(kRowTile);
+    float all = costs(kRowTile);
     cut.height = kRowTile;
-    if (a.small && cost * heads <= (float)kSmall) {
+    if (a.small && all <= (float)kSmall) {
         cut.height = 32;
-        add_up(32);
+        all = costs(32);
     }
     // Pieces of all: at most cost / least and one for each tile, together no more than fill the chip, as far as that leaves pieces to cut.  That counts a
-    // piece's rounding up as a whole one: up to 64 requests' are counted, and shorter pieces taken as far as they are no more than that.
-    const float all = cost * heads, limit = 1073741824.0f;
-    const int most = max((int)fminf(ceilf(all / fmaxf(target - tiles * heads, 0.5f * target)), limit), kLeastPiece);
+    // piece's rounding up as a whole one: shorter ones are tried, and taken if they are no more than fill the chip.
+    const float tiles = sum([&](const Request& r) { return (float)tiles_of(a, r, cut.height); }) * heads, limit = 1073741824.0f;
+    const int most = max((int)fminf(ceilf(all / fmaxf(target - tiles, 0.5f * target)), limit), kLeastPiece);
     const int low = max((int)fminf(ceilf(all / target), limit), kLeastPiece);
     cut.least = most;
-    if (a.requests <= 64) {
-        const int n = tiles_of(a, first, cut.height), own = n > 0 ? costs_of(a, first, n, cut.height) : 0;
-        for (int third = 0; third < 3; ++third) {
-            const int shorter = low + (most - low) * third / 3;
-            if (shorter >= most) break;
-            if (lanes_total(own > kWhole ? (float)n * (float)((own + shorter - 1) / shorter) : (float)n) * heads <= target) {
-                cut.least = shorter;
-                break;
-            }
+    for (int third = 0; third < 3; ++third) {
+        const int shorter = low + (most - low) * third / 3;
+        if (shorter >= most) break;
+        const float pieces = sum([&](const Request& r) -> float {
+            const int n = tiles_of(a, r, cut.height), cost = n > 0 ? costs_of(a, r, n, cut.height) : 0;
+            return cost > kWhole ? (float)n * (float)((cost + shorter - 1) / shorter) : (float)n;
+        });
+        if (pieces * heads <= target) {
+            cut.least = shorter;
+            break;
         }
     }
     cut.height = __builtin_amdgcn_readfirstlane(cut.height);
@@ -186,10 +188,94 @@ __device__ __forceinline__ Shares shares_of(const Args& a, const Request& r, con
     }
     return s;
 }
+// More than 64 requests: a launch in front of the others has one block find out what each would find for itself.
+struct Plan {
+    // [4][requests] behind the height of tiles of rows: where a request's blocks end, where its tiles that are cut end (both without KV heads), its
+    // first piece's place, its pieces
+    static constexpr int kHeader = 4;
+    __host__ __device__ static int64_t bytes(int64_t requests) { return (4 * (kHeader + 4 * requests) + 255) / 256 * 256; }
+};
+constexpr int kPlanThreads = 1024;
+template <int SOURCE>
+__global__ __launch_bounds__(kPlanThreads) void attn_chunk_plan_kernel(Args a, int* plan) {
+    constexpr int WAVES = kPlanThreads / 64;
+    __shared__ float partial[WAVES];
+    __shared__ int sums[3][WAVES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Cut how = cut_of(a, [&](auto f) {
+        float mine = 0.0f, all = 0.0f;
+        for (int r = threadIdx.x; r < a.requests; r += kPlanThreads) mine += f(request_of<SOURCE>(a, r));
+        mine = lanes_total(mine);
+        __syncthreads();
+        if (lane == 0) partial[wave] = mine;
+        __syncthreads();
+        for (int i = 0; i < WAVES; ++i) all += partial[i];
+        return all;
+    });
+    if (threadIdx.x == 0) plan[0] = how.height;
+    int* const at = plan + Plan::kHeader;
+    int before[3] = {0, 0, 0};
+    for (int r0 = 0; r0 < a.requests; r0 += kPlanThreads) {
+        const int r = r0 + (int)threadIdx.x;
+        Shares s = shares_of(a, r < a.requests ? request_of<SOURCE>(a, r) : Request{}, how);
+        // each thread gets the sum of the threads up to its own
+        auto scan = [&](int which, int v) -> int {
+            const int up_to = lanes_scan(v);
+            if (lane == 63) sums[which][wave] = up_to;
+            __syncthreads();
+            int here = before[which];
+            for (int w = 0; w < WAVES; ++w) {
+                if (w < wave) here += sums[which][w];
+                before[which] += sums[which][w];
+            }
+            __syncthreads();
+            return here + up_to;
+        };
+        const int cut = s.pieces > 1 ? s.tiles * s.pieces : 0, cut_end = scan(0, cut);
+        // (as many as were planned for; were there more, they would be left whole)
+        if (cut > 0 && (int64_t)cut_end * a.kv_heads > a.slots) s.pieces = 1;
+        const int end = scan(1, s.tiles * s.pieces), join_end = scan(2, s.pieces > 1 ? s.tiles : 0);
+        if (r < a.requests) {
+            at[r] = end;
+            at[a.requests + r] = join_end;
+            at[2 * a.requests + r] = cut_end - cut;
+            at[3 * a.requests + r] = s.pieces;
+        }
+    }
+}
+template <int SOURCE, bool JOIN> __device__ __forceinline__ Work planned(const Args& a, unsigned place, unsigned kv_head, int lane) {
+    Work w{-1, 0, 0, 1, 0, a.plan[0], {}};
+    const int* const at = a.plan + Plan::kHeader;
+    const int* const ends = at + (JOIN ? a.requests : 0);
+    // the first request that ends behind `place`, among 64 at a time
+    int from = 0, n = a.requests;
+    for (;;) {
+        const int step = (n + 63) / 64, mine = min((lane + 1) * step, n) - 1;
+        const unsigned long long past = __builtin_amdgcn_ballot_w64((unsigned)ends[from + mine] > place);
+        if (!past) return w;
+        const int f = __builtin_ctzll(past);
+        from += f * step;
+        n = min(step, n - f * step);
+        if (step == 1) break;
+    }
+    w.request = __builtin_amdgcn_readfirstlane(from);
+    w.r = request_of<SOURCE>(a, w.request);
+    w.height = height_of(a, w.r, w.height);
+    w.pieces = at[3 * a.requests + w.request];
+    const int begin = w.request > 0 ? ends[w.request - 1] : 0, all = ends[w.request] - begin, own = (int)place - begin, tile = JOIN ? own : own / w.pieces;
+    w.piece = JOIN ? 0 : own - tile * w.pieces;
+    w.tile = (JOIN ? all : all / w.pieces) - 1 - tile;          // the most keys first
+    w.slot = (at[2 * a.requests + w.request] + tile * w.pieces + w.piece) * a.kv_heads + (int)kv_head;
+    if ((unsigned)own >= (unsigned)all) w.request = -1;         // (starts that do not ascend can add up to more than 32 bits hold)
+    return w;
+}
+
 // JOIN: place counts the tiles of rows that are cut, otherwise blocks; both without KV heads
 template <int SOURCE, bool JOIN> __device__ __forceinline__ Work work_of(const Args& a, unsigned place, unsigned kv_head, int lane) {
+    if (a.plan) return planned<SOURCE, JOIN>(a, place, kv_head, lane);
+    // (where something is cut there are no more than 64 requests)
     const Request first = lane < a.requests ? request_of<SOURCE>(a, lane) : Request{};
-    const Cut how = cut_of<SOURCE>(a, first, lane);
+    const Cut how = cut_of(a, [&](auto f) { return lanes_total(f(first)); });
     Work w{-1, 0, 0, 1, 0, how.height, {}};
     for (int r0 = 0, before = 0, cut_before = 0; r0 < a.requests && w.request < 0; r0 += 64) {
         Request r = first;
@@ -211,6 +297,7 @@ template <int SOURCE, bool JOIN> __device__ __forceinline__ Work work_of(const A
             w.r.lq = __builtin_amdgcn_readlane(s.r.lq, f);
             w.r.k_at = __builtin_amdgcn_readlane(s.r.k_at, f);
             w.r.lk = __builtin_amdgcn_readlane(s.r.lk, f);
+            w.height = height_of(a, w.r, how.height);
             w.pieces = __builtin_amdgcn_readlane(s.pieces, f);
             const int tiles = __builtin_amdgcn_readlane(s.tiles, f);
             const int all = __builtin_amdgcn_readlane(own, f), at = (int)place - (before + __builtin_amdgcn_readlane(sum, f) - all);
@@ -1180,11 +1267,19 @@ __global__ __launch_bounds__(256) void attn_chunk_join_kernel(Args a) {
 template <int SOURCE, int D, bool F16> hipError_t launch(Args a, const ChunkPlan& pl, hipStream_t stream) {
     constexpr auto kernel = attn_chunk_kernel<SOURCE, D, F16>;
     constexpr int bytes = 4 * Tile<D, kWaves>::kBytes + kAsideAll<SOURCE == 8 || SOURCE == 4>;
+    static_assert(kRowTile == 128 && kFewRows <= 64, "tiles of rows are counted by shifts, and two for few rows");
     static_assert(kAsideAll<true> >= 2 * kScaleBytes<kKeys>, "two tiles' scales");
     if (hipError_t e = ensure_lds<kernel>(bytes); e != hipSuccess) return e;
     a.target = pl.target;
     a.slots = pl.slots;
     a.small = pl.small;
+    if (pl.plan_bytes > 0) {
+        int* const plan = reinterpret_cast<int*>(a.partial);
+        a.partial += pl.plan_bytes / sizeof(float);
+        hipLaunchKernelGGL((attn_chunk_plan_kernel<SOURCE>), dim3(1), dim3(kPlanThreads), 0, stream, a, plan);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        a.plan = plan;
+    }
     const hipError_t e = launch_blocks(pl.blocks, kThreads, hipSuccess, [&](int64_t first, int64_t count) {
         a.first_block = (unsigned)first;
         hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(kThreads), bytes, stream, a);
@@ -1200,7 +1295,8 @@ template <int SOURCE, int D, bool F16> hipError_t launch(Args a, const ChunkPlan
 ChunkPlan plan_attn_chunk(int64_t requests, int64_t q_tokens, int heads, int kv_heads, int head_dim, int64_t max_tokens, bool cut, int cus) {
     ChunkPlan p{};
     const int64_t shared = heads / kv_heads, some = requests < q_tokens ? requests : q_tokens;
-    auto tiles_of = [&](int height) { return (q_tokens * shared / height + some) * kv_heads; };
+    // (a request's last tile may be short; one of few rows has two)
+    auto tiles_of = [&](int height) { return (q_tokens * shared / height + 2 * some) * kv_heads; };
     int64_t tiles = tiles_of(kRowTile);
     const int64_t units = (max_tokens + kKeys - 1) / kKeys;
     const bool cuts = cut && units > kWhole;
@@ -1208,6 +1304,7 @@ ChunkPlan plan_attn_chunk(int64_t requests, int64_t q_tokens, int heads, int kv_
     p.small = (cuts ? q_tokens * shared / kRowTile * kv_heads : tiles * units) <= kSmall;
     if (p.small) tiles = tiles_of(32);
     p.blocks = tiles;
+    if (cut && requests > 64) p.plan_bytes = p.workspace = (size_t)Plan::bytes(requests);
     if (!cuts) return p;
     p.target = 2 * cus;
     // (pieces of tiles that are cut: cut_of() has it that there are no more than that, but for the rounding of its sums)
@@ -1217,13 +1314,13 @@ ChunkPlan plan_attn_chunk(int64_t requests, int64_t q_tokens, int heads, int kv_
     const int64_t cut_tiles = p.slots / 2 + kv_heads;
     p.cut_tiles = (int)(tiles < cut_tiles ? tiles : cut_tiles);
     p.blocks = tiles + p.slots;
-    p.workspace = (size_t)p.slots * kRowTile * (head_dim + 2) * sizeof(float);
+    p.workspace += (size_t)p.slots * kRowTile * (head_dim + 2) * sizeof(float);
     return p;
 }
 
 hipError_t launch_attn_chunk(const ChunkArgs& c, const any4_kv_cache* cache, const ChunkPlan& pl, void* workspace, hipStream_t stream) {
     Args a{c.q, c.k, c.v, {}, c.table, c.table_stride, (int)c.table_width, c.q_starts, c.k_starts, c.lengths, (int)c.q_tokens, (int)c.k_tokens, c.requests,
-           c.heads, c.kv_heads, c.heads / c.kv_heads, c.window > 0 ? c.window : kNoWindow, c.sinks, 0, 0, 0, 0u, c.softmax_scale * kLog2e, c.out,
+           c.heads, c.kv_heads, c.heads / c.kv_heads, c.window > 0 ? c.window : kNoWindow, c.sinks, 0, 0, 0, nullptr, 0u, c.softmax_scale * kLog2e, c.out,
            static_cast<float*>(workspace), 0u, 31};
     while ((int64_t)1 << (a.shared_shift - 31) < a.shared) ++a.shared_shift;
     a.shared_mul = (uint32_t)((((uint64_t)1 << a.shared_shift) + (uint64_t)a.shared - 1) / (uint64_t)a.shared);

@@ -131,6 +131,20 @@ def test_many_requests(bits, requests):
 
 
 @pytest.mark.parametrize("bits", (16, 8, 4))
+@pytest.mark.parametrize("requests", (64, 65, 200))
+def test_long_contexts_among_many_requests(bits, requests):
+    """what is cut and joined where blocks look for their work themselves, and where a first launch has found it"""
+    parts = [((5 * i) % 7, (29 * i) % 90) for i in range(requests)]
+    parts[3], parts[40], parts[-1] = (3, 15000), (150, 4000), (30, 9000)
+    p = Chunks(parts, bits, BF16, 128, 8, 2, 64, seed=13)
+    out = p.run()
+    p.check(out, requests=[0, 2, 3, 4, 39, 40, 41, 63, requests - 2, requests - 1])
+    p.check(p.run(window=3000, sinks=70), requests=[3, 40, requests - 1], window=3000, sinks=70)
+    for _ in range(2):
+        assert torch.equal(p.run().view(torch.int16), out.view(torch.int16))
+
+
+@pytest.mark.parametrize("bits", (16, 8, 4))
 @pytest.mark.parametrize("k_by,v_by,q_by,scale", [(5.0, 1.0, 1.0, None), (0.5, 300.0, 1.0, None), (1.0, 1e-4, 1.0, None), (1.0, 0.5, 100.0, None), (1.0, 0.5, 1e-3, None),
                                                   (1.0, 0.5, 1.0, 5.0), (1.0, 0.5, 1.0, 1e-3)])
 @pytest.mark.parametrize("dtype", (BF16, F16))

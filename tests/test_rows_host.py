@@ -101,6 +101,7 @@ def test_chunk_workspace(lib):  # noqa: F811
     # room for the pieces that a call can have, however it grows
     assert need(longest=1 << 20) <= need(tokens=1 << 20, longest=1 << 20) == need(tokens=1 << 22, longest=1 << 22) < 160 << 20
     assert need(dim=64) < need()
+    assert 0 < need(requests=65, longest=64) < need(requests=1000, longest=64) < 1 << 15       # (where the requests' blocks end)
 
 
 def test_prompt_window_refuses(lib):  # noqa: F811
