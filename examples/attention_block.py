@@ -2,11 +2,13 @@
 """The attention block of a decoder layer on this library alone: any4 QKV and O projections, a paged key-value cache of 16, 8 or 4 bits,
 prompts (whole, or in parts behind what the cache already holds) and single tokens.
 
-    python examples/attention_block.py [--bits 8] [--requests 4] [--prompt 700] [--tokens 16]
+    python examples/attention_block.py [--bits 8] [--requests 4] [--prompt 700] [--tokens 16] [--window 256 [--sinks 4]] [--separate]
 
 Sizes are Llama-3-8B's (hidden 4096, 32 query heads on 8 KV heads of 128), weights and inputs synthetic.  It feeds each request a prompt in
 two parts and then token after token, and says how far the outputs are from the same block computed in one piece in 32 bits.
-PyTorch does the rotary embedding and the bookkeeping of pages.
+A layer is one call that turns q and k by their positions and writes k and v into the cache, and one of attention over the cache's pages.
+With --separate PyTorch does the rotary embedding, and a prompt's later part reads its context out of the cache first.  PyTorch does the
+bookkeeping of pages.
 """
 import argparse
 import os
@@ -108,8 +110,50 @@ class AttentionBlock:
         out = torch.empty_like(q)
         for j in range(h):
             s = (q[:, j] @ k[:, j].T.contiguous()) * d ** -0.5
-            out[:, j] = torch.softmax(s.masked_fill(at[:, None] < at, float("-inf")), -1) @ v[:, j]
+            out[:, j] = torch.softmax(s.masked_fill(~self._sees(at), float("-inf")), -1) @ v[:, j]
         return out.reshape(n, -1) @ weights[1].T
+
+    def _sees(self, at):
+        return at[:, None] >= at
+
+
+class FusedBlock(AttentionBlock):
+    """the same in two calls between the projections, prompts and single tokens alike; with a window, a token sees only the last `window` and
+    the first `sinks`"""
+
+    def __init__(self, *args, window=None, sinks=0, base=500000.0, **kw):
+        super().__init__(*args, **kw)
+        self.part = {} if window is None else dict(window=window, sinks=sinks)
+        self.freqs = base ** (-torch.arange(self.dim // 2, dtype=torch.float64, device=self.device) / (self.dim // 2))
+
+    def _project(self, x, positions, slots):
+        row = self.qkv(x)
+        n, h, g, d = x.shape[0], self.heads, self.kv_heads, self.dim
+        q, k, v = (t.view(n, -1, d) for t in row.split((h * d, g * d, g * d), 1))          # (as they lie in the projection's rows)
+        return any4.any4_rope_kv_write(q, k, v, positions, self.freqs, slots.to(self.device), self.cache_k, self.cache_v, self.scales, bits=self.bits,
+                                       out=q)                                               # (q is turned where it is)
+
+    def prompt(self, x, tokens):
+        before = list(self.lengths)
+        slots = torch.cat([self._grow(r, n) for r, n in enumerate(tokens)])
+        positions = torch.cat([torch.arange(b, b + n) for b, n in zip(before, tokens)]).to(self.device)
+        q = self._project(x, positions, slots)
+        starts = torch.tensor([0] + list(tokens), dtype=torch.int32).cumsum(0).to(torch.int32).to(self.device)
+        out = any4.any4_attn_chunk(q, self.cache_k, self.cache_v, self.table.to(self.device), starts,
+                                   torch.tensor(self.lengths, dtype=torch.int32, device=self.device), self.scales, bits=self.bits, **self.part)
+        return self.o(out.view(x.shape[0], -1))
+
+    def token(self, x):
+        positions = torch.tensor(self.lengths, device=self.device)
+        slots = torch.cat([self._grow(r, 1) for r in range(x.shape[0])])
+        q = self._project(x, positions, slots)
+        out = any4.any4_attn_decode(q, self.cache_k, self.cache_v, self.table.to(self.device),
+                                    torch.tensor(self.lengths, dtype=torch.int32, device=self.device), self.scales, bits=self.bits, **self.part)
+        return self.o(out.view(x.shape[0], -1))
+
+    def _sees(self, at):
+        ahead = at[:, None] - at
+        return (ahead >= 0) & ((ahead < self.part["window"]) | (at < self.part["sinks"]) if self.part else True)
 
 
 def run(block, requests, prompt, tokens, hidden, seed=0):
@@ -138,9 +182,17 @@ def main():
     ap.add_argument("--requests", type=int, default=4)
     ap.add_argument("--prompt", type=int, default=700)
     ap.add_argument("--tokens", type=int, default=16)
+    ap.add_argument("--window", type=int)
+    ap.add_argument("--sinks", type=int, default=0)
+    ap.add_argument("--separate", action="store_true")
     a = ap.parse_args()
+    if a.separate and a.window is not None:
+        ap.error("--window goes without --separate")
+    if a.sinks and a.window is None:
+        ap.error("--sinks go with --window")
     need = -(-(a.prompt + a.tokens) // 64)
-    block = AttentionBlock(bits=a.bits, requests=a.requests, max_pages=need, pages=need * a.requests)
+    sizes = dict(bits=a.bits, requests=a.requests, max_pages=need, pages=need * a.requests)
+    block = AttentionBlock(**sizes) if a.separate else FusedBlock(window=a.window, sinks=a.sinks, **sizes)
     outputs, x = run(block, a.requests, a.prompt, a.tokens, 4096)
     weights = [any4.any4_dequant(w.codes, w.lut, w.scale, w.offset, w.codes.shape[1] * 8, 4) for w in (block.qkv, block.o)]
     for r, y in enumerate(outputs):
