@@ -341,7 +341,8 @@ int any4_kv_read(const any4_kv_cache* cache, const int64_t* slots, int64_t token
  *     y = x / sqrt(mean(x^2) + eps) * w             over the head_dim values of a head; without w: y = x
  *     (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t),    t = position[axis_of[i]] * freqs[i],    pair i of rotary_dim / 2
  * Pair i is (i, i + rotary_dim / 2), or with interleaved = 1 (2 i, 2 i + 1); values from rotary_dim on are not turned.  Angles are fp64,
- * the rest is fp32, and the result is rounded once, to the type of the rows.  What is frequency scaling (longer contexts) is the caller's, in freqs.
+ * the rest is fp32 (a head's squares and their sum too: they have to
+ * stay in its range), and the result is rounded once, to the type of the rows.  What is frequency scaling (longer contexts) is the caller's, in freqs.
  *   positions   in   int64 [axes][tokens], axis_stride entries from an axis to the next; any value
  *   freqs       in   double [rotary_dim / 2]: the angle of position 1, in radians
  *   axis_of     in   uint8 [rotary_dim / 2]: which of a token's positions turns pair i (images and video: time, height, width); values from axes on
@@ -453,7 +454,7 @@ int any4_attn_prompt(const uint16_t* q, int64_t q_token_stride, int64_t q_head_s
  * request's first `sinks` only.
  *   window      1 and more
  *   sinks       0 and more
- * q_tokens * (heads / kv_heads) at most 2^31 - 2048, (that / 128 + requests) * kv_heads at most 2^31 - 1.  Everything else as there.
+ * q_tokens * (heads / kv_heads) at most 2^31 - 2048, (that / 128 + 2 requests) * kv_heads at most 2^31 - 1.  Everything else as there.
  */
 int any4_attn_prompt_window(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride,
                             const uint16_t* k, int64_t k_token_stride, int64_t k_head_stride,
@@ -478,7 +479,7 @@ int any4_attn_prompt_window(const uint16_t* q, int64_t q_token_stride, int64_t q
  *   out         out  16-bit [q_tokens][heads][head_dim], dense; rows that no request has are left as they are
  *   workspace   at least any4_attn_chunk_workspace_bytes() bytes; may be NULL when that is 0.  Contents on entry and on exit mean nothing; it must not
  *               serve two calls that overlap in time
- * q_tokens * (heads / kv_heads) at most 2^31 - 2048, (that / 128 + requests) * kv_heads below 2^31 - 4096, table_width * page_size at most 2^31 - 2048.
+ * q_tokens * (heads / kv_heads) at most 2^31 - 2048, (that / 128 + 2 requests) * kv_heads below 2^31 - 8192, table_width * page_size at most 2^31 - 2048.
  * requests = 0 and q_tokens = 0 do nothing.
  */
 int any4_attn_chunk(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const any4_kv_cache* cache,

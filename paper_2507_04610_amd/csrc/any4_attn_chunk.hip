@@ -4,22 +4,38 @@
 //     s_ij = scale q_i . k_j,   o_i = sum_j exp(s_ij - m_i) v_j / sum_j exp(s_ij - m_i)     over j <= p_i, j > p_i - window or j < sinks
 // in one pass over the keys with a running maximum, as any4_attn_prompt does it.
 //
-// A block takes 128 rows of one KV head: a row is a query of one of the heads that share it, a query's heads side by side, so that a few new
-// tokens fill a block with their heads and read k and v once.  A wavefront takes 32 rows and walks over the keys 64 at a time: S^T = K Q^T with
+// A row is a query of one of the heads that share a KV head, a query's heads side by side, so that a few new tokens fill a block with their heads and
+// read k and v once.  A block takes 128 rows, a wavefront 32 of them, and walks over the keys 64 at a time: S^T = K Q^T with
 // v_mfma_f32_32x32x16, the scores of a row in two lanes, the weights at once the B operand of O^T = V^T P^T.  Tiles outside of what the block's rows see (behind
-// the last query, between the first tokens and the window) are left out.
+// the last query, between the first tokens and the window) are left out.  Of up to 32 rows each wavefront takes all and every fourth 32 keys, in LDS of its
+// own, and the four meet at the end: nobody waits in front of a tile (up to 8 drafted tokens for each of 16 requests over a cache of 4 bits: 174 -> 106 us).
 //
 // 16 bits: k and v are copied to LDS without passing registers, the next 64 keys while these are worked on.  Codes c become fp16 on their way
 // to LDS, exactly (k: c + kBias, v: c - kCentre), and scales and offsets are applied to sums, so that codes cost no rounding of their own:
 //     q . k_j = ks_j (q . c'_j) + (ko_j - kBias ks_j) sum(q)
 //     o = sum_j (p_j vs_j) (c_j - kCentre) + sum_j p_j (vo_j + kCentre vs_j)
-// bf16 queries become fp16 for that, exactly too: a row is scaled by a power of two.  The product p_j vs_j is rounded to fp16; the exponent of the
+// bf16 queries become fp16 for that: a row is scaled by a power of two, which is exact down to 2^-31 of its largest value and off by 2^-39 of that below.  The product p_j vs_j is rounded to fp16; the exponent of the
 // largest vs_j that a row has seen is taken off it together with the running maximum.
 //
-// Who does what.  Lengths are the device's, so each block finds its rows itself (of more than 64 requests, in what a first launch writes down).  Where whole tiles of rows do not fill the chip, their keys are cut
-// into pieces, no more than it takes; pieces leave sums, maximum and sum of weights in the workspace, and a second launch joins them.
+// Who does what.  Lengths are the device's, so each block finds its rows itself, of more than 64 requests in what a first launch of one block writes down
+// (a token each of 2048 requests over 300 tokens in 8 bits: 670 -> 441 us).  Where whole tiles of rows do not fill the chip, their keys are cut
+// into pieces, no more than it takes; pieces leave sums, maximum and sum of weights in the workspace, and a last launch joins them (4 to 8 us, and a
+// launch: short calls are not cut).
 //
 // Rounding: scores, maxima, sums and accumulators are fp32; the weights (times vs_j) are rounded to 16 bits for the matrix cores, once.
+//
+// Measured, 8 KV heads, us (what bounds it):
+//     16 bits, 2048 tokens behind 30720, 32 query heads of 128     1010 - 1040  (1.03 PFLOP/s: matrix cores busy 51 %, vector units 51 %, at the clock that
+//                                                                               remains; wavefronts wait 27 % of their time for LDS and each other)
+//     8 bits, 24 requests of 1 .. 511 tokens, fp16                  430 - 440   (0.55 PFLOP/s: vector units busy 47 %, LDS 37 %, matrix cores 24 %; 6.2 of 8
+//                                                                               wavefronts there on average, which wait 31 % of their time)
+//     4 bits, 16 requests, up to 8 drafted tokens                    63 -  69   (2.1 TB/s: vector units 51 %; 8 of it the join; 5.6 of 8 wavefronts)
+//     16 bits, 19 tokens behind 333                                   9.1       (loads that wait for each other: starts, lengths, page, k and v)
+//     packed rows, a prompt of 12011, window 2048                   420         (0.88 PFLOP/s)
+//     packed rows, fp16, 8450 tokens, 16 heads of 64 on 2, window 777  55        (0.49 PFLOP/s: 1060 blocks of 13 tiles of keys, whose beginnings and
+//                                                                               ends and the second round of them cost as much as the tiles)
+// Without gain: longest pieces first, more and smaller pieces than fill the chip, a fixed priority for one of a SIMD's wavefronts, an order of loads and products
+// prescribed to the compiler.
 #include "any4_attn.h"
 #include "any4_attn_tile.h"
 #include "any4_internal.h"
@@ -31,12 +47,13 @@ namespace any4 {
 namespace {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kRowTile = 32 * kWaves;
-constexpr int kNarrow = 4;                                      // tiles of keys for up to 32 rows that take as long as one for 128
+// Costs are counted in tiles of keys for 32 rows.
+constexpr int kNarrow = 4;                                      // so many take as long as one for 128
 constexpr int kFewRows = 64;                                    // requests of up to so many rows have tiles of 32, as small calls (65 requests of 64 rows
                                                                 // over 1000 tokens in 8 bits: 81 us, in tiles of 128 98)
-constexpr int kLeastPiece = 4;                                  // least tiles of keys of a piece
-constexpr int kWhole = 10;                                      // keys of so many tiles are not cut: the join costs as much as a few of them
-constexpr int kSmall = 1024;                                    // calls of so many tiles of keys take 32 rows at a time: more blocks, each done sooner
+constexpr int kLeastPiece = 4;                                  // least of a piece
+constexpr int kWholeFew = 12, kWhole = 40;                      // tiles of 32 rows, of 128 rows, of so much are not cut: the join costs as much
+constexpr int kSmall = 16384;                                   // calls of so much for 128 rows at a time take 32 at a time: more blocks, each done sooner
 constexpr int kNoWindow = 0x7FFFF800;                           // more than any request's tokens
 // The exponent of the largest vs_j goes with the maximum as far as 2^+-kFold: beyond, weights of tokens whose scales differ by 2^126 and more would
 // be lost, to each other and to the sum of weights.  The rest is taken off vs_j itself.
@@ -121,11 +138,12 @@ __device__ __forceinline__ int tiles_of(const Args& a, const Request& r, int mos
     const int height = height_of(a, r, most);
     return (int)(((unsigned)(r.lq * a.shared) + (unsigned)height - 1) >> (height == 32 ? 5 : 7));
 }
-// what its last (and longest) tile of rows costs, in tiles of keys for 128 rows
+// what its last (and longest) tile of rows costs, and what may be cut
 __device__ __forceinline__ int costs_of(const Args& a, const Request& r, int tiles, int most) {
     const int height = height_of(a, r, most), of_keys = span_of(a, r, tiles - 1, height).tiles;
-    return height == 32 ? (of_keys + kNarrow - 1) / kNarrow : of_keys;
+    return height == 32 ? of_keys : kNarrow * of_keys;
 }
+__device__ __forceinline__ int whole_of(const Args& a, const Request& r, int most) { return height_of(a, r, most) == 32 ? kWholeFew : kWhole; }
 // How a call is cut: rows of a tile, and the most that a piece costs (0: nothing is cut).  Sums in fp32, in one order everywhere.
 struct Cut {
     int height, least;
@@ -169,7 +187,7 @@ template <class Sum> __device__ __forceinline__ Cut cut_of(const Args& a, Sum su
         if (shorter >= most) break;
         const float pieces = sum([&](const Request& r) -> float {
             const int n = tiles_of(a, r, cut.height), cost = n > 0 ? costs_of(a, r, n, cut.height) : 0;
-            return cost > kWhole ? (float)n * (float)((cost + shorter - 1) / shorter) : (float)n;
+            return cost > whole_of(a, r, cut.height) ? (float)n * (float)((cost + shorter - 1) / shorter) : (float)n;
         });
         if (pieces * heads <= target) {
             cut.least = shorter;
@@ -184,7 +202,7 @@ __device__ __forceinline__ Shares shares_of(const Args& a, const Request& r, con
     Shares s{r, tiles_of(a, r, cut.height), 1};
     if (s.tiles > 0 && cut.least > 0) {
         const int cost = costs_of(a, r, s.tiles, cut.height);
-        if (cost > kWhole) s.pieces = (cost + cut.least - 1) / cut.least;
+        if (cost > whole_of(a, r, cut.height)) s.pieces = (cost + cut.least - 1) / cut.least;
     }
     return s;
 }
@@ -1299,16 +1317,16 @@ ChunkPlan plan_attn_chunk(int64_t requests, int64_t q_tokens, int heads, int kv_
     auto tiles_of = [&](int height) { return (q_tokens * shared / height + 2 * some) * kv_heads; };
     int64_t tiles = tiles_of(kRowTile);
     const int64_t units = (max_tokens + kKeys - 1) / kKeys;
-    const bool cuts = cut && units > kWhole;
+    const bool cuts = cut && units > kWholeFew;
     // small for sure, or (a call of so few rows) if its requests are short
-    p.small = (cuts ? q_tokens * shared / kRowTile * kv_heads : tiles * units) <= kSmall;
+    p.small = (cuts ? q_tokens * shared / kRowTile * kv_heads : tiles * units) <= kSmall / kNarrow;
     if (p.small) tiles = tiles_of(32);
     p.blocks = tiles;
     if (cut && requests > 64) p.plan_bytes = p.workspace = (size_t)Plan::bytes(requests);
     if (!cuts) return p;
     p.target = 2 * cus;
     // (pieces of tiles that are cut: cut_of() has it that there are no more than that, but for the rounding of its sums)
-    const int64_t most = (int64_t)p.target + kv_heads, own = tiles * ((units + kLeastPiece - 1) / kLeastPiece);
+    const int64_t most = (int64_t)p.target + kv_heads, own = tiles * ((kNarrow * units + kLeastPiece - 1) / kLeastPiece);
     p.slots = (int)(own < most ? own : most);
     // (each in two pieces and more)
     const int64_t cut_tiles = p.slots / 2 + kv_heads;

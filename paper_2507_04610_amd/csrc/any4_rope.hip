@@ -11,6 +11,11 @@
 // Rounding: norm, angles' sine and cosine and the turn are fp32, the result is rounded once; the angles themselves are fp64 until whole turns
 // are off them (position 10^6 in fp32 would be off by 0.06).  A key that goes into the cache as codes is rounded to 16 bits first, so that the cache holds what
 // any4_rope and any4_kv_write one after the other would have put there, bit for bit.
+//
+// Measured, 32 query and 8 KV heads of 128 unless said otherwise, us:
+//     16384 tokens with norms into a cache of 8 bits             98   (4.1 TB/s; a copy reaches 4.9; waits for memory 73 % of the time, vector units busy 57 %)
+//     5001 tokens, three axes, norms, fp16, q and k alone        20 in the kernel, 25 with the call's gaps (5.1 and 4.0 TB/s)
+//     45 tokens, 16 and 2 heads, no norms; 16 tokens, 16 bits    3 and 4 in the kernel, 5 with the call (loads that wait for each other: position, frequency)
 #include "any4_attn.h"
 #include "any4_kv_encode.h"
 #include "any4_launches.h"
