@@ -14,8 +14,8 @@
 // to LDS, exactly (k: c + kBias, v: c - kCentre), and scales and offsets are applied to sums, so that codes cost no rounding of their own:
 //     q . k_j = ks_j (q . c'_j) + (ko_j - kBias ks_j) sum(q)
 //     o = sum_j (p_j vs_j) (c_j - kCentre) + sum_j p_j (vo_j + kCentre vs_j)
-// bf16 queries become fp16 for that: a row is scaled by a power of two, which is exact down to 2^-31 of its largest value and off by 2^-39 of that below.  The product p_j vs_j is rounded to fp16; the exponent of the
-// largest vs_j that a row has seen is taken off it together with the running maximum.
+// bf16 queries become fp16 for that: a row is scaled by a power of two, which is exact down to 2^-31 of its largest value and off by 2^-39 of that
+// below.  The product p_j vs_j is rounded to fp16; the exponent of the largest vs_j that a row has seen is taken off it together with the running maximum.
 //
 // Who does what.  Lengths are the device's, so each block finds its rows itself, of more than 64 requests in what a first launch of one block writes down
 // (a token each of 2048 requests over 300 tokens in 8 bits: 670 -> 441 us).  Where whole tiles of rows do not fill the chip, their keys are cut
@@ -25,13 +25,13 @@
 // Rounding: scores, maxima, sums and accumulators are fp32; the weights (times vs_j) are rounded to 16 bits for the matrix cores, once.
 //
 // Measured, 8 KV heads, us (what bounds it):
-//     16 bits, 2048 tokens behind 30720, 32 query heads of 128     1010 - 1040  (1.03 PFLOP/s: matrix cores busy 51 %, vector units 51 %, at the clock that
+//     16 bits, 2048 tokens behind 30720, 32 query heads of 128     1005 - 1040  (1.05 PFLOP/s: matrix cores busy 51 %, vector units 51 %, at the clock that
 //                                                                               remains; wavefronts wait 27 % of their time for LDS and each other)
-//     8 bits, 24 requests of 1 .. 511 tokens, fp16                  430 - 440   (0.55 PFLOP/s: vector units busy 47 %, LDS 37 %, matrix cores 24 %; 6.2 of 8
+//     8 bits, 24 requests of 1 .. 511 tokens, fp16                  414 - 440   (0.57 PFLOP/s: vector units busy 47 %, LDS 37 %, matrix cores 24 %; 6.2 of 8
 //                                                                               wavefronts there on average, which wait 31 % of their time)
-//     4 bits, 16 requests, up to 8 drafted tokens                    63 -  69   (2.1 TB/s: vector units 51 %; 8 of it the join; 5.6 of 8 wavefronts)
+//     4 bits, 16 requests, up to 8 drafted tokens                    65 -  70   (2.1 TB/s: vector units 51 %; 8 of it the join; 5.6 of 8 wavefronts)
 //     16 bits, 19 tokens behind 333                                   9.1       (loads that wait for each other: starts, lengths, page, k and v)
-//     packed rows, a prompt of 12011, window 2048                   420         (0.88 PFLOP/s)
+//     packed rows, a prompt of 12011, window 2048                   412         (0.90 PFLOP/s)
 //     packed rows, fp16, 8450 tokens, 16 heads of 64 on 2, window 777  55        (0.49 PFLOP/s: 1060 blocks of 13 tiles of keys, whose beginnings and
 //                                                                               ends and the second round of them cost as much as the tiles)
 // Without gain: longest pieces first, more and smaller pieces than fill the chip, a fixed priority for one of a SIMD's wavefronts, an order of loads and products
@@ -47,13 +47,18 @@ namespace any4 {
 namespace {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kRowTile = 32 * kWaves;
-// Costs are counted in tiles of keys for 32 rows.
+// Costs are counted in tiles of keys for 32 rows.  Figures: us with 32 query heads on 8 KV heads of 128, 16 bits unless said otherwise.
 constexpr int kNarrow = 4;                                      // so many take as long as one for 128
 constexpr int kFewRows = 64;                                    // requests of up to so many rows have tiles of 32, as small calls (65 requests of 64 rows
                                                                 // over 1000 tokens in 8 bits: 81 us, in tiles of 128 98)
-constexpr int kLeastPiece = 4;                                  // least of a piece
-constexpr int kWholeFew = 12, kWhole = 40;                      // tiles of 32 rows, of 128 rows, of so much are not cut: the join costs as much
-constexpr int kSmall = 16384;                                   // calls of so much for 128 rows at a time take 32 at a time: more blocks, each done sooner
+// Least of a piece.  19 tokens behind 1000: 13.6, with 8 15.8, with 16 18; one token behind 8000 16.5, 15.8, 20.5.
+constexpr int kLeastPiece = 4;
+// Tiles of 32 rows, of 128 rows, of so much are not cut: writing pieces and joining them costs as much.  19 tokens behind 700 (11 tiles): whole 12.9, cut 13.5; behind
+// 1000 whole 15.4, cut 13.6; behind 1500 whole 20.0, cut 13.7.  (Where no request can have more, the join is not launched either.)
+constexpr int kWholeFew = 12, kWhole = 40;
+// Calls of so much for 128 rows at a time take 32 at a time: more blocks, each done sooner.  19 tokens behind 32000: 40, with 4096 55; 512 tokens from the
+// beginning 12.9, 18; 4 requests of 100 of 1000 tokens in 8 bits 34, 48; but 512 behind 7488 98, with 65536 117, and 2048 from the beginning 67, 90.
+constexpr int kSmall = 16384;
 constexpr int kNoWindow = 0x7FFFF800;                           // more than any request's tokens
 // The exponent of the largest vs_j goes with the maximum as far as 2^+-kFold: beyond, weights of tokens whose scales differ by 2^126 and more would
 // be lost, to each other and to the sum of weights.  The rest is taken off vs_j itself.
@@ -76,6 +81,8 @@ struct Args {
     int target, slots;                 // blocks that fill the chip (0: nothing is cut); pieces that the workspace has room for
     int small;                         // whether the call may be one that takes 32 rows at a time
     const int* plan;                   // more than 64 requests: where each one's blocks end (see Plan); NULL: blocks look for themselves
+    int* joins;                        // what the join has to do (see Join); NULL: nothing is cut
+    int cut_tiles;                     // room in it
     unsigned first_block;              // of this launch
     float scale_log2;
     uint16_t* out;
@@ -89,11 +96,14 @@ struct Args {
 // A request's rows and keys.
 struct Request {
     int q_at, lq, k_at, lk;
+    bool back;                         // its rows would end in front of where they begin
 };
 template <int SOURCE> __device__ __forceinline__ Request request_of(const Args& a, int r) {
     Request q;
     q.q_at = min(max(a.q_starts[r], 0), a.q_tokens);
-    q.lq = max(min(max(a.q_starts[r + 1], 0), a.q_tokens) - q.q_at, 0);
+    const int lq = min(max(a.q_starts[r + 1], 0), a.q_tokens) - q.q_at;
+    q.lq = max(lq, 0);
+    q.back = lq < 0;
     if constexpr (SOURCE == kRows) {
         q.k_at = min(max(a.k_starts[r], 0), a.k_tokens);
         q.lk = max(min(max(a.k_starts[r + 1], 0), a.k_tokens) - q.k_at, 0);
@@ -126,6 +136,7 @@ __device__ __forceinline__ Span span_of(const Args& a, const Request& r, int til
 // Which rows and keys a block has.  Blocks of a request: tile of rows by tile of rows, each tile's pieces side by side.
 struct Work {
     int request, tile, piece, pieces, slot, height;
+    int join;                          // which of the tiles of rows that are cut (without KV heads)
     Request r;
 };
 struct Shares {                        // of 64 requests, a lane each
@@ -167,7 +178,8 @@ template <class Sum> __device__ __forceinline__ Cut cut_of(const Args& a, Sum su
     auto costs = [&](int height) {
         return sum([&](const Request& r) -> float {
             const int n = tiles_of(a, r, height);
-            return n > 0 ? (float)n * (float)costs_of(a, r, n, height) : 0.0f;
+            // (where starts go back, requests may have more tiles together than there are blocks, and nothing is cut)
+            return r.back ? 1e30f : n > 0 ? (float)n * (float)costs_of(a, r, n, height) : 0.0f;
         }) * heads;
     };
     float all = costs(kRowTile);
@@ -206,10 +218,17 @@ __device__ __forceinline__ Shares shares_of(const Args& a, const Request& r, con
     }
     return s;
 }
+// Tiles of rows that are cut, for the launch that joins them, which then has nothing to look for (where nothing turns out to be cut that is 3 us less than if its
+// blocks looked: 4 requests of 100 of 1000 tokens 34.5 -> 31.7 us).  First how many there are, then of each:
+struct alignas(16) Join {
+    int q_at, rows, row, height;       // the request's first query and rows, the tile's first row, its rows at most
+    int pieces, slot, unused[2];       // pieces with keys, the first one's place
+    __host__ __device__ static int64_t bytes(int64_t tiles) { return ((tiles + 1) * (int64_t)sizeof(Join) + 255) / 256 * 256; }
+};
 // More than 64 requests: a launch in front of the others has one block find out what each would find for itself.
 struct Plan {
-    // [4][requests] behind the height of tiles of rows: where a request's blocks end, where its tiles that are cut end (both without KV heads), its
-    // first piece's place, its pieces
+    // [4][requests] behind the height of tiles of rows: where a request's blocks end, where its tiles that are cut begin, its first piece's place (all
+    // without KV heads), its pieces
     static constexpr int kHeader = 4;
     __host__ __device__ static int64_t bytes(int64_t requests) { return (4 * (kHeader + 4 * requests) + 255) / 256 * 256; }
 };
@@ -252,19 +271,19 @@ __global__ __launch_bounds__(kPlanThreads) void attn_chunk_plan_kernel(Args a, i
         const int cut = s.pieces > 1 ? s.tiles * s.pieces : 0, cut_end = scan(0, cut);
         // (as many as were planned for; were there more, they would be left whole)
         if (cut > 0 && (int64_t)cut_end * a.kv_heads > a.slots) s.pieces = 1;
-        const int end = scan(1, s.tiles * s.pieces), join_end = scan(2, s.pieces > 1 ? s.tiles : 0);
+        const int joins = s.pieces > 1 ? s.tiles : 0, end = scan(1, s.tiles * s.pieces), join_end = scan(2, joins);
         if (r < a.requests) {
             at[r] = end;
-            at[a.requests + r] = join_end;
+            at[a.requests + r] = join_end - joins;
             at[2 * a.requests + r] = cut_end - cut;
             at[3 * a.requests + r] = s.pieces;
         }
     }
+    if (a.joins && threadIdx.x == 0) a.joins[0] = before[2] * a.kv_heads;
 }
-template <int SOURCE, bool JOIN> __device__ __forceinline__ Work planned(const Args& a, unsigned place, unsigned kv_head, int lane) {
-    Work w{-1, 0, 0, 1, 0, a.plan[0], {}};
-    const int* const at = a.plan + Plan::kHeader;
-    const int* const ends = at + (JOIN ? a.requests : 0);
+template <int SOURCE> __device__ __forceinline__ Work planned(const Args& a, unsigned place, unsigned kv_head, int lane) {
+    Work w{-1, 0, 0, 1, 0, a.plan[0], 0, {}};
+    const int* const ends = a.plan + Plan::kHeader;
     // the first request that ends behind `place`, among 64 at a time
     int from = 0, n = a.requests;
     for (;;) {
@@ -279,22 +298,23 @@ template <int SOURCE, bool JOIN> __device__ __forceinline__ Work planned(const A
     w.request = __builtin_amdgcn_readfirstlane(from);
     w.r = request_of<SOURCE>(a, w.request);
     w.height = height_of(a, w.r, w.height);
-    w.pieces = at[3 * a.requests + w.request];
-    const int begin = w.request > 0 ? ends[w.request - 1] : 0, all = ends[w.request] - begin, own = (int)place - begin, tile = JOIN ? own : own / w.pieces;
-    w.piece = JOIN ? 0 : own - tile * w.pieces;
-    w.tile = (JOIN ? all : all / w.pieces) - 1 - tile;          // the most keys first
-    w.slot = (at[2 * a.requests + w.request] + tile * w.pieces + w.piece) * a.kv_heads + (int)kv_head;
+    w.pieces = ends[3 * a.requests + w.request];
+    const int begin = w.request > 0 ? ends[w.request - 1] : 0, all = ends[w.request] - begin, own = (int)place - begin, tile = own / w.pieces;
+    w.piece = own - tile * w.pieces;
+    w.tile = all / w.pieces - 1 - tile;                         // the most keys first
+    w.join = ends[a.requests + w.request] + tile;
+    w.slot = (ends[2 * a.requests + w.request] + tile * w.pieces + w.piece) * a.kv_heads + (int)kv_head;
     if ((unsigned)own >= (unsigned)all) w.request = -1;         // (starts that do not ascend can add up to more than 32 bits hold)
     return w;
 }
 
-// JOIN: place counts the tiles of rows that are cut, otherwise blocks; both without KV heads
-template <int SOURCE, bool JOIN> __device__ __forceinline__ Work work_of(const Args& a, unsigned place, unsigned kv_head, int lane) {
-    if (a.plan) return planned<SOURCE, JOIN>(a, place, kv_head, lane);
+// place: of the block, without KV heads
+template <int SOURCE> __device__ __forceinline__ Work work_of(const Args& a, unsigned place, unsigned kv_head, int lane) {
+    if (a.plan) return planned<SOURCE>(a, place, kv_head, lane);
     // (where something is cut there are no more than 64 requests)
     const Request first = lane < a.requests ? request_of<SOURCE>(a, lane) : Request{};
     const Cut how = cut_of(a, [&](auto f) { return lanes_total(f(first)); });
-    Work w{-1, 0, 0, 1, 0, how.height, {}};
+    Work w{-1, 0, 0, 1, 0, how.height, 0, {}};
     for (int r0 = 0, before = 0, cut_before = 0; r0 < a.requests && w.request < 0; r0 += 64) {
         Request r = first;
         if (r0 > 0) r = r0 + lane < a.requests ? request_of<SOURCE>(a, r0 + lane) : Request{};
@@ -306,7 +326,12 @@ template <int SOURCE, bool JOIN> __device__ __forceinline__ Work work_of(const A
             s.pieces = 1;
             cut = 0;
         }
-        const int own = JOIN ? (s.pieces > 1 ? s.tiles : 0) : s.tiles * s.pieces, sum = lanes_scan(own);
+        const int own = s.tiles * s.pieces, sum = lanes_scan(own), joins = s.pieces > 1 ? s.tiles : 0;
+        int joins_sum = 0;
+        if (a.joins) {
+            joins_sum = lanes_scan(joins);
+            if ((place | kv_head) == 0u && threadIdx.x == 63) a.joins[0] = joins_sum * a.kv_heads;
+        }
         const unsigned long long past = __builtin_amdgcn_ballot_w64((unsigned)(before + sum) > place);
         if (past) {
             const int f = __builtin_ctzll(past);
@@ -323,9 +348,10 @@ template <int SOURCE, bool JOIN> __device__ __forceinline__ Work work_of(const A
                 w.request = -1;
                 break;
             }
-            const int tile = JOIN ? at : at / w.pieces;
-            w.piece = JOIN ? 0 : at - tile * w.pieces;
+            const int tile = at / w.pieces;
+            w.piece = at - tile * w.pieces;
             w.tile = tiles - 1 - tile;                          // the most keys first
+            w.join = __builtin_amdgcn_readlane(joins_sum - joins, f) + tile;
             w.slot = (cut_before + __builtin_amdgcn_readlane(cut_sum, f) - tiles * w.pieces + tile * w.pieces + w.piece) * a.kv_heads + (int)kv_head;
         }
         before += __builtin_amdgcn_readlane(sum, 63);
@@ -427,13 +453,18 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
 
     // KV heads fastest: blocks that read the same keys tend to share an XCD and its L2
     const unsigned block = a.first_block + blockIdx.x, place = block / (unsigned)a.kv_heads, kv_head = block - place * (unsigned)a.kv_heads;
-    const Work w = work_of<SOURCE, false>(a, place, kv_head, lane);
+    const Work w = work_of<SOURCE>(a, place, kv_head, lane);
     if (w.request < 0) return;
     const int lq = w.r.lq, lk = w.r.lk, rows = lq * a.shared, ahead = lk - lq;
     const Span span = span_of(a, w.r, w.tile, w.height);
     const int each = (span.tiles + w.pieces - 1) / w.pieces;
     const int t_first = w.piece * each, t_end = min(span.tiles, t_first + each);
-    if (w.pieces > 1 && t_first >= t_end) return;               // (the join knows)
+    if (w.pieces > 1) {
+        const int at = w.join * a.kv_heads + (int)kv_head;
+        if (w.piece == 0 && threadIdx.x == 0 && at < a.cut_tiles)
+            reinterpret_cast<Join*>(a.joins)[1 + at] = Join{w.r.q_at, rows, w.tile * w.height, w.height, each > 0 ? (span.tiles + each - 1) / each : 0, w.slot, {0, 0}};
+        if (t_first >= t_end) return;                           // (the join knows)
+    }
 
     // Up to 32 rows: each wavefront takes all of them and every fourth 32 keys, otherwise 32 rows and all keys.
     const bool narrow = w.height == 32 || rows - w.tile * kRowTile <= 32;
@@ -1229,20 +1260,18 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
 
 // Joins the pieces of tiles of rows that were cut: a wavefront has 32 rows at a time and four values of each, in the pieces' own order of lanes.
 constexpr int kAtOnce = 16;                                     // pieces whose loads are out at a time
-template <int SOURCE, int D, bool F16>
+template <int D, bool F16>
 __global__ __launch_bounds__(256) void attn_chunk_join_kernel(Args a) {
     const int lane = threadIdx.x & 63, n = lane & 31, g = lane >> 5;
-    const unsigned place = blockIdx.x / (unsigned)a.kv_heads, kv_head = blockIdx.x - place * (unsigned)a.kv_heads;
-    const Work w = work_of<SOURCE, true>(a, place, kv_head, lane);
-    if (w.request < 0) return;
-    const int rows = w.r.lq * a.shared;
-    const Span span = span_of(a, w.r, w.tile, w.height);
-    const int each = (span.tiles + w.pieces - 1) / w.pieces, pieces = each > 0 ? min(w.pieces, (span.tiles + each - 1) / each) : 0;
+    if ((int)blockIdx.x >= a.joins[0]) return;
+    const unsigned kv_head = blockIdx.x % (unsigned)a.kv_heads;
+    const Join w = reinterpret_cast<const Join*>(a.joins)[1 + blockIdx.x];
+    const int rows = w.rows, pieces = w.pieces;
     const int64_t step = (int64_t)a.kv_heads * kPieceFloats<D>;
     const float* first = a.partial + (int64_t)w.slot * kPieceFloats<D>;
     const int four = 4 * (int)blockIdx.y + (int)(threadIdx.x >> 6);
-    for (int part = 0; 32 * part < w.height && w.tile * w.height + 32 * part < rows; ++part) {
-        const int row = w.tile * w.height + 32 * part + n;
+    for (int part = 0; 32 * part < w.height && w.row + 32 * part < rows; ++part) {
+        const int row = w.row + 32 * part + n;
         const float* ml = first + kRowTile * D + 2 * (32 * part + n);
         const int query = a.query_of(min(row, rows - 1)), head = (int)kv_head * a.shared + (min(row, rows - 1) - query * a.shared);
         const float* sums = first + 4 * ((part * (D / 8) + four) * 64 + lane);
@@ -1276,7 +1305,7 @@ __global__ __launch_bounds__(256) void attn_chunk_join_kernel(Args a) {
         }
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
         if (row < rows) {
-            uint16_t* out = a.out + ((int64_t)(w.r.q_at + query) * a.heads + head) * D + 8 * four + 4 * g;
+            uint16_t* out = a.out + ((int64_t)(w.q_at + query) * a.heads + head) * D + 8 * four + 4 * g;
             *reinterpret_cast<u32x2*>(out) = u32x2{pack<F16>(v[0] * inv, v[1] * inv), pack<F16>(v[2] * inv, v[3] * inv)};
         }
     }
@@ -1291,9 +1320,14 @@ template <int SOURCE, int D, bool F16> hipError_t launch(Args a, const ChunkPlan
     a.target = pl.target;
     a.slots = pl.slots;
     a.small = pl.small;
+    int* const plan = reinterpret_cast<int*>(a.partial);
+    a.partial += pl.plan_bytes / sizeof(float);
+    if (pl.target > 0) {
+        a.joins = reinterpret_cast<int*>(a.partial);
+        a.cut_tiles = pl.cut_tiles;
+        a.partial += Join::bytes(pl.cut_tiles) / sizeof(float);
+    }
     if (pl.plan_bytes > 0) {
-        int* const plan = reinterpret_cast<int*>(a.partial);
-        a.partial += pl.plan_bytes / sizeof(float);
         hipLaunchKernelGGL((attn_chunk_plan_kernel<SOURCE>), dim3(1), dim3(kPlanThreads), 0, stream, a, plan);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
         a.plan = plan;
@@ -1304,7 +1338,7 @@ template <int SOURCE, int D, bool F16> hipError_t launch(Args a, const ChunkPlan
         return hipGetLastError();
     });
     if (e != hipSuccess || pl.target == 0) return e;
-    hipLaunchKernelGGL((attn_chunk_join_kernel<SOURCE, D, F16>), dim3((unsigned)pl.cut_tiles, D / 32), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((attn_chunk_join_kernel<D, F16>), dim3((unsigned)pl.cut_tiles, D / 32), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -1332,13 +1366,13 @@ ChunkPlan plan_attn_chunk(int64_t requests, int64_t q_tokens, int heads, int kv_
     const int64_t cut_tiles = p.slots / 2 + kv_heads;
     p.cut_tiles = (int)(tiles < cut_tiles ? tiles : cut_tiles);
     p.blocks = tiles + p.slots;
-    p.workspace += (size_t)p.slots * kRowTile * (head_dim + 2) * sizeof(float);
+    p.workspace += (size_t)Join::bytes(p.cut_tiles) + (size_t)p.slots * kRowTile * (head_dim + 2) * sizeof(float);
     return p;
 }
 
 hipError_t launch_attn_chunk(const ChunkArgs& c, const any4_kv_cache* cache, const ChunkPlan& pl, void* workspace, hipStream_t stream) {
     Args a{c.q, c.k, c.v, {}, c.table, c.table_stride, (int)c.table_width, c.q_starts, c.k_starts, c.lengths, (int)c.q_tokens, (int)c.k_tokens, c.requests,
-           c.heads, c.kv_heads, c.heads / c.kv_heads, c.window > 0 ? c.window : kNoWindow, c.sinks, 0, 0, 0, nullptr, 0u, c.softmax_scale * kLog2e, c.out,
+           c.heads, c.kv_heads, c.heads / c.kv_heads, c.window > 0 ? c.window : kNoWindow, c.sinks, 0, 0, 0, nullptr, nullptr, 0, 0u, c.softmax_scale * kLog2e, c.out,
            static_cast<float*>(workspace), 0u, 31};
     while ((int64_t)1 << (a.shared_shift - 31) < a.shared) ++a.shared_shift;
     a.shared_mul = (uint32_t)((((uint64_t)1 << a.shared_shift) + (uint64_t)a.shared - 1) / (uint64_t)a.shared);

@@ -247,6 +247,32 @@ def test_queries_without_tokens_and_rows_of_no_request(bits):
         assert torch.equal(p.run(out=out)[same], want[same])
 
 
+@pytest.mark.parametrize("bits", (16, 8, 4))
+@pytest.mark.parametrize("requests", (3, 41, 80))
+def test_starts_that_go_back_behind_long_contexts(bits, requests):
+    """rows of one request alone are its own, and all stays within the rows that some request names, whatever the workspace holds"""
+    p = Chunks([(64, 6000)] + [(0, 6064)] * (requests - 1), bits, BF16, 128, 8, 2, 64, behind=6)
+    need = any4.any4_attn_chunk_workspace_bytes(requests, len(p.q), 8, 2, 128, p.width * 64)
+    ws = torch.empty(need + 4096, dtype=torch.uint8, device="cuda").fill_(0xA5)
+    p.check(p.run(workspace=ws[:need]))                          # (leaves what it cut in the workspace)
+    out = torch.full(p.q.shape, 3.0, dtype=BF16, device="cuda")
+    starts = [0, 40, 10, 60] + [60] * (requests - 3)
+    p.starts.copy_(torch.tensor(starts, dtype=torch.int32))
+    p.run(out=out, workspace=ws[:need])
+    assert (out[60:] == 3).all() and (ws[need:] == 0xA5).all()
+    for i, alone, at in ((0, range(0, 10), 0), (2, range(40, 60), 10)):
+        p.new[i] = starts[i + 1] - starts[i]
+        seen = p.seen(i)
+        for h in range(8):
+            k, v, *codes = p.held(i, h // 4)
+            rows = slice(alone.start, alone.stop)
+            o, allowed = ref.bound(p.q[rows, h].double().cpu().numpy(), k, v, seen[alone.start - at:alone.stop - at], 128 ** -0.5, BF16, bits, *codes)
+            assert (np.abs(out[rows, h].double().cpu().numpy() - o) <= allowed).all()
+    p.starts.copy_(torch.tensor(([0, 64] * requests)[:requests + 1], dtype=torch.int32))      # more rows together than the call has
+    p.run(out=out, workspace=ws[:need])
+    assert (out[64:] == 3).all() and (ws[need:] == 0xA5).all() and out.isfinite().all()
+
+
 @pytest.mark.parametrize("dtype,by", [(F16, 2.0 ** 13), (BF16, 2.0 ** 14), (BF16, 2.0 ** 17)])
 @pytest.mark.parametrize("bits", (16, 8))
 def test_far_scores(dtype, by, bits):

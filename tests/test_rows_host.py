@@ -96,7 +96,7 @@ def test_chunk_refuses_bad_caches(lib, change, code):  # noqa: F811
 def test_chunk_workspace(lib):  # noqa: F811
     def need(requests=3, tokens=40, heads=32, kv_heads=8, dim=128, longest=4096):
         return lib.any4_attn_chunk_workspace_bytes(requests, tokens, heads, kv_heads, dim, longest)
-    assert need(longest=640) == 0 < need(longest=641)                                       # ten tiles of keys are not cut
+    assert need(longest=768) == 0 < need(longest=769)                                       # twelve tiles of keys are not cut
     assert need(requests=0) == need(tokens=0) == need(heads=30) == need(dim=96) == need(longest=0) == need(longest=1 << 31) == need(tokens=1 << 30) == 0
     # room for the pieces that a call can have, however it grows
     assert need(longest=1 << 20) <= need(tokens=1 << 20, longest=1 << 20) == need(tokens=1 << 22, longest=1 << 22) < 160 << 20
