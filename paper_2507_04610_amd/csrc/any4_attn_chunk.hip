@@ -1259,7 +1259,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
 }
 
 // Joins the pieces of tiles of rows that were cut: a wavefront has 32 rows at a time and four values of each, in the pieces' own order of lanes.
-constexpr int kAtOnce = 16;                                     // pieces whose loads are out at a time
+constexpr int kAtOnce = 8, kFewPieces = 4;                      // pieces whose loads are out at a time
 template <int D, bool F16>
 __global__ __launch_bounds__(256) void attn_chunk_join_kernel(Args a) {
     const int lane = threadIdx.x & 63, n = lane & 31, g = lane >> 5;
@@ -1277,24 +1277,25 @@ __global__ __launch_bounds__(256) void attn_chunk_join_kernel(Args a) {
         const float* sums = first + 4 * ((part * (D / 8) + four) * 64 + lane);
         float top = -__builtin_inff(), sum = 0.0f;
         f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int p0 = 0; p0 < pieces; p0 += kAtOnce) {
-            f32x2 x[kAtOnce];
-            f32x4 y[kAtOnce];
+        auto add = [&](auto at_once, int p0) {
+            constexpr int N = decltype(at_once)::value;
+            f32x2 x[N];
+            f32x4 y[N];
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) {
+            for (int i = 0; i < N; ++i) {
                 const int64_t at = min(p0 + i, pieces - 1) * step;
                 x[i] = *reinterpret_cast<const f32x2*>(ml + at);
                 y[i] = *reinterpret_cast<const f32x4*>(sums + at);
             }
             float higher = top;
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) higher = fmaxf(higher, x[i][0]);
+            for (int i = 0; i < N; ++i) higher = fmaxf(higher, x[i][0]);
             const float use = higher == -__builtin_inff() ? 0.0f : higher, f = exp2_fast(top - use);
             sum *= f;
             v *= f;
             top = higher;
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) {
+            for (int i = 0; i < N; ++i) {
                 const float e = p0 + i < pieces ? exp2_fast(x[i][0] - use) : 0.0f;
                 if (e != 0.0f) {
                     sum = fmaf(e, x[i][1], sum);
@@ -1302,6 +1303,11 @@ __global__ __launch_bounds__(256) void attn_chunk_join_kernel(Args a) {
                     for (int j = 0; j < 4; ++j) v[j] = fmaf(e, y[i][j], v[j]);
                 }
             }
+        };
+        if (pieces <= kFewPieces) {
+            if (pieces > 0) add(std::integral_constant<int, kFewPieces>{}, 0);
+        } else {
+            for (int p0 = 0; p0 < pieces; p0 += kAtOnce) add(std::integral_constant<int, kAtOnce>{}, p0);
         }
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
         if (row < rows) {
