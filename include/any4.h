@@ -380,6 +380,7 @@ int any4_rope(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, 
  * any4_rope_kv_write - any4_rope, with k and v written into their slots of the cache: the same cache and q_out, bit for bit, as any4_rope followed by
  * any4_kv_write of its k (keys are rounded to 16 bits before they become codes), in one pass.
  *   slots       in   as for any4_kv_write; q (and k_out) of a token that is left out are turned all the same
+ *                    (a slot named twice holds values of either token, in codes perhaps some of each: the caller's to avoid)
  *   k_out            NULL: the keys go into the cache alone
  * KV heads, head_dim and type are the cache's.
  */

@@ -19,8 +19,8 @@
 //
 // Who does what.  Lengths are the device's, so each block finds its rows itself, of more than 64 requests in what a first launch of one block writes down
 // (a token each of 2048 requests over 300 tokens in 8 bits: 670 -> 441 us).  Where whole tiles of rows do not fill the chip, their keys are cut
-// into pieces, no more than it takes; pieces leave sums, maximum and sum of weights in the workspace, and a last launch joins them (4 to 8 us, and a
-// launch: short calls are not cut).
+// into pieces, no more than it takes; pieces leave sums, maximum and sum of weights in the workspace, and a last launch joins them (3 to 5 us: short
+// calls are not cut).
 //
 // Rounding: scores, maxima, sums and accumulators are fp32; the weights (times vs_j) are rounded to 16 bits for the matrix cores, once.
 //
@@ -29,7 +29,7 @@
 //                                                                               remains; wavefronts wait 27 % of their time for LDS and each other)
 //     8 bits, 24 requests of 1 .. 511 tokens, fp16                  414 - 440   (0.57 PFLOP/s: vector units busy 47 %, LDS 37 %, matrix cores 24 %; 6.2 of 8
 //                                                                               wavefronts there on average, which wait 31 % of their time)
-//     4 bits, 16 requests, up to 8 drafted tokens                    65 -  70   (2.1 TB/s: vector units 51 %; 8 of it the join; 5.6 of 8 wavefronts)
+//     4 bits, 16 requests, up to 8 drafted tokens                    64 -  67   (2.2 TB/s: vector units 51 %; 5 of it the join; 5.6 of 8 wavefronts)
 //     16 bits, 19 tokens behind 333                                   9.1       (loads that wait for each other: starts, lengths, page, k and v)
 //     packed rows, a prompt of 12011, window 2048                   412         (0.90 PFLOP/s)
 //     packed rows, fp16, 8450 tokens, 16 heads of 64 on 2, window 777  55        (0.49 PFLOP/s: 1060 blocks of 13 tiles of keys, whose beginnings and
