@@ -13,7 +13,7 @@
 // any4_rope and any4_kv_write one after the other would have put there, bit for bit.
 //
 // Measured, 32 query and 8 KV heads of 128 unless said otherwise, us:
-//     16384 tokens with norms into a cache of 8 bits             98   (4.1 TB/s; a copy reaches 4.9; waits for memory 73 % of the time, vector units busy 57 %)
+//     16384 tokens with norms into a cache of 8 bits             82   (4.9 TB/s, as a copy; vector units busy 73 %.  Loads when a head is worked on 98)
 //     5001 tokens, three axes, norms, fp16, q and k alone        20 in the kernel, 25 with the call's gaps (5.1 and 4.0 TB/s)
 //     45 tokens, 16 and 2 heads, no norms; 16 tokens, 16 bits    3 and 4 in the kernel, 5 with the call (loads that wait for each other: position, frequency)
 #include "any4_attn.h"
@@ -51,9 +51,32 @@ template <int BITS, int D, bool F16>
 __global__ __launch_bounds__(kThreads) void rope_kernel(Args a) {
     constexpr int LANES = D / 8, AT_ONCE = kThreads / (kTokens * LANES);
     __shared__ f32x2 table[kTokens][D / 2 + 2];                // cosine and sine
+    __shared__ u32x2 norms[2][D / 4];                          // weights (from memory they would be waited for together with the next head's values)
     const int part = threadIdx.x % LANES, vec = threadIdx.x / LANES, mine = vec / AT_ONCE;
     const int64_t t0 = (int64_t)blockIdx.x * kTokens, t = t0 + mine;
     const int half = a.rotary / 2;
+    // this lane's values of a head of q or k: four from `lo`, four from `hi`
+    const bool turned = part * 8 < a.rotary, split = turned && !a.interleaved;
+    const int lo = split ? 4 * part : 8 * part, hi = split ? half + 4 * part : 8 * part + 4;
+    const int first = blockIdx.y * a.per_block + vec % AT_ONCE, all = a.heads + (BITS != 0 ? 2 : 1) * a.kv_heads;   // heads of this block
+    const int end = min(all, (int)(blockIdx.y + 1) * a.per_block);
+    struct Eight {
+        u32x2 lo, hi;
+    };
+    auto fetch = [&](int h) -> Eight {
+        const int j = h - a.heads;
+        const uint16_t* from = j < 0 ? a.q.p + t * a.q.token + h * a.q.head
+                             : BITS == 0 || j < a.kv_heads ? a.k.p + t * a.k.token + j * a.k.head : a.v.p + t * a.v.token + (j - a.kv_heads) * a.v.head;
+        const bool is_v = BITS != 0 && j >= a.kv_heads;
+        return Eight{load_four(from + (is_v ? 8 * part : lo)), load_four(from + (is_v ? 8 * part + 4 : hi))};
+    };
+    // (a head's values are asked for before those of the head in front of it are worked on, the first before the angles)
+    Eight next{};
+    if (t < a.tokens && first < end) next = fetch(first);
+    if (threadIdx.x < D / 2) {
+        const uint16_t* const from = threadIdx.x < D / 4 ? a.q_norm : a.k_norm;
+        if (from) norms[threadIdx.x / (D / 4)][threadIdx.x % (D / 4)] = load_four(from + 4 * (threadIdx.x % (D / 4)));
+    }
     for (int i = threadIdx.x; i < kTokens * half; i += kThreads) {
         const int tok = i / half, j = i - tok * half;
         if (t0 + tok >= a.tokens) break;
@@ -70,15 +93,12 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Args a) {
     __syncthreads();
     if (t >= a.tokens) return;
 
-    // this lane's values of a head: four from `lo`, four from `hi`
-    const bool turned = part * 8 < a.rotary, split = turned && !a.interleaved;
-    const int lo = split ? 4 * part : 8 * part, hi = split ? half + 4 * part : 8 * part + 4;
     f32x2 cs[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) cs[i] = turned ? table[mine][4 * part + i] : f32x2{1.0f, 0.0f};
 
-    auto turn = [&](const uint16_t* from, const uint16_t* weight, uint32_t (&y)[4]) {
-        const u32x2 p = load_four(from + lo), r = load_four(from + hi);
+    auto turn = [&](const Eight& in, int of_k, uint32_t (&y)[4]) {
+        const u32x2 p = in.lo, r = in.hi;
         float x[8];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -87,13 +107,13 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Args a) {
             x[4 + 2 * j] = h16lo_to_f32<F16>(r[j]);
             x[4 + 2 * j + 1] = h16hi_to_f32<F16>(r[j]);
         }
-        if (weight) {
+        if (of_k ? a.k_norm : a.q_norm) {
             float sum = 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum = fmaf(x[j], x[j], sum);
             sum = lanes_reduce<LANES>(sum, [](float u, float v) { return u + v; });
             const float by = rsqrtf(fmaf(sum, 1.0f / D, a.eps));
-            const u32x2 wp = load_four(weight + lo), wr = load_four(weight + hi);
+            const u32x2 wp = norms[of_k][lo / 4], wr = norms[of_k][hi / 4];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 x[2 * j] *= by * h16lo_to_f32<F16>(wp[j]);
@@ -127,12 +147,12 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Args a) {
     const bool kept = BITS != 0 && slot >= 0 && slot < a.c.slots;
     const int page = kept ? (int)(slot >> a.c.page_shift) : 0, place = (int)(slot & ((1 << a.c.page_shift) - 1));
 
-    const int first = blockIdx.y * a.per_block + vec % AT_ONCE, all = a.heads + (BITS != 0 ? 2 : 1) * a.kv_heads;
-    const int end = min(all, (int)(blockIdx.y + 1) * a.per_block);
     for (int h = first; h < end; h += AT_ONCE) {
+        const Eight in = next;
+        if (h + AT_ONCE < end) next = fetch(h + AT_ONCE);
         if (h < a.heads) {
             uint32_t y[4];
-            turn(a.q.p + t * a.q.token + h * a.q.head, a.q_norm, y);
+            turn(in, 0, y);
             uint16_t* to = a.q_out + t * a.qo_token + h * a.qo_head;
             store_four(to + lo, y[0], y[1]);
             store_four(to + hi, y[2], y[3]);
@@ -145,11 +165,12 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Args a) {
         if (is_v) {
             at_lo = 8 * part;
             at_hi = 8 * part + 4;
-            const u32x4 w = *reinterpret_cast<const u32x4*>(a.v.p + t * a.v.token + j * a.v.head + at_lo);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = w[i];
+            y[0] = in.lo[0];
+            y[1] = in.lo[1];
+            y[2] = in.hi[0];
+            y[3] = in.hi[1];
         } else {
-            turn(a.k.p + t * a.k.token + j * a.k.head, a.k_norm, y);
+            turn(in, 1, y);
             if (a.k_out) {
                 uint16_t* to = a.k_out + t * a.ko_token + j * a.ko_head;
                 store_four(to + lo, y[0], y[1]);
