@@ -25,17 +25,17 @@
 // Rounding: scores, maxima, sums and accumulators are fp32; the weights (times vs_j) are rounded to 16 bits for the matrix cores, once.
 //
 // Measured, 8 KV heads, us (what bounds it):
-//     16 bits, 2048 tokens behind 30720, 32 query heads of 128     1005 - 1040  (1.05 PFLOP/s: matrix cores busy 51 %, vector units 51 %, at the clock that
-//                                                                               remains; wavefronts wait 27 % of their time for LDS and each other)
+//     16 bits, 2048 tokens behind 30 k, 32 query heads of 128      1005 - 1040  (1.05 PFLOP/s: matrix cores busy 51 %, vector units 51 %;
+//                                                                               wavefronts wait 27 % of their time for LDS and each other)
 //     8 bits, 24 requests of 1 .. 511 tokens, fp16                  414 - 440   (0.57 PFLOP/s: vector units busy 47 %, LDS 37 %, matrix cores 24 %; 6.2 of 8
 //                                                                               wavefronts there on average, which wait 31 % of their time)
 //     4 bits, 16 requests, up to 8 drafted tokens                    64 -  67   (2.2 TB/s: vector units 51 %; 5 of it the join; 5.6 of 8 wavefronts)
 //     16 bits, 19 tokens behind 333                                   9.1       (loads that wait for each other: starts, lengths, page, k and v)
 //     packed rows, a prompt of 12011, window 2048                   412         (0.90 PFLOP/s)
-//     packed rows, fp16, 8450 tokens, 16 heads of 64 on 2, window 777  55        (0.49 PFLOP/s: 1060 blocks of 13 tiles of keys, whose beginnings and
+//     packed rows, fp16, 8450 tokens, 16 heads of 64 on 2, window 777  55       (0.49 PFLOP/s: 1060 blocks of 13 tiles of keys, whose beginnings and
 //                                                                               ends and the second round of them cost as much as the tiles)
 // Without gain: longest pieces first, more and smaller pieces than fill the chip, a fixed priority for one of a SIMD's wavefronts, an order of loads and products
-// prescribed to the compiler.
+// prescribed to the compiler, a closer search for the length of pieces.
 #include "any4_attn.h"
 #include "any4_attn_tile.h"
 #include "any4_internal.h"
@@ -709,7 +709,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         // four tokens' of an array of scales: keys 32 u + 8 c + 4 g ..
         auto four_of = [&](int array, int u, int c) -> f32x4 { return *(lds_f4)(scales + (uint32_t)(128 * U * array + 4 * (32 * u + 8 * c)) + 16u * (uint32_t)g); };
         // The two wavefronts of a SIMD take turns at its matrix cores and its vector units: one that turns scores into weights goes first, so that its
-        // products come while the other is at its scores or weights.  (2048 tokens behind 30720 in 16 bits 1063 -> 1004 us, with the priority until behind
+        // products come while the other is at its scores or weights.  (2048 tokens behind 30 k in 16 bits 1063 -> 1004 us, with the priority until behind
         // the product 1030; a mixed batch in 8 bits 451 and 434 the other way round.  Heads of 64 have a third wavefront and lose 4 % by it.)
         constexpr bool kFirst = D == 128;
         f32x16 s[U];
