@@ -1296,8 +1296,10 @@ __global__ __launch_bounds__(256) void attn_chunk_join_kernel(Args a) {
             top = higher;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float e = p0 + i < pieces ? exp2_fast(x[i][0] - use) : 0.0f;
-                if (e != 0.0f) {
+                // (a factor of 0 is no reason to leave a piece out: what is not finite in it has to reach the result, and a row whose scores in a piece are all NaN
+                // has a maximum of -inf there)
+                if (p0 + i < pieces) {
+                    const float e = exp2_fast(x[i][0] - use);
                     sum = fmaf(e, x[i][1], sum);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) v[j] = fmaf(e, y[i][j], v[j]);
