@@ -480,8 +480,8 @@ int any4_attn_prompt_window(const uint16_t* q, int64_t q_token_stride, int64_t q
  *   out         out  16-bit [q_tokens][heads][head_dim], dense; rows that no request has are left as they are
  *   workspace   at least any4_attn_chunk_workspace_bytes() bytes; may be NULL when that is 0.  Contents on entry and on exit mean nothing; it must not
  *               serve two calls that overlap in time
- * q_tokens * (heads / kv_heads) at most 2^31 - 2048, (that / 128 + 2 requests) * kv_heads below 2^31 - 8192, table_width * page_size at most 2^31 - 2048.
- * requests = 0 and q_tokens = 0 do nothing.
+ * requests at most 2^29, q_tokens * (heads / kv_heads) at most 2^31 - 2048, (that / 128 + 2 requests) * kv_heads below 2^31 - 8192, table_width * page_size at most
+ * 2^31 - 2048 (ANY4_ERR_SHAPE).  requests = 0 and q_tokens = 0 do nothing.
  */
 int any4_attn_chunk(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const any4_kv_cache* cache,
                     const int32_t* page_table, int64_t table_stride, int64_t table_width, const int32_t* q_starts, const int32_t* lengths,

@@ -14,6 +14,7 @@ bool scale_ok(float s) { return s > 0.0f && s < __builtin_inff(); }
 constexpr int64_t kMaxStride = (int64_t)1 << 23;             // any4_attn_prompt: 64 rows' offsets in 32 bits
 constexpr int kMaxKvHeads = 4095, kMaxHeads = 65535;
 constexpr int64_t kMaxRequests = 65535, kMaxTokens = 0x7FFFFFFF - 2047;
+constexpr int64_t kMaxChunkRequests = (int64_t)1 << 29;      // any4_attn_chunk: what a first launch finds out, four words a request, has 32-bit places
 
 // the units of work of one request are counted in 32 bits
 bool tokens_ok(int64_t max_tokens, int heads, int kv_heads) {
@@ -207,7 +208,7 @@ int any4_attn_prompt_window(const uint16_t* q, int64_t q_token_stride, int64_t q
 }
 
 size_t any4_attn_chunk_workspace_bytes(int64_t requests, int64_t q_tokens, int heads, int kv_heads, int head_dim, int64_t max_tokens) {
-    if (requests < 1 || requests > kMaxTokens || q_tokens < 1 || q_tokens > kMaxTokens || !heads_ok(heads, kv_heads) || (head_dim != 64 && head_dim != 128) ||
+    if (requests < 1 || requests > kMaxChunkRequests || q_tokens < 1 || q_tokens > kMaxTokens || !heads_ok(heads, kv_heads) || (head_dim != 64 && head_dim != 128) ||
         max_tokens < 1 || max_tokens > kMaxTokens || !rows_ok(q_tokens, heads, kv_heads))
         return 0;
     return plan_attn_chunk(requests, q_tokens, heads, kv_heads, head_dim, max_tokens, true, device_compute_units()).workspace;
@@ -217,7 +218,7 @@ int any4_attn_chunk(const uint16_t* q, int64_t q_token_stride, int64_t q_head_st
                     int64_t table_stride, int64_t table_width, const int32_t* q_starts, const int32_t* lengths, int64_t q_tokens, int64_t requests,
                     int heads, int64_t window, int64_t sinks, float softmax_scale, uint16_t* out, void* workspace, size_t workspace_bytes, void* stream) {
     if (int rc = cache_check(cache)) return rc;
-    if (requests < 0 || requests > kMaxTokens || q_tokens < 0 || q_tokens > kMaxTokens || !heads_ok(heads, cache->kv_heads) || !scale_ok(softmax_scale) ||
+    if (requests < 0 || requests > kMaxChunkRequests || q_tokens < 0 || q_tokens > kMaxTokens || !heads_ok(heads, cache->kv_heads) || !scale_ok(softmax_scale) ||
         !strides_ok(q_token_stride, q_head_stride) || table_width < 1 || table_width > kMaxTokens / cache->page_size || table_stride < 0 || window < 0 ||
         sinks < 0 || !rows_ok(q_tokens, heads, cache->kv_heads))
         return ANY4_ERR_SHAPE;
