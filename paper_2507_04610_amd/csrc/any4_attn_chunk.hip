@@ -15,7 +15,8 @@
 //     q . k_j = ks_j (q . c'_j) + (ko_j - kBias ks_j) sum(q)
 //     o = sum_j (p_j vs_j) (c_j - kCentre) + sum_j p_j (vo_j + kCentre vs_j)
 // bf16 queries become fp16 for that: a row is scaled by a power of two, which is exact down to 2^-31 of its largest value and off by 2^-39 of that
-// below.  The product p_j vs_j is rounded to fp16; the exponent of the largest vs_j that a row has seen is taken off it together with the running maximum.
+// below.  The product p_j vs_j is rounded to fp16; the exponent of the largest product that a row has had is taken off it together with the running maximum (that of the
+// largest vs_j alone would leave nothing of the others beside a large value of no weight).
 //
 // Who does what.  Lengths are the device's, so each block finds its rows itself, of more than 64 requests in what a first launch of one block writes down
 // (a token each of 2048 requests over 300 tokens in 8 bits: 670 -> 441 us).  Where whole tiles of rows do not fill the chip, their keys are cut
@@ -60,9 +61,13 @@ constexpr int kWholeFew = 12, kWhole = 40;
 // beginning 12.9, 18; 4 requests of 100 of 1000 tokens in 8 bits 34, 48; but 512 behind 7488 98, with 65536 117, and 2048 from the beginning 67, 90.
 constexpr int kSmall = 16384;
 constexpr int kNoWindow = 0x7FFFF800;                           // more than any request's tokens
-// The exponent of the largest vs_j goes with the maximum as far as 2^+-kFold: beyond, weights of tokens whose scales differ by 2^126 and more would
-// be lost, to each other and to the sum of weights.  The rest is taken off vs_j itself.
+// Codes: what is taken off the exponents of the products p_j vs_j goes with the maximum as far as 2^+-kFold: beyond, weights of tokens whose scales differ by 2^126 and
+// more would be lost to the sum of weights.  The rest is taken off vs_j itself.
 constexpr int kFold = 40;
+// The largest product stands 2^kUp above 1 (2^kSlack more at most, below 2^15 in all): fp16 has steps of 2^-24 down there, and tokens of small weight are many.
+constexpr int kUp = 6;
+// Scales of a tile that lie within 2^kSpread are taken as the largest of them (the largest product then lies as much lower at most), others with their scores.
+constexpr int kSpread = 8;
 typedef __attribute__((address_space(3))) float* lds_f;
 typedef __attribute__((address_space(3))) f32x4* lds_f4;
 typedef __attribute__((address_space(3))) uint32_t* lds_u1;
@@ -364,15 +369,28 @@ template <int SOURCE> __device__ __forceinline__ Work work_of(const Args& a, uns
 // different ones for the writes of widened codes, whose lanes have pieces four (two) apart.
 template <int D> __device__ __forceinline__ constexpr int swizzle_v(int row) { return D == 128 ? 5 * (row & 3) : ((row >> 1) & 1) << 2 | ((row >> 1) & 3); }
 
-// LDS aside from the tiles.  Scales of TOKENS tokens: k's scale and offset, v's likewise, the largest of the third, whose v's are not finite.
-template <int TOKENS> constexpr int kScaleBytes = 16 * TOKENS + 16;
+// LDS aside from the tiles.  Scales of TOKENS tokens: k's scale and offset, v's likewise, the exponent of v's; then the largest of those, whether they lie
+// far apart, whose v's are not finite.
+template <int TOKENS> constexpr int kScaleBytes = 20 * TOKENS + 16;
 template <bool CODES> constexpr int kAsideAll = CODES ? kWaves * kScaleBytes<32> : kWaves * 32 * 8;
 
 // floats of a piece: sums [wavefront][4 values of a row][lane][4], then [row] maximum and sum of weights
 template <int D> constexpr int kPieceFloats = kRowTile * (D + 2);
 
-__device__ __forceinline__ int with_maximum(int e) { return min(max(e, -kFold), kFold); }
-__device__ __forceinline__ int folded(int e) { return e - with_maximum(e); }
+// a - b where a may come out of a product: that is rounded first (from 2^31 on its rounding alone would be hundreds)
+__device__ __forceinline__ float difference(float a, float b) {
+#pragma clang fp contract(off)
+    return a - b;
+}
+// Of the exponent taken off products: with the maximum m, and off vs_j.  (All of it there where m is far, or without a score yet -inf: a sum with m would round it away.)
+__device__ __forceinline__ float with_maximum(float m, float e) { return fabsf(m) > kFar ? 0.0f : fminf(fmaxf(e, (float)-kFold), (float)kFold); }
+__device__ __forceinline__ int folded(float m, float e) { return (int)(e - with_maximum(m, e)); }
+
+// What is kept of a token's v for that: the exponent of its scale (of its middle times 2^-64 if that is more: a constant vector has scale 1 however large it is,
+// and its product with the weight is to stay in fp32's range), 2^kUp lower.
+__device__ __forceinline__ float exponent_of(float vs, float mid) {
+    return fmaxf(ceilf(__builtin_amdgcn_logf(fmaxf(fabsf(vs), fabsf(mid) * 0x1p-64f))), -126.0f) - (float)kUp;
+}
 
 template <int BITS> struct Codes {
     static constexpr float kBias = BITS == 8 ? 1024.0f : 64.0f, kCentre = (float)(1 << (BITS - 1));
@@ -595,7 +613,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     auto bad_of_tile = [&](uint32_t parity) -> unsigned long long {
         unsigned long long bad = 0ull;
         if constexpr (CODES) {
-            const u32x2 two = *(lds_u2)(kAside + parity * kAsideBytes + 16 * kKeys + 8);
+            const u32x2 two = *(lds_u2)(kAside + parity * kAsideBytes + 20 * kKeys + 8);
             bad = (unsigned long long)two[1] << 32 | two[0];
         } else {
 #pragma unroll
@@ -660,15 +678,18 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 const uint32_t aside = kAside + parity * kAsideBytes, to = aside + 4u * (uint32_t)lane;
                 *(lds_f)(to) = ks;
                 *(lds_f)(to + 256) = fmaf(-C::kBias, ks, ko);
-                *(lds_f)(to + 512) = fine ? vs : 0.0f;
-                *(lds_f)(to + 768) = fine ? mid : 0.0f;
-                float big = lanes_reduce<16>(fine ? fabsf(vs) : 0.0f, [](float u, float v) { return fmaxf(u, v); });
+                const float vs_used = fine ? vs : 0.0f, mid_used = fine ? mid : 0.0f, high = exponent_of(vs_used, mid_used);
+                *(lds_f)(to + 512) = vs_used;
+                *(lds_f)(to + 768) = mid_used;
+                *(lds_f)(to + 1024) = high;
+                float big = lanes_reduce<16>(high, [](float u, float v) { return fmaxf(u, v); });
                 big = fmaxf(big, __shfl_xor(big, 16));
                 big = fmaxf(big, __shfl_xor(big, 32));
+                const bool apart = __builtin_amdgcn_ballot_w64(vs_used != 0.0f && big - high > (float)kSpread) != 0ull;
                 const unsigned long long bad = __builtin_amdgcn_ballot_w64(!fine);
                 if (lane == 0) {
-                    *(lds_f)(aside + 16 * kKeys) = big;
-                    *(lds_u2)(aside + 16 * kKeys + 8) = u32x2{(uint32_t)bad, (uint32_t)(bad >> 32)};
+                    *(lds_u2)(aside + 20 * kKeys) = u32x2{__float_as_uint(big), apart ? 1u : 0u};
+                    *(lds_u2)(aside + 20 * kKeys + 8) = u32x2{(uint32_t)bad, (uint32_t)(bad >> 32)};
                 }
             }
         }
@@ -686,9 +707,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     };
 
     float m_ref = -__builtin_inff(), l = 0.0f, v_sum = 0.0f;
-    int exponent = -126;                                        // of the largest vs seen
-    float m_used = CODES ? (float)with_maximum(-126) : 0.0f;    // what is taken off the scores: maximum and exponent
-    int far = 0, folds = CODES ? 1 : 0;                         // whether that is so for some row
+    float exponent = 0.0f;                                      // codes: of the largest product of a weight exp2(s - m_ref) and vs, a whole number
+    float m_used = 0.0f;                                        // what is taken off the scores: maximum and exponent
+    int far = 0, folds = 0;                                     // whether that is so for some row
     f32x16 o[OM];
 #pragma unroll
     for (int m = 0; m < OM; ++m)
@@ -736,12 +757,13 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 }
         }
         after_scores();
+        u32x2 of_all = {0u, 0u};                                 // codes: the largest exponent of the scales, whether they lie far apart
+        if constexpr (CODES) of_all = *(lds_u2)(scales + 640 * U);
         // (places relative to the tile's first key of this half, which may be those of no page)
         const int base = k0 + 4 * g, lim_at = lim - base, lo_at = (max(lim, 0) + 1 - base) - a.window, sinks_at = a.sinks - base;
         auto key_of = [](int u, int r) -> int { return 32 * u + 8 * (r >> 2) + (r & 3); };
         auto last_of = [&](int u, int r) -> int { return !PAGED || ((valid >> (2 * u + (r >> 3))) & 1u) ? lim_at : -0x7FFFFFFF; };
         auto in_part = [&](int u, int r) -> bool { return (bool)((int)(key_of(u, r) >= lo_at) | (int)(key_of(u, r) < sinks_at)); };
-        auto sees = [&](int u, int r) -> bool { return (bool)((int)(key_of(u, r) <= last_of(u, r)) & (int)in_part(u, r)); };
         if (seldom(!whole)) {
             // (behind the last one or on a page that does not exist; in front of the window)
             if (k0 + 32 * U - 1 > all_lim || valid != (1u << 2 * U) - 1u) {
@@ -766,42 +788,55 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
             for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
         top = fmaxf(top, other_half(top)) * scale;
         bool moved = top > m_ref + kSlack;
-        int higher = exponent;
+        const float higher = fmaxf(m_ref, top);
+        float product = 0.0f;                                    // codes: exponent of the largest product of this step, less `higher`
         if constexpr (CODES) {
-            float big = *(lds_f)(scales + 512 * U);
-            if (seldom(!whole)) {
-                big = 0.0f;
+            // (a large scale alone is none: its token may have a weight of nothing, and the others' products are not to vanish beside a product that is none)
+            product = difference(top, higher) + __uint_as_float(of_all[0]);
+            if (seldom((int)!whole | __builtin_amdgcn_readfirstlane((int)of_all[1]))) {
+                product = -__builtin_inff();
+                float by = scale;
+                asm volatile("" : "+v"(by));                     // (or these products and those of far scores are made in front of both branches)
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const f32x4 vs = four_of(2, u, c);
+                        const f32x4 high = four_of(4, u, c);
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) big = sees(u, 4 * c + r) ? fmaxf(big, fabsf(vs[r])) : big;
+                        for (int r = 0; r < 4; ++r) product = fmaxf(product, difference(s[u][4 * c + r] * by, higher) + high[r]);
                     }
-                big = fmaxf(big, other_half(big));
+                product = fmaxf(product, other_half(product));
             }
-            higher = max(exponent, min((int)(__float_as_uint(big) >> 23) - 127, 127));
-            moved |= higher > exponent;
+            moved |= product + (higher - m_ref) > exponent + kSlack;
         }
         // A weight's exponent is scale s - m_sub: a product that is not rounded, less a maximum that is.  Beyond 2^31 that rounding alone would leave
         // the exponents' range: where some row's maximum lies beyond kFar, the scores are replaced by their distance from it, both rounded alike.
         // (All that follows from the maximum and the exponent is set here: set after the branch, the compiler has the sums copied around it.)
         if (seldom(__builtin_amdgcn_ballot_w64(moved) != 0ull)) {
-            const float m_new = moved ? fmaxf(m_ref, top) : m_ref;
-            const float alpha = exp2_fast(m_new > m_ref ? m_ref - m_new : 0.0f);
-            const float less = CODES ? __builtin_ldexpf(1.0f, with_maximum(exponent) - with_maximum(higher)) : 1.0f;
-            const float fold = CODES ? __builtin_ldexpf(1.0f, max(folded(exponent) - folded(higher), -140)) : 1.0f;
-            m_ref = m_new;
-            exponent = higher;
-            l *= alpha * less;
-            v_sum *= alpha * less;
-            const float f = alpha * less * fold;
+            const float m_new = moved ? higher : m_ref;
+            if constexpr (CODES) {
+                // (sums are relative to m_used, o to that and what is taken off vs; without a score yet they are zeros)
+                const float before = m_ref == -__builtin_inff() ? m_ref : m_used;
+                const int was = folded(m_ref, exponent);
+                exponent = moved ? ceilf(fmaxf(fmaxf(exponent + (m_ref - m_new), product), -300.0f)) : exponent;
+                m_used = (m_new == -__builtin_inff() ? 0.0f : m_new) + with_maximum(m_new, exponent);
+                const float less = before - m_used, alpha = exp2_fast(less);
+                l *= alpha;
+                v_sum *= alpha;
+                const int is = folded(m_new, exponent);
+                const float f = exp2_fast(less + (float)(was - is));
 #pragma unroll
-            for (int m = 0; m < OM; ++m) o[m] *= f;
-            m_used = (m_new == -__builtin_inff() ? 0.0f : m_new) + (CODES ? (float)with_maximum(higher) : 0.0f);
+                for (int m = 0; m < OM; ++m) o[m] *= f;
+                folds = __builtin_amdgcn_ballot_w64(is != 0) != 0ull ? 1 : 0;
+            } else {
+                const float alpha = exp2_fast(m_new > m_ref ? m_ref - m_new : 0.0f);
+                l *= alpha;
+#pragma unroll
+                for (int m = 0; m < OM; ++m) o[m] *= alpha;
+                m_used = m_new == -__builtin_inff() ? 0.0f : m_new;
+            }
+            m_ref = m_new;
             far = __builtin_amdgcn_ballot_w64(fabsf(m_used) > kFar) != 0ull ? 1 : 0;
-            if constexpr (CODES) folds = __builtin_amdgcn_ballot_w64(folded(higher) != 0) != 0ull ? 1 : 0;
         }
         float m_sub = m_used;
         if (seldom(far != 0)) {
@@ -830,7 +865,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 }
                 if constexpr (CODES) {
                     f32x4 vs = four_of(2, u, c), vo = four_of(3, u, c);
-                    if (seldom(folds != 0)) vs *= __builtin_ldexpf(1.0f, -folded(exponent));
+                    if (seldom(folds != 0)) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) vs[r] = __builtin_ldexpf(vs[r], -folded(m_ref, exponent));
+                    }
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         v_sum = fmaf(e[r], vo[r], v_sum);
@@ -1083,19 +1121,23 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
             const float ks = bf16lo_to_f32(raw_scales[0]), ko = bf16hi_to_f32(raw_scales[0]), vs = bf16lo_to_f32(raw_scales[1]), vo = bf16hi_to_f32(raw_scales[1]);
             const float mid = fmaf(C::kCentre, vs, vo);
             const bool fine = fabsf(mid) < __builtin_inff();
+            const float vs_used = fine ? vs : 0.0f, mid_used = fine ? mid : 0.0f, high = exponent_of(vs_used, mid_used);
             if (lane < 32) {
                 const uint32_t at = scales + 4u * (uint32_t)lane;
                 *(lds_f)(at) = ks;
                 *(lds_f)(at + 128) = fmaf(-C::kBias, ks, ko);
-                *(lds_f)(at + 256) = fine ? vs : 0.0f;
-                *(lds_f)(at + 384) = fine ? mid : 0.0f;
+                *(lds_f)(at + 256) = vs_used;
+                *(lds_f)(at + 384) = mid_used;
+                *(lds_f)(at + 512) = high;
             }
-            float big = lanes_reduce<16>(fine && lane < 32 ? fabsf(vs) : 0.0f, [](float u, float v) { return fmaxf(u, v); });
+            // (lanes from 32 on have no tokens: scales of 0)
+            float big = lanes_reduce<16>(high, [](float u, float v) { return fmaxf(u, v); });
             big = fmaxf(big, __shfl_xor(big, 16));
+            const bool apart = __builtin_amdgcn_ballot_w64(vs_used != 0.0f && big - high > (float)kSpread) != 0ull;
             const unsigned long long bad = __builtin_amdgcn_ballot_w64(!fine && lane < 32);
             if (lane == 0) {
-                *(lds_f)(scales + 512) = big;
-                *(lds_u2)(scales + 520) = u32x2{(uint32_t)bad, 0u};
+                *(lds_u2)(scales + 640) = u32x2{__float_as_uint(big), apart ? 1u : 0u};
+                *(lds_u2)(scales + 648) = u32x2{(uint32_t)bad, 0u};
             }
         };
 
@@ -1134,7 +1176,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                            if (next < h_end) load_k(next, two);
                        },
                        [] {},
-                       [&]() -> unsigned long long { return (unsigned)__builtin_amdgcn_readfirstlane((int)*(lds_u1)(scales + 520)); }, [](unsigned long long) {});
+                       [&]() -> unsigned long long { return (unsigned)__builtin_amdgcn_readfirstlane((int)*(lds_u1)(scales + 648)); }, [](unsigned long long) {});
                 if (next < h_end) stage_v();
                 if (after < h_end) {
                     valid_after = valid_of_half(two_next);
@@ -1175,11 +1217,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     l += other_half(l);
     if constexpr (CODES) {
         v_sum += other_half(v_sum);
-        const float unfold = __builtin_ldexpf(1.0f, folded(exponent));
+        if (seldom(folds != 0)) {
+            const int unfold = folded(m_ref, exponent);
 #pragma unroll
-        for (int m = 0; m < OM; ++m)
+            for (int m = 0; m < OM; ++m)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) o[m][r] = fmaf(o[m][r], unfold, v_sum);
+                for (int r = 0; r < 16; ++r) o[m][r] = __builtin_ldexpf(o[m][r], unfold);
+        }
+#pragma unroll
+        for (int m = 0; m < OM; ++m) o[m] += v_sum;
         if constexpr (SOURCE == 4) {
 #pragma unroll
             for (int m = 0; m < OM; ++m)
@@ -1196,7 +1242,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         uint16_t* out = a.out + ((int64_t)(w.r.q_at + query_e) * a.heads + head) * D + 4 * g_e + 8 * four;
         *reinterpret_cast<u32x2*>(out) = u32x2{pack<F16>(v[0], v[1]), pack<F16>(v[2], v[3])};
     };
-    const float m_own = m_ref == -__builtin_inff() ? m_ref : m_ref + (CODES ? (float)with_maximum(exponent) : 0.0f);
+    const float m_own = m_ref == -__builtin_inff() ? m_ref : m_used;
     if (narrow) {
         // the wavefronts' sums meet in LDS, [wavefront][4 OM][lane], and each adds up a quarter of the places
         lds_barrier();
