@@ -470,8 +470,8 @@ int any4_attn_prompt_window(const uint16_t* q, int64_t q_token_stride, int64_t q
  * q_starts[r] .. q_starts[r + 1] - 1 of q, nq of them, and its query i sees tokens 0 .. i + lengths[r] - nq, with a window the last `window` of those and
  * the first `sinks` tokens.  A query that sees no token (nq > lengths[r]) gets zeros.  A token that a query does not see has no influence on it,
  * whatever the cache holds there, and entries of the page table all of whose tokens no query sees may be anything.
- * Arithmetic as in any4_attn_decode; with codes p_j times v's scale is what is rounded to 16 bits, as fp16 next to the row's largest such product (one below 2^-23 of that
- * is rounded as if it were so large).  The result is reproducible run to run; its last bits may
+ * Arithmetic as in any4_attn_decode; with codes p_j times v's scale is what is rounded to 16 bits, as fp16 next to the row's largest such product (one below 2^-10
+ * of that may be rounded to a multiple of 2^-20 of it).  The result is reproducible run to run; its last bits may
  * depend on the call's other requests and on the page table's width, which say where long sums are cut.
  *   q           in   16-bit [q_tokens][heads][head_dim], strided rows
  *   q_starts    in   int32 [requests + 1], ascending; values are taken as at least 0 and at most q_tokens

@@ -395,6 +395,11 @@ __device__ __forceinline__ float exponent_of(float vs, float mid) {
 template <int BITS> struct Codes {
     static constexpr float kBias = BITS == 8 ? 1024.0f : 64.0f, kCentre = (float)(1 << (BITS - 1));
 };
+// k's scales and offsets in LDS are 2^-kDown of what they are where they come near fp32's end, kBias times as large (bf16), and q's scale 2^kDown times as large
+template <bool F16> constexpr float kDown = F16 ? 1.0f : 0x1p-4f;
+// Queries whose largest value lies below 2^kSmallQuery: their products with codes are brought back to their own size before they meet k's scale, as far as 2^120
+// (otherwise with the softmax scale, behind it)
+constexpr int kSmallQuery = -8;
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t add_f16(uint32_t x, float y) {
     return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, x) + f16x2{(_Float16)y, (_Float16)y});
@@ -497,6 +502,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     // Q^T, fp16 for codes: a row of bf16 is scaled by a power of two into the upper part of fp16's range
     u32x4 q[QM];
     float scale = a.scale_log2, sum_q = 0.0f;
+    int back = 0, small = 0;                                    // of a small query; whether some row's is
     {
         const int head = (int)kv_head * a.shared + (row - query * a.shared);
         const uint16_t* qp = a.q.p + (int64_t)(w.r.q_at + query) * a.q.token + (int64_t)head * a.q.head;
@@ -515,9 +521,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(bf16lo_to_f32(q[i][j])), fabsf(bf16hi_to_f32(q[i][j]))));
                 top = fmaxf(top, other_half(top));
-                const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 127);
+                const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -113), 127);
                 const float by = __builtin_ldexpf(1.0f, 14 - e);
-                scale *= __builtin_ldexpf(1.0f, e - 14);
+                back = e < kSmallQuery ? e - 14 : 0;
+                small = __builtin_amdgcn_ballot_w64(back != 0) != 0ull ? 1 : 0;
+                scale *= (back != 0 ? 1.0f : __builtin_ldexpf(1.0f, e - 14)) / kDown<F16>;
 #pragma unroll
                 for (int i = 0; i < QM; ++i)
 #pragma unroll
@@ -528,6 +536,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) sum_q += h16lo_to_f32<true>(q[i][j]) + h16hi_to_f32<true>(q[i][j]);
             sum_q += other_half(sum_q);
+            if constexpr (!F16) sum_q = __builtin_ldexpf(sum_q, back);
             if constexpr (SOURCE == 4) {
 #pragma unroll
                 for (int i = 0; i < QM; ++i) {
@@ -672,7 +681,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
             }
             if (wave == (t & (kWaves - 1))) {
                 using C = Codes<CODES ? SOURCE : 8>;
-                const float ks = bf16lo_to_f32(raw.scales[0]), ko = bf16hi_to_f32(raw.scales[0]), vs = bf16lo_to_f32(raw.scales[1]), vo = bf16hi_to_f32(raw.scales[1]);
+                const float ks = kDown<F16> * bf16lo_to_f32(raw.scales[0]), ko = kDown<F16> * bf16hi_to_f32(raw.scales[0]), vs = bf16lo_to_f32(raw.scales[1]), vo = bf16hi_to_f32(raw.scales[1]);
                 const float mid = fmaf(C::kCentre, vs, vo);
                 const bool fine = fabsf(mid) < __builtin_inff();   // (a v without numbers counts for nothing here; see below)
                 const uint32_t aside = kAside + parity * kAsideBytes, to = aside + 4u * (uint32_t)lane;
@@ -747,6 +756,12 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         }
         if constexpr (kFirst) __builtin_amdgcn_s_setprio(1);
         if constexpr (CODES) {
+            if (!F16 && seldom(small != 0)) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[u][r] = __builtin_ldexpf(s[u][r], back);
+            }
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -1118,7 +1133,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 }
             }
             using C = Codes<BITS>;
-            const float ks = bf16lo_to_f32(raw_scales[0]), ko = bf16hi_to_f32(raw_scales[0]), vs = bf16lo_to_f32(raw_scales[1]), vo = bf16hi_to_f32(raw_scales[1]);
+            const float ks = kDown<F16> * bf16lo_to_f32(raw_scales[0]), ko = kDown<F16> * bf16hi_to_f32(raw_scales[0]), vs = bf16lo_to_f32(raw_scales[1]), vo = bf16hi_to_f32(raw_scales[1]);
             const float mid = fmaf(C::kCentre, vs, vo);
             const bool fine = fabsf(mid) < __builtin_inff();
             const float vs_used = fine ? vs : 0.0f, mid_used = fine ? mid : 0.0f, high = exponent_of(vs_used, mid_used);

@@ -3,8 +3,8 @@
 The bound has every token with the weight that it has (p_j, adding to 1; v'_j = scale (code - centre), what the rounded weights multiply):
   rounding of the result      u |o|, fp16 below its normal range half of 2^-24
   rounding of the weights     2^-11 sum_j p_j |v'_j|: p_j times the scale in fp16, whatever the cache's type; below fp16's normal range by half of 2^-24 where the largest
-                              p_j scale_j is 2^-2 at least (2^6 up, 2^8 down for a tile's scales that are taken as one), times codes up to the centre:
-                              2^-23 centre n max_j p_j scale_j
+                              p_j scale_j is 2^-2 at least (2^6 up, and down by exponents rounded up twice and by a tile's scales that are taken as one, which lie within
+                              2^3 here or are looked at one by one), times codes up to the centre: 2^-23 centre n max_j p_j scale_j
   scores                      products of D terms in fp32, eight deviations: e = 8 sqrt(D) 2^-24 scale sum |q| |k'|, k' with the codes' bias of up to 1024; exp2 and its
                               argument 2^-19 (1 + |s| / 16): 2 e sum_j p_j |v_j|
   sums                        8 sqrt(n) 2^-24 sum_j p_j (|v_j| + 2 centre scale_j)"""
@@ -108,6 +108,16 @@ def test_vectors_of_one_value(bits, parts):
         v[alike] = torch.tensor([0.0, 3.0, -1e5, 1e34])[torch.arange(int(alike.sum())) % 4][:, None, None]
         v[alike] *= (torch.arange(int(alike.sum())) % 4 < 3)[:, None, None] if i == 0 else 1
         p.write(i, k, v)
+    out = p.run()
+    assert out.isfinite().all()
+    check(p, out)
+
+
+@pytest.mark.parametrize("bits", (8, 4))
+@pytest.mark.parametrize("parts", PARTS)
+@pytest.mark.parametrize("q_by,k_by", [(1e-33, 1e33), (1e-35, 1e35), (1e-37, 2e37), (1e33, 1e-33), (1e37, 1e-37)])
+def test_small_queries_of_large_keys(bits, parts, q_by, k_by):
+    p = Chunks(PARTS[parts], bits, BF16, 128, 8, 2, 64, seed=34, q_by=q_by, k_by=k_by)
     out = p.run()
     assert out.isfinite().all()
     check(p, out)
