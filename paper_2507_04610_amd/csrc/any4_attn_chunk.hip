@@ -71,7 +71,7 @@ constexpr int kSpread = 8;
 typedef __attribute__((address_space(3))) float* lds_f;
 typedef __attribute__((address_space(3))) f32x4* lds_f4;
 typedef __attribute__((address_space(3))) uint32_t* lds_u1;
-constexpr int kRows = 0;                                        // SOURCE: packed rows; otherwise the cache's bits
+constexpr int kRows = 0;                                        // SOURCE: packed rows (whose keys are never cut); otherwise the cache's bits
 
 struct Args {
     Rows q, k, v;                      // k, v: packed keys
@@ -315,25 +315,29 @@ template <int SOURCE> __device__ __forceinline__ Work planned(const Args& a, uns
 
 // place: of the block, without KV heads
 template <int SOURCE> __device__ __forceinline__ Work work_of(const Args& a, unsigned place, unsigned kv_head, int lane) {
-    if (a.plan) return planned<SOURCE>(a, place, kv_head, lane);
+    constexpr bool CUTS = SOURCE != kRows;
+    if constexpr (CUTS) {
+        if (a.plan) return planned<SOURCE>(a, place, kv_head, lane);
+    }
     // (where something is cut there are no more than 64 requests)
     const Request first = lane < a.requests ? request_of<SOURCE>(a, lane) : Request{};
-    const Cut how = cut_of(a, [&](auto f) { return lanes_total(f(first)); });
+    Cut how{a.small ? 32 : kRowTile, 0};
+    if constexpr (CUTS) how = cut_of(a, [&](auto f) { return lanes_total(f(first)); });
     Work w{-1, 0, 0, 1, 0, how.height, 0, {}};
     for (int r0 = 0, before = 0, cut_before = 0; r0 < a.requests && w.request < 0; r0 += 64) {
         Request r = first;
         if (r0 > 0) r = r0 + lane < a.requests ? request_of<SOURCE>(a, r0 + lane) : Request{};
         Shares s = shares_of(a, r, how);
-        int cut = s.pieces > 1 ? s.tiles * s.pieces : 0;
-        const int cut_sum = lanes_scan(cut);
-        // (as many as were planned for; were there more, they would be left whole)
-        if (cut > 0 && (int64_t)(cut_before + cut_sum) * a.kv_heads > a.slots) {
-            s.pieces = 1;
-            cut = 0;
+        int cut_sum = 0;
+        if constexpr (CUTS) {
+            const int cut = s.pieces > 1 ? s.tiles * s.pieces : 0;
+            cut_sum = lanes_scan(cut);
+            // (as many as were planned for; were there more, they would be left whole)
+            if (cut > 0 && (int64_t)(cut_before + cut_sum) * a.kv_heads > a.slots) s.pieces = 1;
         }
         const int own = s.tiles * s.pieces, sum = lanes_scan(own), joins = s.pieces > 1 ? s.tiles : 0;
         int joins_sum = 0;
-        if (a.joins) {
+        if (CUTS && a.joins) {
             joins_sum = lanes_scan(joins);
             if ((place | kv_head) == 0u && threadIdx.x == 63) a.joins[0] = joins_sum * a.kv_heads;
         }
@@ -467,7 +471,7 @@ __device__ __forceinline__ float other_half(float v) {
 template <int SOURCE, int D, bool F16>
 __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     using T = Tile<D, kWaves>;
-    constexpr bool CODES = SOURCE == 8 || SOURCE == 4, PAGED = SOURCE != kRows, MMA16 = F16 || CODES;
+    constexpr bool CODES = SOURCE == 8 || SOURCE == 4, PAGED = SOURCE != kRows, CUTS = PAGED, MMA16 = F16 || CODES;
     constexpr int QM = D / 16, OM = D / 32;
     // LDS: two tiles of k, two of v; per tile either rows of v that are not finite (16 bits a wavefront), or the tokens' scales, the largest, and whose are not finite
     constexpr uint32_t kAside = 4 * T::kBytes, kAsideBytes = CODES ? kScaleBytes<kKeys> : 16;
@@ -480,9 +484,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     if (w.request < 0) return;
     const int lq = w.r.lq, lk = w.r.lk, rows = lq * a.shared, ahead = lk - lq;
     const Span span = span_of(a, w.r, w.tile, w.height);
-    const int each = (span.tiles + w.pieces - 1) / w.pieces;
-    const int t_first = w.piece * each, t_end = min(span.tiles, t_first + each);
-    if (w.pieces > 1) {
+    const int each = CUTS ? (span.tiles + w.pieces - 1) / w.pieces : span.tiles;
+    const int t_first = CUTS ? w.piece * each : 0, t_end = min(span.tiles, t_first + each);
+    const bool in_pieces = CUTS && w.pieces > 1;
+    if (in_pieces) {
         const int at = w.join * a.kv_heads + (int)kv_head;
         if (w.piece == 0 && threadIdx.x == 0 && at < a.cut_tiles)
             reinterpret_cast<Join*>(a.joins)[1 + at] = Join{w.r.q_at, rows, w.tile * w.height, w.height, each > 0 ? (span.tiles + each - 1) / each : 0, w.slot, {0, 0}};
@@ -1282,7 +1287,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
             m[i] = exp2_fast(__uint_as_float(ml[i][0]) - use);
             sum = fmaf(m[i], __uint_as_float(ml[i][1]), sum);
         }
-        const float inv = w.pieces > 1 ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum;
+        const float inv = in_pieces ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum;
         float* to = a.partial + (int64_t)w.slot * kPieceFloats<D>;
 #pragma unroll
         for (int x = 0; x < OM; ++x) {
@@ -1294,13 +1299,13 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = fmaf(m[i], y[e], v[e]);
             }
-            if (w.pieces > 1) reinterpret_cast<f32x4*>(to)[four * 64 + (thread & 63)] = v;
+            if (in_pieces) reinterpret_cast<f32x4*>(to)[four * 64 + (thread & 63)] = v;
             else if (row0 + n_e < rows) store_row(row0 + n_e, four, f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv});
         }
-        if (w.pieces > 1 && wave == 0 && g_e == 0) reinterpret_cast<f32x2*>(to + kRowTile * D)[n_e] = f32x2{top, sum};
+        if (in_pieces && wave == 0 && g_e == 0) reinterpret_cast<f32x2*>(to + kRowTile * D)[n_e] = f32x2{top, sum};
         return;
     }
-    if (w.pieces > 1) {
+    if (in_pieces) {
         float* to = a.partial + (int64_t)w.slot * kPieceFloats<D>;
         f32x4* sums = reinterpret_cast<f32x4*>(to) + wave * (4 * OM) * 64 + (thread & 63);
 #pragma unroll
@@ -1389,24 +1394,26 @@ template <int SOURCE, int D, bool F16> hipError_t launch(Args a, const ChunkPlan
     a.target = pl.target;
     a.slots = pl.slots;
     a.small = pl.small;
-    int* const plan = reinterpret_cast<int*>(a.partial);
-    a.partial += pl.plan_bytes / sizeof(float);
-    if (pl.target > 0) {
-        a.joins = reinterpret_cast<int*>(a.partial);
-        a.cut_tiles = pl.cut_tiles;
-        a.partial += Join::bytes(pl.cut_tiles) / sizeof(float);
-    }
-    if (pl.plan_bytes > 0) {
-        hipLaunchKernelGGL((attn_chunk_plan_kernel<SOURCE>), dim3(1), dim3(kPlanThreads), 0, stream, a, plan);
-        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        a.plan = plan;
+    if constexpr (SOURCE != kRows) {
+        int* const plan = reinterpret_cast<int*>(a.partial);
+        a.partial += pl.plan_bytes / sizeof(float);
+        if (pl.target > 0) {
+            a.joins = reinterpret_cast<int*>(a.partial);
+            a.cut_tiles = pl.cut_tiles;
+            a.partial += Join::bytes(pl.cut_tiles) / sizeof(float);
+        }
+        if (pl.plan_bytes > 0) {
+            hipLaunchKernelGGL((attn_chunk_plan_kernel<SOURCE>), dim3(1), dim3(kPlanThreads), 0, stream, a, plan);
+            if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+            a.plan = plan;
+        }
     }
     const hipError_t e = launch_blocks(pl.blocks, kThreads, hipSuccess, [&](int64_t first, int64_t count) {
         a.first_block = (unsigned)first;
         hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(kThreads), bytes, stream, a);
         return hipGetLastError();
     });
-    if (e != hipSuccess || pl.target == 0) return e;
+    if (SOURCE == kRows || e != hipSuccess || pl.target == 0) return e;
     hipLaunchKernelGGL((attn_chunk_join_kernel<D, F16>), dim3((unsigned)pl.cut_tiles, D / 32), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
