@@ -838,7 +838,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 // (sums are relative to m_used, o to that and what is taken off vs; without a score yet they are zeros)
                 const float before = m_ref == -__builtin_inff() ? m_ref : m_used;
                 const int was = folded(m_ref, exponent);
-                exponent = moved ? ceilf(fmaxf(fmaxf(exponent + (m_ref - m_new), product), -300.0f)) : exponent;
+                exponent = moved ? fmaxf(fmaxf(floorf(exponent + (m_ref - m_new)), ceilf(product)), -300.0f) : exponent;   // (down, or it would rise with every move)
                 m_used = (m_new == -__builtin_inff() ? 0.0f : m_new) + with_maximum(m_new, exponent);
                 const float less = before - m_used, alpha = exp2_fast(less);
                 l *= alpha;
@@ -884,15 +884,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                     l += e[r];
                 }
                 if constexpr (CODES) {
-                    f32x4 vs = four_of(2, u, c), vo = four_of(3, u, c);
-                    if (seldom(folds != 0)) {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) vs[r] = __builtin_ldexpf(vs[r], -folded(m_ref, exponent));
-                    }
+                    const f32x4 vs = four_of(2, u, c), vo = four_of(3, u, c);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         v_sum = fmaf(e[r], vo[r], v_sum);
                         e[r] *= vs[r];
+                    }
+                    if (seldom(folds != 0)) {                    // (off the product: a scale alone may lie further from the largest product than fp32 reaches)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) e[r] = __builtin_ldexpf(e[r], -folded(m_ref, exponent));
                     }
                 }
                 p[2 * u + (c >> 1)][2 * (c & 1)] = pack<MMA16>(e[0], e[1]);

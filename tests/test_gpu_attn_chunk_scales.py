@@ -82,6 +82,22 @@ def test_large_values_of_no_weight(bits, parts, dtype, ratio, where):
 
 @pytest.mark.parametrize("bits", (8, 4))
 @pytest.mark.parametrize("parts", PARTS)
+@pytest.mark.parametrize("every", (23, 64))
+def test_scales_further_apart_than_fp32_reaches(bits, parts, every):
+    """values of 1e29 with weights of 2^-270 beside such of 1e-29, from the first token on"""
+    p = Chunks(PARTS[parts], bits, BF16, 128, 8, 2, 64, seed=36)
+    p.q.copy_((p.q * 0.2 + 1).to(BF16))
+    for i, n in enumerate(p.lengths):
+        g = torch.Generator().manual_seed(i)
+        large = torch.arange(n) % every == 0
+        k, v = along(n, 2, 128, g), torch.randn(n, 2, 128, generator=g)
+        k[large] *= -16
+        p.write(i, k, v * torch.where(large, 1e29, 1e-29)[:, None, None])
+    check(p, p.run())
+
+
+@pytest.mark.parametrize("bits", (8, 4))
+@pytest.mark.parametrize("parts", PARTS)
 def test_large_values_first_then_the_weight(bits, parts):
     """scores rise from the first key to the last by 60 while values fall by 2^40, and the other way round: the largest product moves by little"""
     for rising in (True, False):
