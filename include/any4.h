@@ -393,7 +393,8 @@ int any4_rope_kv_write(const uint16_t* q, int64_t q_token_stride, int64_t q_head
  * any4_attn_decode - one new token of each request attends to the first lengths[r] tokens of its pages:
  *     s_j = softmax_scale * q . k_j,   out = sum_j softmax(s)_j v_j
  * Query head h reads KV head h / (heads / kv_heads).  A request without a token gets zeros.  Scores, softmax and sums
- * are fp32; the weights are rounded to 16 bits for the matrix cores, the result once to the output's type.  The result is
+ * are fp32; the weights (with codes times v's scale; in fp16 next to the head's largest such product) are rounded to 16 bits for the matrix cores, the result once to
+ * the output's type.  The result is
  * reproducible run to run; its last bits may depend on the page table's width and on the lengths of the call's other
  * requests, which say where a long request's sums are cut.
  *   q           in   16-bit [requests][heads][head_dim], strided rows

@@ -20,7 +20,8 @@
 // front of adding sum(.. c'_j), both on the matrix cores: the rounding of the weights meets values around 0 as it does without codes, and the running sums
 // hold no bias, whose roundings would grow with the tokens (taken off once at the end: 1e-2 of the result at 131072 tokens a block, fp16, 4 bits).
 //
-// Rounding: scores, maxima, sums and accumulators are fp32; p (times vs) is rounded to 16 bits for the matrix cores, once.
+// Rounding: scores, maxima, sums and accumulators are fp32; p (times vs) is rounded to 16 bits for the matrix cores, once; in fp16 with the exponent of a head's largest
+// such product taken off (that of its largest vs alone would leave nothing of the others beside a large value of no weight).
 //
 // Who does what.  Lengths are the device's, so each block finds its share itself: a request has units of 32 tokens a wavefront (128 or
 // 256 tokens a block), all units of all requests and KV heads stand in one line, and the blocks that fit the chip take equal parts
@@ -51,6 +52,9 @@ constexpr int kFewGroups = 64;                                  // below: blocks
 constexpr int kMaxRequests = 2048;                              // of a launch: their units' beginnings lie in LDS
 constexpr int kWholeUnits = 4;                                  // with fewer units a group (on average) no group is cut for the sake of more blocks
 constexpr int kJoin = 16;                                       // pieces whose loads are out at a time
+// fp16 weights p * vs: the largest lies 2^kUp above 1 (fp16 has steps of 2^-24 down there, and tokens of small weight are many).  Scales of a step within 2^kSpread are
+// taken as the largest of them (the largest product then lies as much lower at most), others with their scores.
+constexpr float kUp = 6.0f, kSpread = 256.0f;
 
 // where the join's parts begin in LDS, behind a factor for each head and piece: they are pairs of floats
 __host__ __device__ constexpr int parts_at(int heads, int pieces) { return (heads * pieces + 1) & ~1; }
@@ -308,8 +312,8 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
             f32x4 o[VM];
 #pragma unroll
             for (int m = 0; m < VM; ++m) o[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            // fp16 weights p * vs: held as p * (vs * 2^-exponent), with the largest vs so far between 1 and 2, or small scales would leave fp16's range
-            int exponent = -126;
+            // fp16 weights p * vs: held as p * (vs * 2^-exponent), the exponent being that of the largest so far, less kUp
+            float exponent = 0.0f;
 
             // One step's tokens: which of the two 16s' exist, and what the lanes load of them.
             struct Step {
@@ -443,32 +447,45 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
 
                 float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
                 top = head_reduce(top, [](float u, float v) { return fmaxf(u, v); });
-                float factor = 1.0f;
                 bool moved = top > m_ref;
+                float product = 0.0f;                                   // the exponent of this step's largest product, less the maximum behind it
                 if constexpr (QUANT && F16) {
-                    float big = 0.0f;
+                    const float higher = fmaxf(m_ref, top);
+                    float big = 0.0f, least = __builtin_inff();
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) big = fmaxf(big, fabsf(vs[j]));
-                    big = head_reduce(big, [](float u, float v) { return fmaxf(u, v); });
-                    const int e = min(max((int)(__float_as_uint(big) >> 23) - 127, -126), 126);
-                    if (e > exponent) {
-                        factor = __builtin_ldexpf(1.0f, max(exponent - e, -126));
-                        exponent = e;
-                        moved = true;
+                    for (int j = 0; j < 8; ++j) {
+                        big = fmaxf(big, fabsf(vs[j]));
+                        least = fminf(least, fabsf(vs[j]));
                     }
+                    big = head_reduce(big, [](float u, float v) { return fmaxf(u, v); });
+                    product = (top - higher) + __builtin_amdgcn_logf(big);
+                    if (__builtin_expect(__builtin_amdgcn_ballot_w64(least * kSpread < big) != 0ull, 0)) {
+                        product = -__builtin_inff();
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) product = fmaxf(product, (x[j] - higher) + __builtin_amdgcn_logf(fabsf(vs[j])));
+                        product = head_reduce(product, [](float u, float v) { return fmaxf(u, v); });
+                    }
+                    product = fminf(fmaxf(ceilf(product) - kUp, -126.0f), 126.0f);
+                    moved |= product + (higher - m_ref) > exponent;
                 }
                 if (__builtin_amdgcn_ballot_w64(moved)) {
-                    const float m_new = fmaxf(m_ref, top);
-                    const float alpha = m_new > m_ref ? exp2_fast(m_ref - m_new) : 1.0f;
+                    const float m_new = fmaxf(m_ref, top), less = m_new > m_ref ? m_ref - m_new : 0.0f;
+                    const float alpha = exp2_fast(less);
                     m_ref = m_new;
                     l *= alpha;
                     vo_sum *= alpha;
-                    const float f = alpha * factor;
+                    float f = alpha;
+                    if constexpr (QUANT && F16) {
+                        const float before = exponent;
+                        // (a whole number, so that a weight of 1 costs vs nothing; down, or it would rise with every move)
+                        exponent = fmaxf(floorf(exponent + less), product);
+                        f = exp2_fast(less + (before - exponent));
+                    }
 #pragma unroll
                     for (int m = 0; m < VM; ++m) o[m] *= f;
                 }
                 const float m_use = m_ref == -__builtin_inff() ? 0.0f : m_ref;
-                const float unit = __builtin_ldexpf(1.0f, -exponent);
+                const float unit = __builtin_ldexpf(1.0f, -(int)exponent);
                 u32x4 p;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -476,7 +493,8 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
                     l += x[j];
                     if constexpr (QUANT) {
                         vo_sum = fmaf(x[j], vo[j], vo_sum);
-                        x[j] *= F16 ? vs[j] * unit : vs[j];
+                        x[j] *= vs[j];
+                        if constexpr (F16) x[j] *= unit;
                     }
                 }
 #pragma unroll
@@ -506,7 +524,7 @@ __global__ __launch_bounds__(64 * WAVES, AHEAD ? 2 : 3) void attn_decode_kernel(
             float* ml = lds + WAVES * here * PAD;
             __syncthreads();                                            // (nobody reads what another piece left there)
             if (col_e < here) {
-                const float back = QUANT && F16 ? __builtin_ldexpf(1.0f, exponent) : 1.0f;
+                const float back = QUANT && F16 ? __builtin_ldexpf(1.0f, (int)exponent) : 1.0f;
                 float* to_lds = lds + (wave * here + col_e) * PAD;
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
