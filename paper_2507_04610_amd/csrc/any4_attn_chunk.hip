@@ -14,9 +14,9 @@
 // to LDS, exactly (k: c + kBias, v: c - kCentre), and scales and offsets are applied to sums, so that codes cost no rounding of their own:
 //     q . k_j = ks_j (q . c'_j) + (ko_j - kBias ks_j) sum(q)
 //     o = sum_j (p_j vs_j) (c_j - kCentre) + sum_j p_j (vo_j + kCentre vs_j)
-// bf16 queries become fp16 for that: a row is scaled by a power of two, which is exact down to 2^-31 of its largest value and off by 2^-39 of that
-// below.  The product p_j vs_j is rounded to fp16; the exponent of the largest product that a row has had is taken off it together with the running maximum (that of the
-// largest vs_j alone would leave nothing of the others beside a large value of no weight).
+// bf16 queries become fp16 for that: a row is scaled by a power of two, which is exact down to 2^-15 of its largest value and off by 2^-26 of that
+// below, less than the fp32 sums are.  The product p_j vs_j is rounded to fp16; the exponent of the largest product that a row has had is taken off it together
+// with the running maximum (that of the largest vs_j alone would leave nothing of the others beside a large value of no weight).
 //
 // Who does what.  Lengths are the device's, so each block finds its rows itself, of more than 64 requests in what a first launch of one block writes down
 // (a token each of 2048 requests over 300 tokens in 8 bits: 670 -> 441 us).  Where whole tiles of rows do not fill the chip, their keys are cut
@@ -390,6 +390,17 @@ __device__ __forceinline__ float difference(float a, float b) {
 __device__ __forceinline__ float with_maximum(float m, float e) { return fabsf(m) > kFar ? 0.0f : fminf(fmaxf(e, (float)-kFold), (float)kFold); }
 __device__ __forceinline__ int folded(float m, float e) { return (int)(e - with_maximum(m, e)); }
 
+// the largest of LANES lanes (32, the first, or 64), in all.  (No lane reads LDS for that, as shuffles do: others wait for the wavefront that is at a tile's scales.)
+template <int LANES> __device__ __forceinline__ float lanes_largest(float v) {
+    v = lanes_reduce<16>(v, [](float a, float b) { return fmaxf(a, b); });
+    auto before = [&](auto ctrl, auto rows) {
+        v = fmaxf(v, __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(v), __float_as_uint(v), decltype(ctrl)::value, decltype(rows)::value, 0xF, false)));
+    };
+    before(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});    // row_bcast:15
+    if constexpr (LANES == 64) before(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});    // row_bcast:31
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), LANES - 1));
+}
+
 // What is kept of a token's v for that: the exponent of its scale (of its middle times 2^-64 if that is more: a constant vector has scale 1 however large it is,
 // and its product with the weight is to stay in fp32's range), 2^kUp lower.
 __device__ __forceinline__ float exponent_of(float vs, float mid) {
@@ -399,11 +410,11 @@ __device__ __forceinline__ float exponent_of(float vs, float mid) {
 template <int BITS> struct Codes {
     static constexpr float kBias = BITS == 8 ? 1024.0f : 64.0f, kCentre = (float)(1 << (BITS - 1));
 };
-// k's scales and offsets in LDS are 2^-kDown of what they are where they come near fp32's end, kBias times as large (bf16), and q's scale 2^kDown times as large
-template <bool F16> constexpr float kDown = F16 ? 1.0f : 0x1p-4f;
-// Queries whose largest value lies below 2^kSmallQuery: their products with codes are brought back to their own size before they meet k's scale, as far as 2^120
-// (otherwise with the softmax scale, behind it)
-constexpr int kSmallQuery = -8;
+// Scores over codes of bf16 pass fp32 between q in fp16's range and the end, whatever the sizes of q and k: k's scales and offsets lie in LDS 2^kDown lower (exactly,
+// as every bf16 value does that far down), q's largest value lies at 2^kTop, so that its product with codes, their bias and the largest scale stays below 2^127; or, from
+// 2^kLarge on, where the scale that undoes all that has to stay there as well, at 2^kTopLarge.
+constexpr int kDown = 14, kTop = 1, kLarge = 32, kTopLarge = 15;
+template <bool F16> constexpr float kLowered = F16 ? 1.0f : 1.0f / (float)(1 << kDown);
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t add_f16(uint32_t x, float y) {
     return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, x) + f16x2{(_Float16)y, (_Float16)y});
@@ -504,10 +515,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
     // all rows see keys up to `all_lim` that lie at `all_lo` or behind it or are among the first
     const int all_lim = ahead + span.first, all_lo = max(ahead + span.last, 0) + 1 - a.window;
 
-    // Q^T, fp16 for codes: a row of bf16 is scaled by a power of two into the upper part of fp16's range
+    // Q^T, fp16 for codes: a row of bf16 is scaled by a power of two into fp16's range
     u32x4 q[QM];
     float scale = a.scale_log2, sum_q = 0.0f;
-    int back = 0, small = 0;                                    // of a small query; whether some row's is
     {
         const int head = (int)kv_head * a.shared + (row - query * a.shared);
         const uint16_t* qp = a.q.p + (int64_t)(w.r.q_at + query) * a.q.token + (int64_t)head * a.q.head;
@@ -526,11 +536,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(bf16lo_to_f32(q[i][j])), fabsf(bf16hi_to_f32(q[i][j]))));
                 top = fmaxf(top, other_half(top));
-                const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -113), 127);
-                const float by = __builtin_ldexpf(1.0f, 14 - e);
-                back = e < kSmallQuery ? e - 14 : 0;
-                small = __builtin_amdgcn_ballot_w64(back != 0) != 0ull ? 1 : 0;
-                scale *= (back != 0 ? 1.0f : __builtin_ldexpf(1.0f, e - 14)) / kDown<F16>;
+                const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 127), less = e - (e < kLarge ? kTop : kTopLarge);
+                const float by = __builtin_ldexpf(1.0f, -less);
+                scale = __builtin_ldexpf(scale, less + kDown);
 #pragma unroll
                 for (int i = 0; i < QM; ++i)
 #pragma unroll
@@ -541,7 +549,6 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) sum_q += h16lo_to_f32<true>(q[i][j]) + h16hi_to_f32<true>(q[i][j]);
             sum_q += other_half(sum_q);
-            if constexpr (!F16) sum_q = __builtin_ldexpf(sum_q, back);
             if constexpr (SOURCE == 4) {
 #pragma unroll
                 for (int i = 0; i < QM; ++i) {
@@ -686,7 +693,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
             }
             if (wave == (t & (kWaves - 1))) {
                 using C = Codes<CODES ? SOURCE : 8>;
-                const float ks = kDown<F16> * bf16lo_to_f32(raw.scales[0]), ko = kDown<F16> * bf16hi_to_f32(raw.scales[0]), vs = bf16lo_to_f32(raw.scales[1]), vo = bf16hi_to_f32(raw.scales[1]);
+                const float ks = kLowered<F16> * bf16lo_to_f32(raw.scales[0]), ko = kLowered<F16> * bf16hi_to_f32(raw.scales[0]), vs = bf16lo_to_f32(raw.scales[1]), vo = bf16hi_to_f32(raw.scales[1]);
                 const float mid = fmaf(C::kCentre, vs, vo);
                 const bool fine = fabsf(mid) < __builtin_inff();   // (a v without numbers counts for nothing here; see below)
                 const uint32_t aside = kAside + parity * kAsideBytes, to = aside + 4u * (uint32_t)lane;
@@ -696,9 +703,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 *(lds_f)(to + 512) = vs_used;
                 *(lds_f)(to + 768) = mid_used;
                 *(lds_f)(to + 1024) = high;
-                float big = lanes_reduce<16>(high, [](float u, float v) { return fmaxf(u, v); });
-                big = fmaxf(big, __shfl_xor(big, 16));
-                big = fmaxf(big, __shfl_xor(big, 32));
+                const float big = lanes_largest<64>(high);
                 const bool apart = __builtin_amdgcn_ballot_w64(vs_used != 0.0f && big - high > (float)kSpread) != 0ull;
                 const unsigned long long bad = __builtin_amdgcn_ballot_w64(!fine);
                 if (lane == 0) {
@@ -761,12 +766,6 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         }
         if constexpr (kFirst) __builtin_amdgcn_s_setprio(1);
         if constexpr (CODES) {
-            if (!F16 && seldom(small != 0)) {
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[u][r] = __builtin_ldexpf(s[u][r], back);
-            }
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -890,14 +889,22 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                         v_sum = fmaf(e[r], vo[r], v_sum);
                         e[r] *= vs[r];
                     }
-                    if (seldom(folds != 0)) {                    // (off the product: a scale alone may lie further from the largest product than fp32 reaches)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) e[r] = __builtin_ldexpf(e[r], -folded(m_ref, exponent));
-                    }
                 }
-                p[2 * u + (c >> 1)][2 * (c & 1)] = pack<MMA16>(e[0], e[1]);
-                p[2 * u + (c >> 1)][2 * (c & 1) + 1] = pack<MMA16>(e[2], e[3]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[u][4 * c + r] = e[r];
             }
+        // (off the products: a scale alone may lie further from the largest product than fp32 reaches)
+        if (CODES && seldom(folds != 0)) {
+            const int less = -folded(m_ref, exponent);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[u][r] = __builtin_ldexpf(s[u][r], less);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int x = 0; x < 8; ++x) p[2 * u + (x >> 2)][x & 3] = pack<MMA16>(s[u][2 * x], s[u][2 * x + 1]);
 
         // 0 times what is not finite would be NaN: tokens with such a v (in tiles that not all rows see, with codes in all) are added one by one to
         // the rows that see them, and are zeros in the product.
@@ -1138,7 +1145,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 }
             }
             using C = Codes<BITS>;
-            const float ks = kDown<F16> * bf16lo_to_f32(raw_scales[0]), ko = kDown<F16> * bf16hi_to_f32(raw_scales[0]), vs = bf16lo_to_f32(raw_scales[1]), vo = bf16hi_to_f32(raw_scales[1]);
+            const float ks = kLowered<F16> * bf16lo_to_f32(raw_scales[0]), ko = kLowered<F16> * bf16hi_to_f32(raw_scales[0]), vs = bf16lo_to_f32(raw_scales[1]), vo = bf16hi_to_f32(raw_scales[1]);
             const float mid = fmaf(C::kCentre, vs, vo);
             const bool fine = fabsf(mid) < __builtin_inff();
             const float vs_used = fine ? vs : 0.0f, mid_used = fine ? mid : 0.0f, high = exponent_of(vs_used, mid_used);
@@ -1151,8 +1158,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
                 *(lds_f)(at + 512) = high;
             }
             // (lanes from 32 on have no tokens: scales of 0)
-            float big = lanes_reduce<16>(high, [](float u, float v) { return fmaxf(u, v); });
-            big = fmaxf(big, __shfl_xor(big, 16));
+            const float big = lanes_largest<32>(high);
             const bool apart = __builtin_amdgcn_ballot_w64(vs_used != 0.0f && big - high > (float)kSpread) != 0ull;
             const unsigned long long bad = __builtin_amdgcn_ballot_w64(!fine && lane < 32);
             if (lane == 0) {
