@@ -19,21 +19,23 @@
 // with the running maximum (that of the largest vs_j alone would leave nothing of the others beside a large value of no weight).
 //
 // Who does what.  Lengths are the device's, so each block finds its rows itself, of more than 64 requests in what a first launch of one block writes down
-// (a token each of 2048 requests over 300 tokens in 8 bits: 670 -> 441 us).  Where whole tiles of rows do not fill the chip, their keys are cut
+// (a token each of 2048 requests over 300 tokens in 8 bits: 449 us, 670 if each block looks).  Where whole tiles of rows do not fill the chip, their keys are cut
 // into pieces, no more than it takes; pieces leave sums, maximum and sum of weights in the workspace, and a last launch joins them (3 to 5 us: short
 // calls are not cut).
 //
 // Rounding: scores, maxima, sums and accumulators are fp32; the weights (times vs_j) are rounded to 16 bits for the matrix cores, once.
 //
 // Measured, 8 KV heads, us (what bounds it):
-//     16 bits, 2048 tokens behind 30 k, 32 query heads of 128      1005 - 1040  (1.05 PFLOP/s: matrix cores busy 51 %, vector units 51 %;
+//     16 bits, 2048 tokens behind 30720, 32 query heads of 128     1005 - 1040  (1.05 PFLOP/s: matrix cores busy 49 %, vector units 49 %;
 //                                                                               wavefronts wait 27 % of their time for LDS and each other)
-//     8 bits, 24 requests of 1 .. 511 tokens, fp16                  414 - 440   (0.57 PFLOP/s: vector units busy 47 %, LDS 37 %, matrix cores 24 %; 6.2 of 8
+//     the same, window of 4096 and first 4                           154 - 159  (0.89 PFLOP/s)
+//     the same over 8 and 4 bits, bf16                     1405 - 1430, 1385 - 1410  (0.75 and 0.76 PFLOP/s); 8 bits with the window 205 (0.67)
+//     8 bits, 24 requests of 1 .. 511 tokens, fp16                   410 - 430  (0.57 PFLOP/s: vector units busy 50 %, LDS 37 %, matrix cores 24 %; 6.5 of 8
 //                                                                               wavefronts there on average, which wait 31 % of their time)
-//     4 bits, 16 requests, up to 8 drafted tokens                    64 -  67   (2.2 TB/s: vector units 51 %; 5 of it the join; 5.6 of 8 wavefronts)
-//     16 bits, 19 tokens behind 333                                   9.1       (loads that wait for each other: starts, lengths, page, k and v)
-//     packed rows, a prompt of 12011, window 2048                   412         (0.90 PFLOP/s)
-//     packed rows, fp16, 8450 tokens, 16 heads of 64 on 2, window 777  55       (0.49 PFLOP/s: 1060 blocks of 13 tiles of keys, whose beginnings and
+//     4 bits, 16 requests, up to 8 drafted tokens                     63 -  68  (2.2 TB/s: vector units 51 %; 5 of it the join; 5.6 of 8 wavefronts)
+//     16 bits, 19 tokens behind 333                                   9.5       (loads that wait for each other: starts, lengths, page, k and v)
+//     packed rows, a prompt of 12011, window 2048                   412 - 418   (0.89 PFLOP/s)
+//     packed rows, fp16, 8450 tokens, 16 heads of 64 on 2, window 777  54       (0.50 PFLOP/s: 1060 blocks of 13 tiles of keys, whose beginnings and
 //                                                                               ends and the second round of them cost as much as the tiles)
 // Without gain: longest pieces first, more and smaller pieces than fill the chip, a fixed priority for one of a SIMD's wavefronts, an order of loads and products
 // prescribed to the compiler, a closer search for the length of pieces.
@@ -51,14 +53,15 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves, kRowTile = 32 * kWaves;
 // Costs are counted in tiles of keys for 32 rows.  Figures: us with 32 query heads on 8 KV heads of 128, 16 bits unless said otherwise.
 constexpr int kNarrow = 4;                                      // so many take as long as one for 128
 constexpr int kFewRows = 64;                                    // requests of up to so many rows have tiles of 32, as small calls (65 requests of 64 rows
-                                                                // over 1000 tokens in 8 bits: 81 us, in tiles of 128 98)
-// Least of a piece.  19 tokens behind 1000: 13.6, with 8 15.8, with 16 18; one token behind 8000 16.5, 15.8, 20.5.
+                                                                // over 1000 tokens in 8 bits: 78 us, in tiles of 128 94)
+// Least of a piece.  19 of 1000 tokens: 12.6, with 8 14.4, with 16 17.9; one of 8000 16.1, 15.6, 19.1.
 constexpr int kLeastPiece = 4;
-// Tiles of 32 rows, of 128 rows, of so much are not cut: writing pieces and joining them costs as much.  19 tokens behind 700 (11 tiles): whole 12.9, cut 13.5; behind
-// 1000 whole 15.4, cut 13.6; behind 1500 whole 20.0, cut 13.7.  (Where no request can have more, the join is not launched either.)
+// Tiles of 32 rows, of 128 rows, of so much are not cut: writing pieces and joining them costs as much.  19 of 700 tokens (11 tiles): whole 13.2, cut 12.5; of 1000
+// whole 15.8, cut 12.6; of 1500 whole 20.6, cut 13.0.  Where no request can have more, the join is not launched either (1024 of 1024 tokens 30.3, with a join of nothing 33;
+// 64 requests of a token of 1000 in 8 bits 28.4 and 33.3).
 constexpr int kWholeFew = 12, kWhole = 40;
-// Calls of so much for 128 rows at a time take 32 at a time: more blocks, each done sooner.  19 tokens behind 32000: 40, with 4096 55; 512 tokens from the
-// beginning 12.9, 18; 4 requests of 100 of 1000 tokens in 8 bits 34, 48; but 512 behind 7488 98, with 65536 117, and 2048 from the beginning 67, 90.
+// Calls of so much for 128 rows at a time take 32 at a time: more blocks, each done sooner.  19 of 32000 tokens: 38.9, with 4096 50.2; 512 of 512 13.0, 18.1; 4 requests
+// of 100 of 1000 tokens in 8 bits 30.9, 35.2; but 512 of 8000 86, with 65536 111, and 2048 of 2048 61.6, 81.3.
 constexpr int kSmall = 16384;
 constexpr int kNoWindow = 0x7FFFF800;                           // more than any request's tokens
 // Codes: what is taken off the exponents of the products p_j vs_j goes with the maximum as far as 2^+-kFold: beyond, weights of tokens whose scales differ by 2^126 and

@@ -37,8 +37,8 @@
 //     4 bits, one request of 131071 tokens, 64 query heads                  39   (3.7 TB/s; 3 us until the first bytes are asked for, 6 for the
 //                                                                                join of 32 pieces; vector units busy half of the time)
 //     16 bits, one request of 333 tokens, 32 query heads                     8.3 (loads that wait for each other: length, page, k and v)
-//     16 bits, 48 requests of 1 .. 32768 tokens, window 4096, 32 query heads 124 (6.0 TB/s)
-//     4 bits, fp16, one request, window, heads of 64                         10.8
+//     16 bits, 48 requests of 1 .. 32768 tokens, window 4096, 32 query heads 124 (6.0 TB/s; over 8 bits 76, 5.1 TB/s, over 4 bits 52, 3.9 TB/s)
+//     4 bits, fp16, one request, window, heads of 64                         10.9
 #include "any4_attn.h"
 #include "any4_internal.h"
 #include "any4_splitk.h"

@@ -14,6 +14,7 @@
 //
 // Measured, 32 query and 8 KV heads of 128 unless said otherwise, us:
 //     16384 tokens with norms into a cache of 8 bits             82   (4.9 TB/s, as a copy; vector units busy 73 %.  Loads when a head is worked on 98)
+//     the same into a cache of 4 bits, and read back             98  (into 8 bits 103, 82 of it the write)
 //     5001 tokens, three axes, norms, fp16, q and k alone        20 in the kernel, 25 with the call's gaps (5.1 and 4.0 TB/s)
 //     45 tokens, 16 and 2 heads, no norms; 16 tokens, 16 bits    3 and 4 in the kernel, 5 with the call (loads that wait for each other: position, frequency)
 #include "any4_attn.h"
