@@ -29,8 +29,8 @@
 //     16 bits, 2048 tokens behind 30720, 32 query heads of 128     1005 - 1040  (1.05 PFLOP/s: matrix cores busy 49 %, vector units 49 %;
 //                                                                               wavefronts wait 27 % of their time for LDS and each other)
 //     the same, window of 4096 and first 4                           154 - 159  (0.89 PFLOP/s)
-//     the same over 8 and 4 bits, bf16                     1405 - 1430, 1385 - 1410  (0.75 and 0.76 PFLOP/s); 8 bits with the window 205 (0.67)
-//     8 bits, 24 requests of 1 .. 511 tokens, fp16                   410 - 430  (0.57 PFLOP/s: vector units busy 50 %, LDS 37 %, matrix cores 24 %; 6.5 of 8
+//     the same over 8 and 4 bits, bf16                     1405 - 1480, 1385 - 1445  (0.72 - 0.77 PFLOP/s); 8 bits with the window 205 (0.67)
+//     8 bits, 24 requests of 1 .. 511 tokens, fp16                   410 - 435  (0.57 PFLOP/s: vector units busy 50 %, LDS 37 %, matrix cores 24 %; 6.5 of 8
 //                                                                               wavefronts there on average, which wait 31 % of their time)
 //     4 bits, 16 requests, up to 8 drafted tokens                     63 -  68  (2.2 TB/s: vector units 51 %; 5 of it the join; 5.6 of 8 wavefronts)
 //     16 bits, 19 tokens behind 333                                   9.5       (loads that wait for each other: starts, lengths, page, k and v)
@@ -65,7 +65,7 @@ constexpr int kWholeFew = 12, kWhole = 40;
 constexpr int kSmall = 16384;
 constexpr int kNoWindow = 0x7FFFF800;                           // more than any request's tokens
 // Codes: what is taken off the exponents of the products p_j vs_j goes with the maximum as far as 2^+-kFold: beyond, weights of tokens whose scales differ by 2^126 and
-// more would be lost to the sum of weights.  The rest is taken off vs_j itself.
+// more would be lost to the sum of weights.  The rest is taken off the products themselves.
 constexpr int kFold = 40;
 // The largest product stands 2^kUp above 1 (2^kSlack more at most, below 2^15 in all): fp16 has steps of 2^-24 down there, and tokens of small weight are many.
 constexpr int kUp = 6;
@@ -389,7 +389,7 @@ __device__ __forceinline__ float difference(float a, float b) {
 #pragma clang fp contract(off)
     return a - b;
 }
-// Of the exponent taken off products: with the maximum m, and off vs_j.  (All of it there where m is far, or without a score yet -inf: a sum with m would round it away.)
+// Of the exponent taken off products: with the maximum m, and off the products themselves.  (All of it there where m is far, or without a score yet -inf: a sum with m would round it away.)
 __device__ __forceinline__ float with_maximum(float m, float e) { return fabsf(m) > kFar ? 0.0f : fminf(fmaxf(e, (float)-kFold), (float)kFold); }
 __device__ __forceinline__ int folded(float m, float e) { return (int)(e - with_maximum(m, e)); }
 
@@ -414,8 +414,8 @@ template <int BITS> struct Codes {
     static constexpr float kBias = BITS == 8 ? 1024.0f : 64.0f, kCentre = (float)(1 << (BITS - 1));
 };
 // Scores over codes of bf16 pass fp32 between q in fp16's range and the end, whatever the sizes of q and k: k's scales and offsets lie in LDS 2^kDown lower (exactly,
-// as every bf16 value does that far down), q's largest value lies at 2^kTop, so that its product with codes, their bias and the largest scale stays below 2^127; or, from
-// 2^kLarge on, where the scale that undoes all that has to stay there as well, at 2^kTopLarge.
+// as every bf16 value does that far down), q's largest value lies at 2^kTop, so that its product with codes, their bias and the largest scale stays below 2^127; or, where
+// with the softmax scale it comes to 2^kLarge and more, so that what undoes all that has to stay there as well, at 2^kTopLarge.
 constexpr int kDown = 14, kTop = 1, kLarge = 32, kTopLarge = 15;
 template <bool F16> constexpr float kLowered = F16 ? 1.0f : 1.0f / (float)(1 << kDown);
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -539,7 +539,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(bf16lo_to_f32(q[i][j])), fabsf(bf16hi_to_f32(q[i][j]))));
                 top = fmaxf(top, other_half(top));
-                const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 127), less = e - (e < kLarge ? kTop : kTopLarge);
+                const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 127), of_scale = (int)(__float_as_uint(scale) >> 23) - 127;
+                const int less = e - (e + of_scale < kLarge ? kTop : kTopLarge);
                 const float by = __builtin_ldexpf(1.0f, -less);
                 scale = __builtin_ldexpf(scale, less + kDown);
 #pragma unroll
@@ -837,7 +838,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
         if (seldom(__builtin_amdgcn_ballot_w64(moved) != 0ull)) {
             const float m_new = moved ? higher : m_ref;
             if constexpr (CODES) {
-                // (sums are relative to m_used, o to that and what is taken off vs; without a score yet they are zeros)
+                // (sums are relative to m_used, o to that and what is taken off the products; without a score yet they are zeros)
                 const float before = m_ref == -__builtin_inff() ? m_ref : m_used;
                 const int was = folded(m_ref, exponent);
                 exponent = moved ? fmaxf(fmaxf(floorf(exponent + (m_ref - m_new)), ceilf(product)), -300.0f) : exponent;   // (down, or it would rise with every move)

@@ -140,6 +140,16 @@ def test_small_queries_of_large_keys(bits, parts, q_by, k_by):
 
 
 @pytest.mark.parametrize("bits", (8, 4))
+@pytest.mark.parametrize("parts", PARTS)
+@pytest.mark.parametrize("q_by,k_by,scale", [(1.0, 1e-35, 3e35), (1e-18, 1e-17, 1e35), (1e20, 1e15, 1e-35), (1e-5, 1e30, 1e-25)])
+def test_softmax_scales_of_any_size(bits, parts, q_by, k_by, scale):
+    p = Chunks(PARTS[parts], bits, BF16, 128, 8, 2, 64, seed=37, q_by=q_by, k_by=k_by)
+    out = p.run(softmax_scale=scale)
+    assert out.isfinite().all()
+    check(p, out, scale=scale)
+
+
+@pytest.mark.parametrize("bits", (8, 4))
 @pytest.mark.parametrize("dtype,v_by", [(F16, 1e-3), (F16, 100.0), (BF16, 1e-10), (BF16, 1.0), (BF16, 1e8), (BF16, 1e30)])
 @pytest.mark.parametrize("parts", PARTS)
 def test_far_scores_that_are_alike(bits, dtype, v_by, parts):
