@@ -891,24 +891,27 @@ __global__ __launch_bounds__(kThreads, 2) void attn_chunk_kernel(Args a) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         v_sum = fmaf(e[r], vo[r], v_sum);
-                        e[r] *= vs[r];
+                        s[u][4 * c + r] = e[r] * vs[r];
                     }
+                } else {
+                    p[2 * u + (c >> 1)][2 * (c & 1)] = pack<MMA16>(e[0], e[1]);
+                    p[2 * u + (c >> 1)][2 * (c & 1) + 1] = pack<MMA16>(e[2], e[3]);
                 }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[u][4 * c + r] = e[r];
             }
-        // (off the products: a scale alone may lie further from the largest product than fp32 reaches)
-        if (CODES && seldom(folds != 0)) {
-            const int less = -folded(m_ref, exponent);
+        if constexpr (CODES) {
+            // (off the products: a scale alone may lie further from the largest product than fp32 reaches)
+            if (seldom(folds != 0)) {
+                const int less = -folded(m_ref, exponent);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[u][r] = __builtin_ldexpf(s[u][r], less);
+            }
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[u][r] = __builtin_ldexpf(s[u][r], less);
+                for (int x = 0; x < 8; ++x) p[2 * u + (x >> 2)][x & 3] = pack<MMA16>(s[u][2 * x], s[u][2 * x + 1]);
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int x = 0; x < 8; ++x) p[2 * u + (x >> 2)][x & 3] = pack<MMA16>(s[u][2 * x], s[u][2 * x + 1]);
 
         // 0 times what is not finite would be NaN: tokens with such a v (in tiles that not all rows see, with codes in all) are added one by one to
         // the rows that see them, and are zeros in the product.
