@@ -26,7 +26,7 @@
 // Rounding: scores, maxima, sums and accumulators are fp32; the weights (times vs_j) are rounded to 16 bits for the matrix cores, once.
 //
 // Measured, 8 KV heads, us (what bounds it):
-//     16 bits, 2048 tokens behind 30720, 32 query heads of 128     1005 - 1040  (1.05 PFLOP/s: matrix cores busy 49 %, vector units 49 %;
+//     16 bits, 2048 tokens behind 30720, 32 query heads of 128     1005 - 1055  (1.01 - 1.06 PFLOP/s: matrix cores busy 49 %, vector units 49 %;
 //                                                                               wavefronts wait 27 % of their time for LDS and each other)
 //     the same, window of 4096 and first 4                           154 - 159  (0.89 PFLOP/s)
 //     the same over 8 and 4 bits, bf16                     1405 - 1480, 1385 - 1445  (0.72 - 0.77 PFLOP/s); 8 bits with the window 205 (0.67)
@@ -34,7 +34,7 @@
 //                                                                               wavefronts there on average, which wait 31 % of their time)
 //     4 bits, 16 requests, up to 8 drafted tokens                     63 -  68  (2.2 TB/s: vector units 51 %; 5 of it the join; 5.6 of 8 wavefronts)
 //     16 bits, 19 tokens behind 333                                   9.5       (loads that wait for each other: starts, lengths, page, k and v)
-//     packed rows, a prompt of 12011, window 2048                   412 - 418   (0.89 PFLOP/s)
+//     packed rows, a prompt of 12011, window 2048                   412 - 425   (0.88 - 0.90 PFLOP/s)
 //     packed rows, fp16, 8450 tokens, 16 heads of 64 on 2, window 777  54       (0.50 PFLOP/s: 1060 blocks of 13 tiles of keys, whose beginnings and
 //                                                                               ends and the second round of them cost as much as the tiles)
 // Without gain: longest pieces first, more and smaller pieces than fill the chip, a fixed priority for one of a SIMD's wavefronts, an order of loads and products
